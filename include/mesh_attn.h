@@ -373,6 +373,194 @@ ma_status_t mesh_attn_tile_bwd(const ma_problem_t* prob, const int32_t* q_idx,
                                float* dv, int32_t accumulate, void* ws,
                                size_t ws_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Paged key/value cache in 4 bits: what one GPU keeps of K and V after a
+ * prompt, and the attention of new queries over it.
+ *
+ * A cache is num_pages pages; a page holds page_size stored tokens of every KV
+ * head.  A sequence (request) owns the pages listed in its row of the block
+ * table: its stored token r is token r % page_size of page
+ * block_table[b][r / page_size], and slot page * page_size + r % page_size.
+ * Of n GPUs that share the sequences, partition p stores the positions
+ * p, p + n, p + 2n, .. (MA_LAYOUT_STRIPED; n = 1 stores everything) or
+ * p * P .. p * P + P - 1 (MA_LAYOUT_CONTIGUOUS), in that order; the other
+ * GPUs' partial (O, LSE) of the same queries are folded by
+ * mesh_attn_lse_merge.
+ *
+ * Every 32 consecutive dims of a stored K or V row are a group: 32 four-bit
+ * E2M1 values (sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6) and one scale byte c that
+ * stands for 2^(c - 127), c = 255 for a group that is all NaN.  A (page, KV
+ * head) block is page_size * (d + d / 16) bytes:
+ *   K codes   [page_size][d/2]            byte j: dim 2j (low four bits), 2j + 1
+ *   V codes   [page_size/8][16][8][d/32]  token 8a + c, dims n * d/16 .. at
+ *                                         [a][n][c]: the eight tokens of a
+ *                                         matrix operand lie together
+ *   K scales  [page_size][d/32]
+ *   V scales  [d/32][page_size]
+ * and the cache is [num_pages][num_kv_heads] of them, 16-byte aligned.
+ * mesh_attn_cache_append writes scale codes 1 .. 252 and 255 only; bytes of
+ * slots that were never written may hold anything.
+ *
+ * Lengths, tables and slots are device arrays, so that a captured step serves
+ * every batch that fits its sizes.  The kernels check what they read there:
+ * nothing outside the buffers is touched whatever it is.  None of these calls
+ * keeps state, allocates, or uses host memory after it returns, so all may be
+ * captured into graphs (unlike the tile calls with workspaces); a workspace
+ * serves one call, or one replay, at a time.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t num_pages;      /* >= 1; num_pages * page_size <= 2^40             */
+  int32_t page_size;      /* stored tokens per page: 16, 32, 64, 128 or 256  */
+  int32_t num_kv_heads;   /* 1 .. 1024                                       */
+  int32_t head_dim;       /* 64 or 128                                       */
+  int32_t max_pages;      /* entries of a request's block table row, >= 1;
+                             max_pages * page_size <= 2^30                   */
+  int32_t layout;         /* an ma_layout_t: which positions are stored here */
+  int32_t num_partitions; /* n >= 1                                          */
+  int32_t partition;      /* p in [0, n)                                     */
+  int32_t partition_len;  /* P >= 1 (MA_LAYOUT_CONTIGUOUS only)              */
+} ma_cache_t;
+
+/* Most requests of one call. */
+#define MA_CACHE_MAX_REQUESTS 4096
+
+/* Bytes of the cache; 0 for an invalid description. */
+size_t mesh_attn_cache_bytes(const ma_cache_t* cache);
+
+/* Block tables, slots and positions of a step from the requests' lengths, in
+ * one launch.  Request b has lens[b] tokens and gets new_lens[b] more
+ * (negative counts as 0), whose rows lie packed in request order: rows
+ * cu_new[b] .. cu_new[b + 1] - 1.  The pages that its stored tokens then need
+ * are taken, in request order, from free_pages[free_range[0] ..
+ * free_range[1] - 1] (clipped to num_free).  A request is refused if its pages
+ * exceed max_pages or, with those of the requests before it, the free ones, or
+ * if its length would pass 2^31 - 1: it gets no page, its length stays, its
+ * rows have slot and position -1.
+ *   lens, new_lens  [num_requests] int32 device.
+ *   free_pages      [num_free] int32 device, page numbers.
+ *   free_range      [2] int32 device;  free_range_out [2]: after this step.
+ *   block_table     [num_requests][max_pages] int32 device, in and out: the
+ *                   entries of the new pages are written, no other.
+ *   lens_out        [num_requests] int32: lens + new_lens (lens if refused).
+ *   cu_new          [num_requests + 1] int32 (capped at 2^31 - 1).
+ *   slots           [rows] int64: where row r's K, V go; -1 for a row whose
+ *                   position another GPU stores, whose page number is not in
+ *                   [0, num_pages), or behind the last request.
+ *   positions       [rows] int32: row r's position in its sequence; -1 behind
+ *                   the last request.
+ *   refused         [1] int32: number of refused requests.
+ * rows may be larger or smaller than the number of new tokens (rows past it
+ * get -1; tokens past rows get no slot).  Outputs must not alias inputs: a
+ * loop of steps alternates between two buffers each for the lengths and the
+ * free range. */
+ma_status_t mesh_attn_cache_tables(
+    const ma_cache_t* cache, int32_t num_requests, const int32_t* lens,
+    const int32_t* new_lens, const int32_t* free_pages, int32_t num_free,
+    const int32_t* free_range, int32_t* block_table, int32_t* lens_out,
+    int32_t* cu_new, int64_t rows, int64_t* slots, int32_t* positions,
+    int32_t* free_range_out, int32_t* refused, hipStream_t stream);
+
+/* Stores rows of K and V in 4 bits.
+ *   k, v   row r, head h at k + r * k_stride + h * head_dim, bf16 device; the
+ *          strides are in elements, multiples of 8, >= Hkv * d (slices of a
+ *          fused projection's output).
+ *   slots  [rows] int64 device; a slot outside [0, num_pages * page_size)
+ *          stores nothing.  If two rows have the same slot, either's bytes may
+ *          be there.
+ *   data   the cache.
+ * A group's scale is 2^e with e = floor(log2 amax) - 2, plus 1 where amax >
+ * 1.75 * 2^floor(log2 amax), clipped to [-126, 125]; its values are
+ * x * 2^-e rounded to the nearest E2M1 value, ties to the even code, at most 6
+ * in magnitude: off by at most half a step wherever e was not clipped.  A
+ * group with an infinity or a NaN is stored as NaN, one of zeros with e =
+ * -126. */
+ma_status_t mesh_attn_cache_append(const ma_cache_t* cache, int64_t rows,
+                                   const void* k, int64_t k_stride,
+                                   const void* v, int64_t v_stride,
+                                   const int64_t* slots, void* data,
+                                   hipStream_t stream);
+
+/* Reads stored rows back, exactly, as bf16 [rows][Hkv][d]: the KV buffer of
+ * the tile calls (a cached prefix under a new tile).  Rows whose slot is out of
+ * range are 0. */
+ma_status_t mesh_attn_cache_read(const ma_cache_t* cache, int64_t rows,
+                                 const int64_t* slots, const void* data,
+                                 void* k, void* v, hipStream_t stream);
+
+/* Device workspace bytes of mesh_attn_cache_fwd (0 if it needs none, or for
+ * invalid arguments); at most 68 MB.  Never less for more rows or requests. */
+size_t mesh_attn_cache_fwd_workspace_size(const ma_cache_t* cache,
+                                          int32_t num_q_heads,
+                                          int32_t num_requests, int64_t rows);
+
+/* Attention of packed query rows over the stored keys of their requests.
+ *   q          row r, head h at q + r * q_stride + h * d, bf16 device; the
+ *              stride is in elements, a multiple of 8, >= Hq * d.
+ *   positions  [rows] int32 device: row r sees the stored keys whose position
+ *              is not larger; a negative one sees none.
+ *   cu_new     [num_requests + 1] int32 device, not decreasing: request b's
+ *              rows are cu_new[b] .. cu_new[b + 1] - 1 (clipped to rows).
+ *   lens       [num_requests] int32 device: length of the sequence so far, the
+ *              new tokens included; keys at positions >= lens[b] are not seen.
+ *   block_table [num_requests][max_pages] int32 device.  Keys of a page whose
+ *              entry is outside [0, num_pages), or past max_pages, are not seen.
+ *   data       the cache.
+ *   o          [rows][Hq][d] device, bf16 or float32 (a partial to be merged
+ *              exactly later).
+ *   lse        [Hq][rows] float32 device, natural log; -inf for a row that
+ *              sees no key, whose O row is 0.
+ * Rows of no request are left as they were.  O and LSE are those of
+ * mesh_attn_tile_fwd over the stored values: exact products, float32
+ * accumulation and softmax; the probabilities enter the second product in bf16
+ * for a bf16 O, and as a sum of two bf16 for a float32 O.  A NaN key or value
+ * reaches the rows that see it and no other.  A split of the keys over
+ * workgroups depends on the sizes and lengths alone: equal calls give equal
+ * bits. */
+ma_status_t mesh_attn_cache_fwd(
+    const ma_cache_t* cache, int32_t num_q_heads, float softmax_scale,
+    int32_t num_requests, int64_t rows, const void* q, int64_t q_stride,
+    const int32_t* positions, const int32_t* cu_new, const int32_t* lens,
+    const int32_t* block_table, const void* data, void* o, ma_dtype_t o_dtype,
+    float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Rotary positions with several axes, of Q and K together.
+ *
+ * The first rotary_dim dims of every head are pairs (a, b): dims i and
+ * i + rotary_dim/2, or 2i and 2i + 1 (interleaved).  Pair i turns by
+ * positions[axis[i]][row] * inv_freq[i]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin);
+ * inverse = 1 turns it back, which is also the gradient.  The other dims are
+ * copied.  Angles are reduced exactly (64-bit fractions of a turn), so far
+ * positions are as accurate as near ones.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int32_t head_dim;       /* a multiple of 16, at most 256                   */
+  int32_t rotary_dim;     /* a multiple of 16, 16 .. head_dim                */
+  int32_t num_axes;       /* 1 .. 8                                          */
+  int32_t interleaved;    /* 0 or 1                                          */
+  const double* inv_freq; /* host [rotary_dim/2], radians per position, finite
+                             and below 2^31 in magnitude                     */
+  const int32_t* axis;    /* host [rotary_dim/2], in [0, num_axes); may be
+                             NULL for one axis                               */
+} ma_rope_t;
+
+/*   positions  [num_axes][rows] int32 device (any value).
+ *   q, k       row r, head h at q + r * q_stride + h * head_dim; strides in
+ *              elements, whole 16-byte units, >= heads * head_dim; dtype bf16
+ *              or float32 for all four (the tile backward's dQ, dK are
+ *              float32).  k_heads may be 0.
+ *   q_out, k_out  as q, k with strides of their own; q_out may be q with the
+ *              same stride, k_out k (in place), and must not overlap them
+ *              otherwise. */
+ma_status_t mesh_attn_rope(const ma_rope_t* rope, int64_t rows,
+                           const int32_t* positions, int32_t q_heads,
+                           const void* q, int64_t q_stride, void* q_out,
+                           int64_t q_out_stride, int32_t k_heads,
+                           const void* k, int64_t k_stride, void* k_out,
+                           int64_t k_out_stride, ma_dtype_t dtype,
+                           int32_t inverse, hipStream_t stream);
+
 /* Text of the last non-OK status returned on the calling thread ("" if none).
  * The pointer stays valid until the next library call on that thread. */
 const char* mesh_attn_last_error(void);

@@ -20,6 +20,8 @@ against the paper by eye, not for speed:
 * ``worklist``   -- classification of the tile's (Q block, KV block) pairs into
   empty / partially masked / fully visible (causal rule of Section 3.7) and the
   canonical run list built from it.
+* ``cache``      -- the paged 4-bit key/value cache (quantization, layout, page
+  tables), attention over it and rotary positions.
 * ``tiling``     -- the Q/KV partition index lists of a GPU's tile under basic
   2-D tiling (Section 3.2) and under KV Partition Rotation (Section 3.3).
 
@@ -51,4 +53,5 @@ from .worklist import (  # noqa: F401
     run_list,
     kv_major_run_list,
 )
+from . import cache  # noqa: F401
 from .tiling import basic_tile, kvr_tile  # noqa: F401

@@ -34,7 +34,18 @@ from ._binding import (  # noqa: F401
     mesh_attn_chunk_bwd_workspace_size,
     mesh_attn_chunk_bwd,
     mesh_attn_goo_plan,
+    mesh_attn_cache_bytes,
+    mesh_attn_cache_tables,
+    mesh_attn_cache_append,
+    mesh_attn_cache_read,
+    mesh_attn_cache_fwd_workspace_size,
+    mesh_attn_cache_fwd,
+    mesh_attn_rope,
     mesh_attn_last_error,
+    Cache,
+    Rope,
+    MA_LAYOUT_CONTIGUOUS,
+    MA_LAYOUT_STRIPED,
     Chunk,
     GooStep,
     MA_GOO_NONE,

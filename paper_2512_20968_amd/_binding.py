@@ -89,11 +89,71 @@ MA_GOO_NONE, MA_GOO_AG_Q, MA_GOO_AG_KV, MA_GOO_RS_Q = 0, 1, 2, 3
 GOO_KIND_NAMES = {MA_GOO_AG_Q: "AG-Q", MA_GOO_AG_KV: "AG-KV",
                   MA_GOO_RS_Q: "RS-Q"}
 
+
+class Cache(ctypes.Structure):
+    """ma_cache_t: a paged key/value cache in 4 bits and the positions of a
+    sequence it stores.  ``Cache.make`` takes a mapping with the field names;
+    without a layout a cache stores every position."""
+    _fields_ = [("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32),
+                ("layout", ctypes.c_int32),
+                ("num_partitions", ctypes.c_int32),
+                ("partition", ctypes.c_int32),
+                ("partition_len", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, cache):
+        if isinstance(cache, Cache):
+            return cache
+        return cls(num_pages=int(cache["num_pages"]),
+                   page_size=int(cache["page_size"]),
+                   num_kv_heads=int(cache["num_kv_heads"]),
+                   head_dim=int(cache["head_dim"]),
+                   max_pages=int(cache["max_pages"]),
+                   layout=int(cache.get("layout", MA_LAYOUT_STRIPED)),
+                   num_partitions=int(cache.get("num_partitions", 1)),
+                   partition=int(cache.get("partition", 0)),
+                   partition_len=int(cache.get("partition_len", 0)))
+
+
+class Rope(ctypes.Structure):
+    """ma_rope_t.  ``Rope.make`` takes a mapping with the field names
+    (``interleaved`` and, for one axis, ``axis`` may be left out)."""
+    _fields_ = [("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32),
+                ("num_axes", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32),
+                ("inv_freq", ctypes.POINTER(ctypes.c_double)),
+                ("axis", ctypes.POINTER(ctypes.c_int32))]
+
+    @classmethod
+    def make(cls, rope):
+        if isinstance(rope, Rope):
+            return rope
+        rot, axes = int(rope["rotary_dim"]), int(rope.get("num_axes", 1))
+        freq = [float(x) for x in rope["inv_freq"]]
+        axis = rope.get("axis")
+        axis = [0] * len(freq) if axis is None and axes == 1 else list(axis)
+        if len(freq) != rot // 2 or len(axis) != rot // 2:
+            raise ValueError(f"inv_freq and axis need rotary_dim / 2 = "
+                             f"{rot // 2} entries, got {len(freq)} and "
+                             f"{len(axis)}")
+        # ctypes keeps the arrays alive with the structure.
+        return cls(head_dim=int(rope["head_dim"]), rotary_dim=rot,
+                   num_axes=axes, interleaved=int(rope.get("interleaved", 0)),
+                   inv_freq=(ctypes.c_double * len(freq))(*freq),
+                   axis=(ctypes.c_int32 * len(axis))(*map(int, axis)))
+
+
 _i32 = ctypes.c_int32
 _i64 = ctypes.c_int64
 _p = ctypes.c_void_p
 _sz = ctypes.c_size_t
 _PROB = ctypes.POINTER(Problem)
+_CACHE = ctypes.POINTER(Cache)
 _I32P = ctypes.POINTER(ctypes.c_int32)
 
 _SIGNATURES = {
@@ -130,6 +190,19 @@ _SIGNATURES = {
                                   ctypes.POINTER(ctypes.c_double),
                                   ctypes.c_double, ctypes.POINTER(GooStep),
                                   _i32, _I32P, _I32P]),
+    "mesh_attn_cache_bytes": (_sz, [_CACHE]),
+    "mesh_attn_cache_tables": (_i32, [_CACHE, _i32, _p, _p, _p, _i32, _p, _p,
+                                      _p, _p, _i64, _p, _p, _p, _p, _p]),
+    "mesh_attn_cache_append": (_i32, [_CACHE, _i64, _p, _i64, _p, _i64, _p, _p,
+                                      _p]),
+    "mesh_attn_cache_read": (_i32, [_CACHE, _i64, _p, _p, _p, _p, _p]),
+    "mesh_attn_cache_fwd_workspace_size": (_sz, [_CACHE, _i32, _i32, _i64]),
+    "mesh_attn_cache_fwd": (_i32, [_CACHE, _i32, ctypes.c_float, _i32, _i64,
+                                   _p, _i64, _p, _p, _p, _p, _p, _p, _i32, _p,
+                                   _p, _sz, _p]),
+    "mesh_attn_rope": (_i32, [ctypes.POINTER(Rope), _i64, _p, _i32, _p, _i64,
+                              _p, _i64, _i32, _p, _i64, _p, _i64, _i32, _i32,
+                              _p]),
     "mesh_attn_last_error": (ctypes.c_char_p, []),
 }
 
@@ -523,3 +596,201 @@ def mesh_attn_goo_plan(k_q, k_kv, t_ag_q, t_ag_kv, t_rs_q, t_c, gamma=1.05):
                            for t in range(s_.first_task,
                                           s_.first_task + s_.num_tasks)]))
     return out
+
+
+# ---------------------------------------------------------------------------
+# Paged key/value cache in 4 bits
+# ---------------------------------------------------------------------------
+
+def _one_device(stream, *tensors):
+    # Launches go to the current device (or the stream's): a tensor of another
+    # one would be an address it may not know.
+    index = (_torch()._C._cuda_getDevice() if stream is None
+             else stream.device.index)
+    for t in tensors:
+        if t.get_device() != index:
+            raise ValueError(f"tensor on {t.device}, the call on cuda:{index}")
+
+
+def _heads(t, name, rows, heads, d, dtypes):
+    """Pointer and row stride of [rows, heads, d] whose heads are dense."""
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a GPU, got {t.device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} dtype {t.dtype} not in {dtypes}")
+    if t.shape != (rows, heads, d):
+        raise ValueError(f"{name} shape {tuple(t.shape)} != "
+                         f"{(rows, heads, d)}")
+    row, head, dim = t.stride()
+    if rows <= 1:  # the stride of a single row says nothing
+        row = max(row, heads * d)
+        row += -row % 8
+    if dim != 1 or (heads > 1 and head != d) or row < heads * d:
+        raise ValueError(f"{name} strides {t.stride()}: the heads of a row "
+                         f"must be dense and rows must not overlap")
+    return t.data_ptr(), row
+
+
+def _cache_data(c, data):
+    shape = (c.num_pages, c.num_kv_heads,
+             c.page_size * (c.head_dim + c.head_dim // 16))
+    return _dev(data, "data", shape, (_torch().uint8,))
+
+
+def mesh_attn_cache_bytes(cache):
+    """Bytes of a cache: a uint8 tensor of shape ``[num_pages, num_kv_heads,
+    page_size * (d + d / 16)]``."""
+    n = int(load_library().mesh_attn_cache_bytes(
+        ctypes.byref(Cache.make(cache))))
+    if n == 0:
+        raise MeshAttnError("mesh_attn_cache_bytes", MA_ERR_INVALID_ARG,
+                            mesh_attn_last_error())
+    return n
+
+
+def mesh_attn_cache_tables(cache, lens, new_lens, free_pages, free_range,
+                           block_table, lens_out, cu_new, slots, positions,
+                           free_range_out, refused, stream=None):
+    """Block table, slots and positions of a step from the requests' lengths;
+    all int32 but ``slots`` (int64).  Returns ``(block_table, lens_out, cu_new,
+    slots, positions, free_range_out, refused)``."""
+    torch = _torch()
+    c = Cache.make(cache)
+    i32 = (torch.int32,)
+    b, rows, num_free = lens.numel(), slots.numel(), free_pages.numel()
+    a = [_dev(lens, "lens", (b,), i32),
+         _dev(new_lens, "new_lens", (b,), i32),
+         _dev(free_pages, "free_pages", (num_free,), i32), num_free,
+         _dev(free_range, "free_range", (2,), i32),
+         _dev(block_table, "block_table", (b, c.max_pages), i32),
+         _dev(lens_out, "lens_out", (b,), i32),
+         _dev(cu_new, "cu_new", (b + 1,), i32), rows,
+         _dev(slots, "slots", (rows,), (torch.int64,)),
+         _dev(positions, "positions", (rows,), i32),
+         _dev(free_range_out, "free_range_out", (2,), i32),
+         _dev(refused, "refused", (1,), i32)]
+    _one_device(stream, lens, new_lens, free_pages, free_range, block_table,
+                lens_out, cu_new, slots, positions, free_range_out, refused)
+    st = load_library().mesh_attn_cache_tables(ctypes.byref(c), b, *a,
+                                               _stream_ptr(stream))
+    _check("mesh_attn_cache_tables", st)
+    return (block_table, lens_out, cu_new, slots, positions, free_range_out,
+            refused)
+
+
+def mesh_attn_cache_append(cache, k, v, slots, data, stream=None):
+    """Stores rows ``k, v [rows, Hkv, d]`` (bf16; row strides as they are) in 4
+    bits at ``slots [rows]`` (int64; out of range: not stored)."""
+    torch = _torch()
+    c = Cache.make(cache)
+    rows = slots.numel()
+    bf = (torch.bfloat16,)
+    kp, ks = _heads(k, "k", rows, c.num_kv_heads, c.head_dim, bf)
+    vp, vs = _heads(v, "v", rows, c.num_kv_heads, c.head_dim, bf)
+    sp = _dev(slots, "slots", (rows,), (torch.int64,))
+    dp = _cache_data(c, data)
+    _one_device(stream, k, v, slots, data)
+    st = load_library().mesh_attn_cache_append(
+        ctypes.byref(c), rows, kp, ks, vp, vs, sp, dp, _stream_ptr(stream))
+    _check("mesh_attn_cache_append", st)
+    return data
+
+
+def mesh_attn_cache_read(cache, slots, data, k, v, stream=None):
+    """The stored rows at ``slots`` as bf16 ``k, v [rows, Hkv, d]``, the KV
+    buffer of the tile calls."""
+    torch = _torch()
+    c = Cache.make(cache)
+    rows = slots.numel()
+    shape, bf = (rows, c.num_kv_heads, c.head_dim), (torch.bfloat16,)
+    a = [_dev(slots, "slots", (rows,), (torch.int64,)), _cache_data(c, data),
+         _dev(k, "k", shape, bf), _dev(v, "v", shape, bf)]
+    _one_device(stream, slots, data, k, v)
+    st = load_library().mesh_attn_cache_read(ctypes.byref(c), rows, *a,
+                                             _stream_ptr(stream))
+    _check("mesh_attn_cache_read", st)
+    return k, v
+
+
+def mesh_attn_cache_fwd_workspace_size(cache, num_q_heads, num_requests, rows):
+    return int(load_library().mesh_attn_cache_fwd_workspace_size(
+        ctypes.byref(Cache.make(cache)), int(num_q_heads), int(num_requests),
+        int(rows)))
+
+
+def mesh_attn_cache_fwd(cache, softmax_scale, q, positions, cu_new, lens,
+                        block_table, data, o, lse, ws=None, stream=None):
+    """O and LSE of the query rows ``q [rows, Hq, d]`` (bf16; row stride as it
+    is) over the stored keys of their requests.  ``o`` bf16 (final) or float32
+    (partial) ``[rows, Hq, d]``, ``lse [Hq, rows]``; rows of no request stay as
+    they were."""
+    torch = _torch()
+    c = Cache.make(cache)
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, heads, head_dim]")
+    rows, hq, _ = q.shape
+    b = lens.numel()
+    i32 = (torch.int32,)
+    qp, qs = _heads(q, "q", rows, hq, c.head_dim, (torch.bfloat16,))
+    a = [_dev(positions, "positions", (rows,), i32),
+         _dev(cu_new, "cu_new", (b + 1,), i32), _dev(lens, "lens", (b,), i32),
+         _dev(block_table, "block_table", (b, c.max_pages), i32),
+         _cache_data(c, data),
+         _dev(o, "o", (rows, hq, c.head_dim), (torch.bfloat16, torch.float32)),
+         _dtype_code(o), _dev(lse, "lse", (hq, rows), (torch.float32,))]
+    _one_device(stream, q, positions, cu_new, lens, block_table, data, o, lse)
+    if ws is None:
+        n = mesh_attn_cache_fwd_workspace_size(c, hq, b, rows)
+        ws = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
+        if stream is not None:
+            ws.record_stream(stream)
+    elif not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor")
+    _one_device(stream, ws)
+    st = load_library().mesh_attn_cache_fwd(
+        ctypes.byref(c), hq, float(softmax_scale), b, rows, qp, qs, *a,
+        ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(stream))
+    _check("mesh_attn_cache_fwd", st)
+    return o, lse
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions
+# ---------------------------------------------------------------------------
+
+def mesh_attn_rope(rope, positions, q, q_out, k=None, k_out=None, inverse=0,
+                   stream=None):
+    """Turns the heads of ``q [rows, heads, d]`` (and of ``k``) by their rows'
+    ``positions [num_axes, rows]`` (int32; ``[rows]`` does for one axis) into ``q_out``, ``k_out`` (the same
+    tensors for in place); bf16 or float32, row strides as they are.
+    ``inverse=1`` turns back: the gradient."""
+    torch = _torch()
+    r = Rope.make(rope)
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise ValueError("q and k must be [rows, heads, head_dim]")
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out go together")
+    rows, hq, _ = q.shape
+    d, dtypes = r.head_dim, (q.dtype,)
+    if q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"q dtype {q.dtype} is not bfloat16 or float32")
+    shape = (r.num_axes, rows)
+    if r.num_axes == 1 and positions.dim() == 1:
+        shape = (rows,)
+    pp = _dev(positions, "positions", shape, (torch.int32,))
+    qp, qs = _heads(q, "q", rows, hq, d, dtypes)
+    qo, qos = _heads(q_out, "q_out", rows, hq, d, dtypes)
+    _one_device(stream, positions, q, q_out)
+    hk = kp = ks = ko = kos = 0
+    if k is not None:
+        hk = k.shape[1]
+        kp, ks = _heads(k, "k", rows, hk, d, dtypes)
+        ko, kos = _heads(k_out, "k_out", rows, hk, d, dtypes)
+        _one_device(stream, k, k_out)
+    st = load_library().mesh_attn_rope(
+        ctypes.byref(r), rows, pp, hq, qp, qs, qo, qos, hk, kp or None, ks,
+        ko or None, kos, _dtype_code(q), int(inverse), _stream_ptr(stream))
+    _check("mesh_attn_rope", st)
+    return q_out, k_out
