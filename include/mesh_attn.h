@@ -493,7 +493,8 @@ size_t mesh_attn_cache_fwd_workspace_size(const ma_cache_t* cache,
                                           int32_t num_q_heads,
                                           int32_t num_requests, int64_t rows);
 
-/* Attention of packed query rows over the stored keys of their requests.
+/* Attention of packed query rows over the stored keys of their requests;
+ * rows * Hq < 2^30.
  *   q          row r, head h at q + r * q_stride + h * d, bf16 device; the
  *              stride is in elements, a multiple of 8, >= Hq * d.
  *   positions  [rows] int32 device: row r sees the stored keys whose position

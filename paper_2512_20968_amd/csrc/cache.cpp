@@ -258,6 +258,9 @@ ma_status_t mesh_attn_cache_fwd(
                 "finite");
   if (o_dtype != MA_BF16 && o_dtype != MA_FP32)
     return fail(MA_ERR_INVALID_ARG, "o_dtype %d invalid", (int)o_dtype);
+  if (rows * num_q_heads >= int64_t{1} << 30)
+    return fail(MA_ERR_INVALID_ARG, "rows * num_q_heads %lld not below 2^30",
+                static_cast<long long>(rows) * num_q_heads);
   MA_TRY(check_stride("q_stride", q_stride, int64_t{num_q_heads} * p.c.d, 8));
   if (rows == 0 || num_requests == 0) return ok();
   const Arg args[] = {{"q", q, 16},

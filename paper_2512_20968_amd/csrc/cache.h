@@ -77,6 +77,12 @@ struct LoadParams {
 };
 hipError_t launch_cache_read(const LoadParams& p, hipStream_t stream);
 
+// A sequence of the attention whose partial results are to be joined: the runs
+// of `parts` workgroups from this one on (0: none starts here).
+struct CacheFold {
+  int32_t first, rr0, rr_end, kvh, parts, pad[3];
+};
+
 struct CacheFwdParams {
   CacheDims c;
   const uint16_t* q;
@@ -92,6 +98,10 @@ struct CacheFwdParams {
   int32_t hq, group, num_requests;
   int32_t max_tiles;  // no more tiles for rows that do not overlap
   float scale_log2;
+  int32_t split, min_units;  // whether sequences are cut; least units of a run
+  CacheFold* fold;           // [workgroup]
+  float* part_o;             // [2 * workgroups][rows of a tile][d]
+  float* part_ml;            // .. [2]: reference (log2 units) and sum
 };
 
 hipError_t launch_cache_fwd(const CacheFwdParams& p, bool out_f32, void* ws,

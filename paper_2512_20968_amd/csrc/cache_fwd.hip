@@ -37,6 +37,20 @@ constexpr int NT = 256;
 constexpr int kWaves = NT / 64;
 constexpr int kStep = 32;  // keys of a wave's step
 
+// Read-only data through the constant address space: uniform addresses become
+// scalar loads.
+template <typename T>
+__device__ __forceinline__ T load_const(const T* p, int64_t i) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef const __attribute__((address_space(4))) T* cptr;
+  T v;
+  __builtin_memcpy(&v, (cptr)(p) + i, sizeof(T));
+  return v;
+#else
+  return p[i];
+#endif
+}
+
 __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b,
                                         const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -52,94 +66,190 @@ __device__ __forceinline__ float across_quarters(float x, Op op) {
 // What a wave loads for a step: codes and scale codes of its lanes' keys.
 template <int D>
 struct StepData {
-  static constexpr int kKWords = D / 32;      // of a key's quarter
-  static constexpr int kVWords = D / 16;      // of a column's eight keys
-  uint32_t kc[2][kKWords];
+  uint32_t kc[2][D / 32];  // of a key's quarter
   uint32_t ks[2];
-  uint32_t vc[kVWords];
+  uint32_t vc[D / 16];  // of a column's eight keys
   u32x2 vs;
-  bool ok;  // the page of keys 8 g .. 8 g + 7 is valid
 };
 
-template <int D>
-struct Head {
-  const uint8_t* base;   // of this KV head in page 0
+// A request's keys of one KV head.  Everything but the lane's offsets is
+// uniform over the wave.
+struct Keys {
+  const uint8_t* base;   // of the KV head in page 0
   const int32_t* table;  // the request's block table row
   int64_t page_bytes;    // from page to page
   int32_t lg, num_pages, last_page, local;
+  // Offsets of the lane's operands in a step's first page (P16: in its page).
+  uint32_t kc, ks, vc, vs;
 };
 
-template <int D>
-__device__ __forceinline__ int page_of(const Head<D>& h, int key, bool* ok) {
-  const int32_t id = h.table[min(key >> h.lg, h.last_page)];
-  *ok = id >= 0 && id < h.num_pages;
-  return *ok ? id : 0;
+// Pages of the two halves of the step at key kb (the same one unless a page is
+// 16 tokens).  Scalar loads: the next step's numbers are there, without waiting
+// for the vector loads in between, when its addresses are made.
+struct StepPages {
+  int32_t id[2];
+};
+
+template <bool P16>
+__device__ __forceinline__ StepPages load_pages(const Keys& h, int kb) {
+  StepPages s;
+  const int at = kb >> h.lg;
+  s.id[0] = load_const(h.table, min(at, h.last_page));
+  s.id[1] = P16 ? load_const(h.table, min(at + 1, h.last_page)) : s.id[0];
+  return s;
 }
 
-// Loads of the step at key kb.  Keys past the end load some byte of the last
-// page; compute() does not use them.
-template <int D>
-__device__ __forceinline__ void load_step(const Head<D>& h, int kb, int r,
-                                          int g, StepData<D>* s) {
-  using B = Block<D>;
-  const int mask = (1 << h.lg) - 1;
-  const int kkey = kb + 8 * (r >> 2) + (r & 3), vkey = kb + 8 * g;
-  bool kok;
-  const uint8_t* kblk = h.base + page_of<D>(h, kkey, &kok) * h.page_bytes;
-  const uint8_t* vblk = h.base + page_of<D>(h, vkey, &s->ok) * h.page_bytes;
+__device__ __forceinline__ bool valid_page(const Keys& h, int32_t id) {
+  return id >= 0 && id < h.num_pages;
+}
+
+// The block of the page of half `second` of a step; page 0's for an invalid
+// page, whose keys compute_step() does not use.
+template <bool P16>
+__device__ __forceinline__ const uint8_t* page_block(const Keys& h,
+                                                     const StepPages& pages,
+                                                     bool second) {
+  const int32_t i0 = valid_page(h, pages.id[0]) ? pages.id[0] : 0;
+  const uint8_t* p0 = h.base + i0 * h.page_bytes;
+  if (!P16) return p0;
+  const int32_t i1 = valid_page(h, pages.id[1]) ? pages.id[1] : 0;
+  const uint8_t* p1 = h.base + i1 * h.page_bytes;
+  return second ? p1 : p0;
+}
+
+// Whether the page of the lane's keys 8 g .. 8 g + 7 of a step is valid.
+template <bool P16>
+__device__ __forceinline__ bool lane_ok(const Keys& h, const StepPages& pages,
+                                        int g) {
+  return valid_page(h, pages.id[P16 && g >= 2 ? 1 : 0]);
+}
+
+template <typename T>
+__device__ __forceinline__ T load_at(const uint8_t* p) {
+  return *reinterpret_cast<const T*>(p);
+}
+
+// Loads of K and of V of the step at key kb.  Keys past the end load bytes of
+// the last page.
+template <int D, bool P16>
+__device__ __forceinline__ void load_k(const Keys& h, const StepPages& pages,
+                                       int kb, int r, StepData<D>* s) {
+  const uint8_t* kp = page_block<P16>(h, pages, r >= 8);
+  // The step's first token in its page (0 with pages of 16).
+  const uint32_t t0 = kb & ((1 << h.lg) - 1);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int tok = (kkey & mask) + 4 * t;
-    const uint8_t* kp = kblk + B::k_codes(h.lg, tok) + g * (D / 8);
+    const uint8_t* at = kp + t0 * (D / 2) + h.kc + t * (4 * (D / 2));
     if constexpr (D == 128) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(kp);
+      const u32x4 w = load_at<u32x4>(at);
 #pragma unroll
       for (int i = 0; i < 4; ++i) s->kc[t][i] = w[i];
     } else {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(kp);
+      const u32x2 w = load_at<u32x2>(at);
       s->kc[t][0] = w[0];
       s->kc[t][1] = w[1];
     }
-    s->ks[t] = kblk[B::k_scale(h.lg, tok, g * B::kGroups / 4)];
+    s->ks[t] = kp[t0 * (D / 32) + h.ks + t * (4 * (D / 32))];
   }
-  const int vtok = vkey & mask;
-  const u32x4* vp =
-      reinterpret_cast<const u32x4*>(vblk + B::v_codes(h.lg, vtok, r));
+}
+
+template <int D, bool P16>
+__device__ __forceinline__ void load_v(const Keys& h, const StepPages& pages,
+                                       int kb, int g, StepData<D>* s) {
+  const uint8_t* vp = page_block<P16>(h, pages, g >= 2);
+  const uint32_t t0 = kb & ((1 << h.lg) - 1);
 #pragma unroll
   for (int j = 0; j < D / 64; ++j) {
-    const u32x4 w = vp[j];
+    const u32x4 w = load_at<u32x4>(vp + t0 * (D / 2) + h.vc + 16 * j);
 #pragma unroll
     for (int i = 0; i < 4; ++i) s->vc[4 * j + i] = w[i];
   }
-  s->vs = *reinterpret_cast<const u32x2*>(
-      vblk + B::v_scale(h.lg, vtok, r * B::kGroups / 16));
+  s->vs = load_at<u32x2>(vp + t0 + h.vs);
+}
+
+// The lane's offsets for pages of 2^lg tokens.
+template <int D>
+__device__ __forceinline__ void lane_offsets(Keys* h, int r, int g) {
+  using B = Block<D>;
+  const int mask = (1 << h->lg) - 1;
+  const int kt = (8 * (r >> 2) + (r & 3)) & mask, vt = (8 * g) & mask;
+  h->kc = B::k_codes(h->lg, kt) + g * (D / 8);
+  h->ks = B::k_scale(h->lg, kt, g * B::kGroups / 4);
+  h->vc = B::v_codes(h->lg, vt, r);
+  h->vs = B::v_scale(h->lg, vt, r * B::kGroups / 16);
 }
 
 // The item's rows and running state, 16 rows (columns of the MFMAs) per q.
+//
+// Up to 32 rows keep Q in registers; 64 rows would not fit beside O, and read it
+// from LDS, in the order of the operand's lanes.
+template <int NQ>
+constexpr bool kQInLds = NQ > 2;
+
 template <int D, int NQ>
 struct State {
-  bf16x8 q[NQ][D / 32];
+  bf16x8 q[kQInLds<NQ> ? 1 : NQ][D / 32];
   f32x4 o[NQ][D / 16];  // O^T, MFMA m of the lane's D/4 dims
   float m[NQ], l[NQ];   // running maximum (log2 units); this lane's share of
                         // the sum
   int vis[NQ];          // stored keys that the column's row sees
 };
 
+// The running maximum may lag behind by this much (log2 units): probabilities
+// stay below 2^kLag, as exact relative to each other as below 1, and the
+// accumulators are rescaled a few times per item instead of whenever a row's
+// maximum grows.
+constexpr float kLag = 8.f;
+
+// Probabilities as the second product's operand.  For a bf16 O: rounded to
+// bf16, 2^-8 of each, as O itself is.  For a float32 O: as the sum of three bf16
+// that hold all 24 bits, cut off one after the other.
+template <bool EXACT>
+struct Probs {
+  bf16x8 part[EXACT ? 3 : 1];
+};
+
+template <bool EXACT>
+__device__ __forceinline__ void split_probs(const float (&p)[8],
+                                            Probs<EXACT>* out) {
+  if constexpr (EXACT) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = p[i];
+#pragma unroll
+    for (int n = 0; n < 3; ++n) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = __float_as_uint(x[2 * i]);
+        const uint32_t hi = __float_as_uint(x[2 * i + 1]);
+        w[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+        x[2 * i] -= __uint_as_float(lo & 0xffff0000u);
+        x[2 * i + 1] -= __uint_as_float(hi & 0xffff0000u);
+      }
+      out->part[n] = __builtin_bit_cast(bf16x8, w);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out->part[0][i] = static_cast<__bf16>(p[i]);
+  }
+}
+
 // The rest of a step once its scores x are there: keys 8 g + 4 t + i of column
-// r.  SPLIT: the probabilities enter as a sum of two bf16.
-template <int D, int NQ, bool SPLIT>
+// r.
+template <int D, int NQ, bool EXACT>
 __device__ __forceinline__ void finish_step(State<D, NQ>& st,
                                             f32x4 (&x)[NQ][2],
                                             const StepData<D>& s,
                                             float scale_log2, u32x2 vs) {
-  bf16x8 ph[NQ], pl[NQ];
+  Probs<EXACT> ph[NQ];
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
     float top = x[q][0][0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) top = fmaxf(top, x[q][i >> 2][i & 3]);
     top *= scale_log2;
-    if (__any(top > st.m[q])) {
+    if (__any(top > st.m[q] + kLag)) {
       const float mn = fmaxf(
           st.m[q],
           across_quarters(top, [](float a, float b) { return fmaxf(a, b); }));
@@ -151,16 +261,13 @@ __device__ __forceinline__ void finish_step(State<D, NQ>& st,
       for (int m = 0; m < D / 16; ++m) st.o[q][m] *= f;
     }
     const float ref = st.m[q] == -INFINITY ? 0.f : st.m[q];
-    float sum = 0.f;
+    float p[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float p = __builtin_amdgcn_exp2f(
+    for (int i = 0; i < 8; ++i)
+      p[i] = __builtin_amdgcn_exp2f(
           fmaf(x[q][i >> 2][i & 3], scale_log2, -ref));
-      sum += p;
-      ph[q][i] = static_cast<__bf16>(p);
-      if (SPLIT) pl[q][i] = static_cast<__bf16>(p - static_cast<float>(ph[q][i]));
-    }
-    st.l[q] += sum;
+    st.l[q] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    split_probs<EXACT>(p, &ph[q]);
   }
   float scale[8];
 #pragma unroll
@@ -192,14 +299,12 @@ __device__ __forceinline__ void finish_step(State<D, NQ>& st,
     const bf16x8 a0 = __builtin_bit_cast(bf16x8, even);
     const bf16x8 a1 = __builtin_bit_cast(bf16x8, odd);
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      st.o[q][2 * mp] = mfma16(a0, ph[q], st.o[q][2 * mp]);
-      st.o[q][2 * mp + 1] = mfma16(a1, ph[q], st.o[q][2 * mp + 1]);
-      if (SPLIT) {
-        st.o[q][2 * mp] = mfma16(a0, pl[q], st.o[q][2 * mp]);
-        st.o[q][2 * mp + 1] = mfma16(a1, pl[q], st.o[q][2 * mp + 1]);
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int n = 0; n < (EXACT ? 3 : 1); ++n) {
+        st.o[q][2 * mp] = mfma16(a0, ph[q].part[n], st.o[q][2 * mp]);
+        st.o[q][2 * mp + 1] = mfma16(a1, ph[q].part[n], st.o[q][2 * mp + 1]);
       }
-    }
   }
 }
 
@@ -209,17 +314,17 @@ __device__ __forceinline__ void finish_step(State<D, NQ>& st,
 // out of the product (0 * NaN is NaN) and given to those that see it.
 template <int D, int NQ>
 __device__ __forceinline__ u32x2 mask_step(State<D, NQ>& st, f32x4 (&x)[NQ][2],
-                                           const StepData<D>& s, int kb,
-                                           int local, int r, int g) {
+                                           const StepData<D>& s, bool ok,
+                                           int kb, int local, int g) {
   u32x2 vs = s.vs;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (!s.ok || kb + 8 * g + i >= local) vs[i >> 2] &= ~(255u << (8 * (i & 3)));
+    if (!ok || kb + 8 * g + i >= local) vs[i >> 2] &= ~(255u << (8 * (i & 3)));
 #pragma unroll
   for (int q = 0; q < NQ; ++q)
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (!s.ok || kb + 8 * g + i >= st.vis[q]) x[q][i >> 2][i & 3] = -INFINITY;
+      if (!ok || kb + 8 * g + i >= st.vis[q]) x[q][i >> 2][i & 3] = -INFINITY;
   // Bit i: key 8 g + i of the lane's group of dims is NaN.
   uint32_t nan = 0;
 #pragma unroll
@@ -229,54 +334,61 @@ __device__ __forceinline__ u32x2 mask_step(State<D, NQ>& st, f32x4 (&x)[NQ][2],
       vs[i >> 2] &= ~(255u << (8 * (i & 3)));
     }
   if (__any(nan != 0)) {
-    // The lane's accumulators hold dims g D/4 ..: their group belongs to
-    // columns n of 16 * (that dim) / D.
+    // The lane's accumulators hold dims g D/4 ..: column n = 4 g is of their
+    // group.
+    bool hit[NQ] = {};
     for (int o = 0; o < 4; ++o) {  // keys 8 o ..
-      const uint32_t bits =
-          __shfl(nan, 16 * o + 4 * g);  // column n = 4 g has the lane's dims
+      const uint32_t bits = __shfl(nan, 16 * o + 4 * g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-#pragma unroll
-        for (int q = 0; q < NQ; ++q)
-          if ((bits >> i & 1) && kb + 8 * o + i < st.vis[q])
-#pragma unroll
-            for (int m = 0; m < D / 16; ++m) st.o[q][m] += NAN;
+      for (int q = 0; q < NQ; ++q) {
+        const int seen = min(max(st.vis[q] - (kb + 8 * o), 0), 8);
+        hit[q] |= (bits & ((1u << seen) - 1)) != 0;
       }
+    }
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const float add = hit[q] ? NAN : 0.f;
+#pragma unroll
+      for (int m = 0; m < D / 16; ++m) st.o[q][m] += add;
     }
   }
   return vs;
 }
 
-template <int D, int NQ, bool SPLIT>
-__device__ __forceinline__ void compute_step(State<D, NQ>& st,
-                                             const StepData<D>& s, int kb,
-                                             int local, int all_see,
-                                             float scale_log2, int r, int g) {
-  f32x4 x[NQ][2];
+// x = K Q^T of a step.  q_lds: Q in LDS, [q][c][lane].
+template <int D, int NQ>
+__device__ __forceinline__ void score_step(const State<D, NQ>& st,
+                                           const bf16x8* q_lds,
+                                           const StepData<D>& s, int lane,
+                                           f32x4 (&x)[NQ][2]) {
+  float sc[2];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const float sc = s.ks[t] == kScaleNaN ? NAN : scale_of(s.ks[t]);
+  for (int t = 0; t < 2; ++t)
+    sc[t] = s.ks[t] == kScaleNaN ? NAN : scale_of(s.ks[t]);
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-      const bf16x8 a = dequant8(s.kc[t][c], sc);
+  for (int c = 0; c < D / 32; ++c) {
+    const bf16x8 a0 = dequant8(s.kc[0][c], sc[0]);
+    const bf16x8 a1 = dequant8(s.kc[1][c], sc[1]);
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        if (c == 0) x[q][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        x[q][t] = mfma16(a, st.q[q][c], x[q][t]);
-      }
+    for (int q = 0; q < NQ; ++q) {
+      if (c == 0) x[q][0] = x[q][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      bf16x8 b;
+      if constexpr (kQInLds<NQ>)
+        b = q_lds[(q * (D / 32) + c) * 64 + lane];
+      else
+        b = st.q[q][c];
+      x[q][0] = mfma16(a0, b, x[q][0]);
+      x[q][1] = mfma16(a1, b, x[q][1]);
     }
   }
-  u32x2 vs = s.vs;
-  if (kb + kStep > all_see || !__all(s.ok))
-    vs = mask_step<D, NQ>(st, x, s, kb, local, r, g);
-  finish_step<D, NQ, SPLIT>(st, x, s, scale_log2, vs);
 }
 
-// One row's final results.
+// One row's final results from its sums at reference m.
 template <int D, bool OUT_F32>
 __device__ __forceinline__ void store_row(const CacheFwdParams& p, int64_t row,
-                                          int head, int dim0, float (&acc)[8],
-                                          float m, float l) {
+                                          int head, int dim0,
+                                          const float (&acc)[8], float m,
+                                          float l) {
   const float inv = l > 0.f ? 1.f / l : l;  // 0 for no key; NaN stays
   const int64_t at = (row * p.hq + head) * D + dim0;
   if (OUT_F32) {
@@ -303,34 +415,58 @@ __device__ __forceinline__ void store_row(const CacheFwdParams& p, int64_t row,
 
 // Rows [first, end) of request b in the packed rows.
 __device__ __forceinline__ void request_rows(const CacheFwdParams& p, int b,
-                                             int64_t* first, int64_t* end) {
-  const int64_t rows = p.rows;
-  const int64_t a = p.cu[b], e = p.cu[b + 1];
-  *first = a < 0 ? 0 : a > rows ? rows : a;
-  *end = e < *first ? *first : e > rows ? rows : e;
+                                             int* first, int* end) {
+  const int rows = static_cast<int>(p.rows);
+  *first = min(max(load_const(p.cu, b), 0), rows);
+  *end = min(max(load_const(p.cu, b + 1), *first), rows);
 }
 
-template <int D, int NQ, bool OUT_F32>
-__global__ __launch_bounds__(NT) void cache_fwd_kernel(CacheFwdParams p) {
+__device__ __forceinline__ int32_t stored_keys(const CacheFwdParams& p,
+                                               int32_t len) {
+  const int64_t most = int64_t{p.c.max_pages} << p.c.page_log2;
+  const int64_t n = p.c.share.below(len < 0 ? 0 : len);
+  return static_cast<int32_t>(n < most ? n : most);
+}
+
+// Work of a launch.  A sequence is a tile of a request's rows and a KV head; it
+// is cut into units of 128 keys, a step of each wave (at least one unit, which
+// writes the results of rows without keys).  All sequences' units in a row are
+// dealt to the workgroups in equal runs of `per`, so every workgroup has the
+// same work whatever the lengths, which only the device knows.  A sequence that
+// lies in several runs leaves partial results, two slots a workgroup at most:
+// slot 2 w for the piece that goes on from an earlier run, slot 2 w + 1 for the
+// one that starts in run w and goes on after it; cache_fold_kernel joins them.
+// p.split 0: every sequence is one unit of its own, and no piece is split.
+constexpr int kUnit = kWaves * kStep;
+
+template <int D, int NQ, bool OUT_F32, bool P16>
+__global__ __launch_bounds__(NT, NQ == 1 ? 4 : NQ == 2 ? 3 : 2)
+void cache_fwd_kernel(CacheFwdParams p) {
   constexpr int kRows = 16 * NQ;
   constexpr int kPad = D + 4;  // row stride of the fold, in floats
   __shared__ float s_o[kWaves][16][kPad];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  extern __shared__ int32_t s_tiles[];  // [B + 1] first tile of a request
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ bf16x8 s_q[kQInLds<NQ> ? NQ * (D / 32) * 64 : 1];
+  extern __shared__ int64_t s_units[];  // [B + 1] first unit of a request
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int B = p.num_requests;
+  const int B = p.num_requests, hkv = p.c.hkv;
 
-  // Tiles of 16 NQ rows per request: prefix sums by one wave.
+  // First units of the requests: prefix sums by one wave.
   if (wave == 0) {
-    int base = 0;
+    int64_t base = 0;
+    int tiles = 0;  // so far; capped, in case rows overlap
     for (int b0 = 0; b0 < B; b0 += 64) {
-      int n = 0;
-      if (b0 + lane < B) {
-        int64_t first, end;
-        request_rows(p, b0 + lane, &first, &end);
-        const int64_t t = ((end - first) * p.group + kRows - 1) / kRows;
-        n = static_cast<int>(t < p.max_tiles ? t : p.max_tiles);
+      const int b = b0 + lane;
+      int n = 0, nu = 1;
+      if (b < B) {
+        int first, end;
+        request_rows(p, b, &first, &end);
+        const uint32_t rr = uint32_t(end - first) * p.group;  // below 2^31
+        n = min(int((rr + kRows - 1) / kRows), p.max_tiles);
+        if (p.split)
+          nu = max((stored_keys(p, p.lens[b]) + kUnit - 1) / kUnit, 1);
       }
       int y = n;
 #pragma unroll
@@ -338,58 +474,90 @@ __global__ __launch_bounds__(NT) void cache_fwd_kernel(CacheFwdParams p) {
         const int z = __shfl_up(y, o);
         if (lane >= o) y = min(y + z, p.max_tiles);
       }
-      const int before = __shfl_up(y, 1);
-      if (b0 + lane < B)
-        s_tiles[b0 + lane] =
-            lane == 0 ? base : min(base + before, p.max_tiles);
-      base = min(base + __shfl(y, 63), p.max_tiles);
+      // This request's tiles under the cap.  (Every lane takes part in the
+      // shuffle: one that does not would have nothing to give.)
+      int before = __shfl_up(y, 1);
+      if (lane == 0) before = 0;
+      n = min(tiles + y, p.max_tiles) - min(tiles + before, p.max_tiles);
+      tiles = min(tiles + __shfl(y, 63), p.max_tiles);
+      int64_t u = int64_t{n} * nu * hkv;
+      const int64_t mine = u;
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) {
+        const int64_t z = __shfl_up(u, o);
+        if (lane >= o) u += z;
+      }
+      if (b < B) s_units[b] = base + u - mine;
+      base += __shfl(u, 63);
     }
-    if (lane == 0) s_tiles[B] = base;
+    if (lane == 0) s_units[B] = base;
   }
   __syncthreads();
-  const int64_t items = int64_t{s_tiles[B]} * p.c.hkv;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int tile = static_cast<int>(item / p.c.hkv);
-    const int kvh = static_cast<int>(item - int64_t{tile} * p.c.hkv);
+  const int64_t total = s_units[B];
+  int64_t per = 1, at = blockIdx.x, stop = total;
+  if (p.split) {
+    per = (total + gridDim.x - 1) / gridDim.x;
+    per = per > p.min_units ? per : p.min_units;
+    at = per * blockIdx.x;
+    stop = at + per < total ? at + per : total;
+    if (tid == 0) p.fold[blockIdx.x].parts = 0;
+  }
+
+  while (at < stop) {
     int lo = 0, hi = B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (s_tiles[mid] <= tile)
+      if (s_units[mid] <= at)
         lo = mid;
       else
         hi = mid;
     }
-    const int b = lo;
-    int64_t first, end;
+    const int b = __builtin_amdgcn_readfirstlane(lo);
+    int first, end;
     request_rows(p, b, &first, &end);
-    const int64_t rr0 = int64_t{tile - s_tiles[b]} * kRows;
-    const int64_t rr_end = (end - first) * p.group;
+    const int rr_end = (end - first) * p.group;
+    Keys h;
+    h.local = stored_keys(p, load_const(p.lens, b));
+    const int nu = p.split ? max((h.local + kUnit - 1) / kUnit, 1) : 1;
+    const int64_t off = at - s_units[b];
+    const int seq = __builtin_amdgcn_readfirstlane(int(off / nu));
+    const int u0 =
+        __builtin_amdgcn_readfirstlane(int(off - int64_t{seq} * nu));
+    const int64_t left = stop - at;
+    const int u1 = p.split ? __builtin_amdgcn_readfirstlane(
+                                 int(u0 + left < nu ? u0 + left : nu))
+                           : 1;
+    const int rr0 = __builtin_amdgcn_readfirstlane(seq / hkv) * kRows;
+    const int kvh = seq - rr0 / kRows * hkv;
 
-    Head<D> h;
     h.lg = p.c.page_log2;
     h.num_pages = p.c.num_pages;
     h.table = p.block_table + int64_t{b} * p.c.max_pages;
-    const int64_t most = int64_t{p.c.max_pages} << h.lg;
-    const int32_t stored = p.c.share.below(max(p.lens[b], 0));
-    h.local = static_cast<int32_t>(stored < most ? stored : most);
     h.last_page = max((h.local - 1) >> h.lg, 0);
-    h.page_bytes = int64_t{p.c.hkv} * p.c.block_bytes();
+    h.page_bytes = int64_t{hkv} * p.c.block_bytes();
     h.base = p.data + int64_t{kvh} * p.c.block_bytes();
+    lane_offsets<D>(&h, r, g);
 
     State<D, NQ> st;
     int most_seen = 0, all_see = INT32_MAX;
+    if (kQInLds<NQ>) __syncthreads();  // the last item's Q has been read
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      const int64_t rr = rr0 + 16 * q + r;
-      const bool valid = rr < rr_end;
-      const int64_t row = first + (valid ? rr : rr0) / p.group;
-      const int head = kvh * p.group +
-                       static_cast<int>((valid ? rr : rr0) % p.group);
+      const bool valid = rr0 + 16 * q + r < rr_end;
+      const uint32_t rr = valid ? rr0 + 16 * q + r : rr0;
+      const uint32_t tok = rr / uint32_t(p.group);
+      const int64_t row = first + int64_t{tok};
+      const int head = kvh * p.group + int(rr - tok * p.group);
       const uint16_t* src =
           p.q + row * p.q_stride + int64_t{head} * D + g * (D / 4);
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c)
-        st.q[q][c] = *reinterpret_cast<const bf16x8*>(src + 8 * c);
+      for (int c = 0; c < D / 32; ++c) {
+        if constexpr (!kQInLds<NQ>)
+          st.q[q][c] = *reinterpret_cast<const bf16x8*>(src + 8 * c);
+        else if (q % kWaves == wave)
+          s_q[(q * (D / 32) + c) * 64 + lane] =
+              *reinterpret_cast<const bf16x8*>(src + 8 * c);
+      }
       const int64_t pos = p.positions[row];
       st.vis[q] =
           valid ? min(p.c.share.below(pos < 0 ? 0 : pos + 1), h.local) : 0;
@@ -407,17 +575,53 @@ __global__ __launch_bounds__(NT) void cache_fwd_kernel(CacheFwdParams p) {
     }
     most_seen = __builtin_amdgcn_readfirstlane(most_seen);
     all_see = __builtin_amdgcn_readfirstlane(all_see);
+    if (kQInLds<NQ>) __syncthreads();
 
-    for (int kb = wave * kStep; kb < most_seen; kb += kWaves * kStep) {
+    // The next step's K is loaded into the registers of this one's as soon as
+    // the first product has read them, its V after the second: each is in
+    // flight for about half a step, without registers of its own.
+    const int kend = p.split ? min(u1 * kUnit, most_seen) : most_seen;
+    int kb = u0 * kUnit + wave * kStep;
+    if (kb < kend) {
       StepData<D> s;
-      load_step<D>(h, kb, r, g, &s);
-      compute_step<D, NQ, OUT_F32>(st, s, kb, h.local, all_see, p.scale_log2, r,
-                                   g);
+      StepPages pg = load_pages<P16>(h, kb);
+      load_k<D, P16>(h, pg, kb, r, &s);
+      load_v<D, P16>(h, pg, kb, g, &s);
+      for (;;) {
+        const int next = kb + kUnit;
+        const bool more = next < kend;
+        const StepPages pn = load_pages<P16>(h, next);
+        f32x4 x[NQ][2];
+        score_step<D, NQ>(st, s_q, s, lane, x);
+        if (more) load_k<D, P16>(h, pn, next, r, &s);
+        u32x2 vs = s.vs;
+        const bool ok = lane_ok<P16>(h, pg, g);
+        if (kb + kStep > all_see || !__all(ok))
+          vs = mask_step<D, NQ>(st, x, s, ok, kb, h.local, g);
+        finish_step<D, NQ, OUT_F32>(st, x, s, p.scale_log2, vs);
+        if (!more) break;
+        load_v<D, P16>(h, pn, next, g, &s);
+        pg = pn;
+        kb = next;
+      }
     }
 
+    const bool whole = u0 == 0 && u1 == nu;
+    const int slot = 2 * blockIdx.x + (u0 == 0 ? 1 : 0);
+    if (p.split && u0 == 0 && !whole && tid == 0) {
+      CacheFold f;
+      f.first = first;
+      f.rr0 = rr0;
+      f.rr_end = rr_end;
+      f.kvh = kvh;
+      // Runs that the sequence's units lie in.
+      f.parts = static_cast<int32_t>((at + nu - 1) / per - blockIdx.x + 1);
+      p.fold[blockIdx.x] = f;
+    }
     // Fold the waves, 16 rows at a time.
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
+      if (rr0 + 16 * q >= rr_end) break;
       const float l = across_quarters(
           st.l[q], [](float a, float b) { return a + b; });
       __syncthreads();
@@ -432,7 +636,8 @@ __global__ __launch_bounds__(NT) void cache_fwd_kernel(CacheFwdParams p) {
           s_o[wave][r][g * (D / 4) + i * (D / 16) + m] = st.o[q][m][i];
       __syncthreads();
       const int row16 = tid / (D / 8), dim0 = tid % (D / 8) * 8;
-      if (row16 < 16) {
+      const int rr = rr0 + 16 * q + row16;
+      if (row16 < 16 && rr < rr_end) {
         float M = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][row16]);
@@ -440,53 +645,191 @@ __global__ __launch_bounds__(NT) void cache_fwd_kernel(CacheFwdParams p) {
         float L = 0.f, acc[8] = {};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          const float f = __builtin_amdgcn_exp2f(s_m[w][row16] - ref);
-          // A wave without a key has weight 0 (its sum is 0, not NaN).
-          const float sm = s_m[w][row16] == -INFINITY ? 1.f : f;
+          // A wave without a maximum has sums of 0, or of NaN.
+          const float sm = s_m[w][row16] == -INFINITY
+                               ? 1.f
+                               : __builtin_amdgcn_exp2f(s_m[w][row16] - ref);
           L += s_l[w][row16] * sm;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            acc[i] += s_o[w][row16][dim0 + i] * sm;
+          for (int i = 0; i < 8; ++i) acc[i] += s_o[w][row16][dim0 + i] * sm;
         }
-        const int64_t rr = rr0 + 16 * q + row16;
-        if (rr < rr_end)
+        if (whole) {
           store_row<D, OUT_F32>(p, first + rr / p.group,
-                                kvh * p.group + static_cast<int>(rr % p.group),
+                                kvh * p.group + rr % p.group,
                                 dim0, acc, ref, L);
+        } else {
+          const int64_t pr = int64_t{slot} * kRows + 16 * q + row16;
+          f32x4* dst = reinterpret_cast<f32x4*>(p.part_o + pr * D + dim0);
+          dst[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+          dst[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
+          if (dim0 == 0) {
+            p.part_ml[2 * pr] = M;
+            p.part_ml[2 * pr + 1] = L;
+          }
+        }
       }
+    }
+    at += p.split ? u1 - u0 : int64_t{gridDim.x};
+  }
+}
+
+// Joins the partial results of the sequence that starts in run blockIdx.x and
+// goes on after it: slots 2 w + 1, 2 (w + 1), 2 (w + 2), .. in that order,
+// whatever order they were made in.  Eight dims per thread, kFoldRows rows at a
+// time, the pieces dealt to kFoldParts threads.
+constexpr int kFoldRows = 4, kFoldParts = 8;
+
+template <int D, int NQ, bool OUT_F32>
+__global__ __launch_bounds__(kFoldRows * kFoldParts * (D / 8))
+void cache_fold_kernel(CacheFwdParams p) {
+  constexpr int kRows = 16 * NQ, kDimThreads = D / 8;
+  __shared__ float s_acc[kFoldParts][kFoldRows][D];
+  __shared__ float s_m[kFoldParts][kFoldRows], s_l[kFoldParts][kFoldRows];
+  const int w = blockIdx.x;
+  const CacheFold f = load_const(p.fold, w);
+  if (f.parts < 2) return;
+  const int dim0 = threadIdx.x % kDimThreads * 8;
+  const int row4 = threadIdx.x / kDimThreads % kFoldRows;
+  const int pg = threadIdx.x / (kDimThreads * kFoldRows);
+  for (int q0 = 0; q0 < kRows; q0 += kFoldRows) {
+    if (f.rr0 + q0 >= f.rr_end) return;
+    const int row = q0 + row4;
+    const int rr = f.rr0 + row;
+    const bool valid = rr < f.rr_end;
+    float M = -INFINITY, L = 0.f, acc[8] = {};
+    auto fold = [&](float m, float l, const float* x) {
+      const float mn = fmaxf(M, m);
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      const float a = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - ref);
+      const float b = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - ref);
+      L = L * a + l * b;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] = acc[i] * a + x[i] * b;
+      M = mn;
+    };
+    if (valid)
+      for (int i = pg; i < f.parts; i += kFoldParts) {
+        const int64_t slot = i == 0 ? 2 * int64_t{w} + 1 : 2 * (int64_t{w} + i);
+        const int64_t pr = slot * kRows + row;
+        float x[8];
+        const f32x4* src =
+            reinterpret_cast<const f32x4*>(p.part_o + pr * D + dim0);
+        const f32x4 lo = src[0], hi = src[1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j] = lo[j];
+          x[4 + j] = hi[j];
+        }
+        fold(p.part_ml[2 * pr], p.part_ml[2 * pr + 1], x);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s_acc[pg][row4][dim0 + i] = acc[i];
+    if (dim0 == 0) {
+      s_m[pg][row4] = M;
+      s_l[pg][row4] = L;
+    }
+    __syncthreads();
+    if (pg == 0 && valid) {
+      M = -INFINITY;
+      L = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kFoldParts; ++j)
+        fold(s_m[j][row4], s_l[j][row4], &s_acc[j][row4][dim0]);
+      store_row<D, OUT_F32>(p, f.first + rr / p.group,
+                            f.kvh * p.group + rr % p.group,
+                            dim0, acc, M == -INFINITY ? 0.f : M, L);
     }
   }
 }
 
-template <int D, int NQ>
-hipError_t launch(CacheFwdParams p, bool out_f32, hipStream_t stream) {
-  int64_t tiles = p.rows * p.group / (16 * NQ) + p.num_requests;
-  if (tiles > 1 << 29) tiles = 1 << 29;  // sums of two fit 32 bits
-  p.max_tiles = static_cast<int32_t>(tiles);
-  int64_t grid = tiles * p.c.hkv;
-  if (grid > 65536) grid = 65536;
-  const size_t lds = (static_cast<size_t>(p.num_requests) + 1) * 4;
-  if (out_f32)
-    hipLaunchKernelGGL((cache_fwd_kernel<D, NQ, true>),
-                       dim3(static_cast<unsigned>(grid)), dim3(NT), lds, stream,
-                       p);
+// How a call is launched, from its sizes alone.
+struct Shape {
+  int nq;          // 16-row columns per tile
+  int64_t tiles;   // most tiles of all requests together
+  bool split;
+  int grid;
+};
+
+Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
+               int64_t rows) {
+  const int group = hq / c.hkv;
+  Shape s;
+  // Rows of a request, were they all alike.
+  const int64_t each = (rows + num_requests - 1) / num_requests * group;
+  s.nq = each <= 16 ? 1 : each <= 32 ? 2 : 4;
+  s.tiles = rows * group / (16 * s.nq) + num_requests;
+  if (s.tiles > 1 << 29) s.tiles = 1 << 29;  // sums of two fit 32 bits
+  const int64_t seqs = s.tiles * c.hkv;
+  const int slots = s.nq == 1 ? 1024 : s.nq == 2 ? 768 : 512;
+  s.split = (int64_t{c.max_pages} << c.page_log2) > kUnit && seqs < 4 * slots;
+  const int64_t grid = s.split ? slots : seqs;
+  s.grid = static_cast<int>(grid < 65536 ? grid : 65536);
+  return s;
+}
+
+// Workspace of a split launch: CacheFold per workgroup, then the partial
+// results.
+size_t fold_bytes(const Shape& s) { return sizeof(CacheFold) * s.grid; }
+size_t part_rows(const Shape& s) { return size_t{32} * s.nq * s.grid; }
+
+template <int D, int NQ, bool OUT_F32>
+hipError_t launch(const CacheFwdParams& p, const Shape& s, hipStream_t stream) {
+  const size_t lds = (static_cast<size_t>(p.num_requests) + 1) * 8;
+  const dim3 grid(static_cast<unsigned>(s.grid));
+  if (p.c.page_log2 == 4)
+    hipLaunchKernelGGL((cache_fwd_kernel<D, NQ, OUT_F32, true>), grid, dim3(NT),
+                       lds, stream, p);
   else
-    hipLaunchKernelGGL((cache_fwd_kernel<D, NQ, false>),
-                       dim3(static_cast<unsigned>(grid)), dim3(NT), lds, stream,
-                       p);
+    hipLaunchKernelGGL((cache_fwd_kernel<D, NQ, OUT_F32, false>), grid,
+                       dim3(NT), lds, stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !s.split) return e;
+  hipLaunchKernelGGL((cache_fold_kernel<D, NQ, OUT_F32>), grid,
+                     dim3(kFoldRows * kFoldParts * (D / 8)), 0, stream, p);
   return hipGetLastError();
+}
+
+template <int D, int NQ>
+hipError_t launch_out(const CacheFwdParams& p, const Shape& s, bool out_f32,
+                      hipStream_t stream) {
+  return out_f32 ? launch<D, NQ, true>(p, s, stream)
+                 : launch<D, NQ, false>(p, s, stream);
+}
+
+template <int D>
+hipError_t launch_d(const CacheFwdParams& p, const Shape& s, bool out_f32,
+                    hipStream_t stream) {
+  if (s.nq == 1) return launch_out<D, 1>(p, s, out_f32, stream);
+  if (s.nq == 2) return launch_out<D, 2>(p, s, out_f32, stream);
+  return launch_out<D, 4>(p, s, out_f32, stream);
 }
 
 }  // namespace
 
-size_t cache_fwd_workspace(const CacheDims&, int32_t, int32_t, int64_t) {
-  return 0;
+size_t cache_fwd_workspace(const CacheDims& c, int32_t hq, int32_t num_requests,
+                           int64_t rows) {
+  if (rows == 0 || num_requests == 0) return 0;
+  // The most that a call of no more rows and requests needs: 16 rows a tile
+  // and all workgroups, or fewer of both.
+  return size_t{1024} * (sizeof(CacheFold) + 2 * 32 * size_t(c.d + 2) * 4);
 }
 
-hipError_t launch_cache_fwd(const CacheFwdParams& p, bool out_f32, void*,
+hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws,
                             hipStream_t stream) {
-  if (p.c.d == 128) return launch<128, 1>(p, out_f32, stream);
-  return launch<64, 1>(p, out_f32, stream);
+  const Shape s = shape_of(params.c, params.hq, params.num_requests,
+                           params.rows);
+  CacheFwdParams p = params;
+  p.max_tiles = static_cast<int32_t>(s.tiles);
+  p.split = s.split;
+  p.min_units = 1;
+  p.fold = static_cast<CacheFold*>(ws);
+  p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + fold_bytes(s));
+  p.part_ml = p.part_o + part_rows(s) * p.c.d;
+  return p.c.d == 128 ? launch_d<128>(p, s, out_f32, stream)
+                      : launch_d<64>(p, s, out_f32, stream);
 }
 
 }  // namespace mesh_attn

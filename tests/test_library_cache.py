@@ -144,7 +144,8 @@ def _fwd(c=None, hq=4, scale=0.125, num_requests=3, rows=5, q=A, qs=256,
     (dict(scale=float("nan")), "softmax_scale"),
     (dict(num_requests=-1), "num_requests"),
     (dict(num_requests=4097), "num_requests"), (dict(rows=-1), "rows"),
-    (dict(rows=2**31), "rows"), (dict(dtype=2), "o_dtype"),
+    (dict(rows=2**31), "rows"), (dict(rows=2**29), "rows * num_q_heads"),
+    (dict(dtype=2), "o_dtype"),
     (dict(qs=255), "q_stride"), (dict(qs=260), "q_stride"),
     (dict(q=None), "q is NULL"), (dict(q=A + 8), "q is not 16"),
     (dict(positions=None), "positions is NULL"),
