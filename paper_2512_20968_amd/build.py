@@ -31,7 +31,12 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # The forward is scheduled with the target's own register-pressure trackers:
 # its float32-output kernel then fits 256 registers without a spill, and the
 # bf16-output kernel's schedule runs 0.5-1.6 % faster.
-EXTRA = {"tile_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+# The attention over the cache keeps every join's own restore of the execution
+# mask: without it a register that was saved inside a nested branch of the fold
+# was restored for the inner branch's lanes alone (seen in the assembly of the
+# 64-row float32 kernel, whose next item then used it in an address).
+EXTRA = {"cache_fwd.hip": ["-mllvm", "-amdgpu-remove-redundant-endcf=0"],
+         "tile_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "tile_fwd.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers"]}
 
 

@@ -96,9 +96,10 @@ struct CacheFwdParams {
   float* lse;
   int64_t rows;
   int32_t hq, group, num_requests;
-  int32_t max_tiles;  // no more tiles for rows that do not overlap
   float scale_log2;
-  int32_t split, min_units;  // whether sequences are cut; least units of a run
+  int32_t split;      // whether sequences are cut
+  int32_t unit_log2;  // keys of a unit
+  int32_t min_units, max_units;  // least of a run; most of a launch
   CacheFold* fold;           // [workgroup]
   float* part_o;             // [2 * workgroups][rows of a tile][d]
   float* part_ml;            // .. [2]: reference (log2 units) and sum

@@ -389,6 +389,10 @@ __device__ __forceinline__ void store_row(const CacheFwdParams& p, int64_t row,
                                           int head, int dim0,
                                           const float (&acc)[8], float m,
                                           float l) {
+  if (dim0 == 0)
+    p.lse[int64_t{head} * p.rows + row] =
+        l == 0.f ? -INFINITY
+                 : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
   const float inv = l > 0.f ? 1.f / l : l;  // 0 for no key; NaN stays
   const int64_t at = (row * p.hq + head) * D + dim0;
   if (OUT_F32) {
@@ -407,18 +411,6 @@ __device__ __forceinline__ void store_row(const CacheFwdParams& p, int64_t row,
     for (int i = 0; i < 8; ++i) v[i] = static_cast<__bf16>(acc[i] * inv);
     *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.o) + at) = v;
   }
-  if (dim0 == 0)
-    p.lse[int64_t{head} * p.rows + row] =
-        l == 0.f ? -INFINITY
-                 : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
-}
-
-// Rows [first, end) of request b in the packed rows.
-__device__ __forceinline__ void request_rows(const CacheFwdParams& p, int b,
-                                             int* first, int* end) {
-  const int rows = static_cast<int>(p.rows);
-  *first = min(max(load_const(p.cu, b), 0), rows);
-  *end = min(max(load_const(p.cu, b + 1), *first), rows);
 }
 
 __device__ __forceinline__ int32_t stored_keys(const CacheFwdParams& p,
@@ -429,15 +421,82 @@ __device__ __forceinline__ int32_t stored_keys(const CacheFwdParams& p,
 }
 
 // Work of a launch.  A sequence is a tile of a request's rows and a KV head; it
-// is cut into units of 128 keys, a step of each wave (at least one unit, which
-// writes the results of rows without keys).  All sequences' units in a row are
-// dealt to the workgroups in equal runs of `per`, so every workgroup has the
-// same work whatever the lengths, which only the device knows.  A sequence that
-// lies in several runs leaves partial results, two slots a workgroup at most:
-// slot 2 w for the piece that goes on from an earlier run, slot 2 w + 1 for the
-// one that starts in run w and goes on after it; cache_fold_kernel joins them.
-// p.split 0: every sequence is one unit of its own, and no piece is split.
-constexpr int kUnit = kWaves * kStep;
+// is cut into units of 2^unit_log2 keys, a step of each wave or more (at least
+// one unit, which writes the results of rows without keys).  All sequences'
+// units in a row are dealt to the workgroups in equal runs of `per`, so every
+// workgroup has the same work whatever the lengths, which only the device
+// knows.  A sequence that lies in several runs leaves partial results, two slots
+// a workgroup at most: slot 2 w for the piece that goes on from an earlier run,
+// slot 2 w + 1 for the one that starts in run w and goes on after it;
+// cache_fold_kernel joins them.  p.split 0: every sequence is one unit, and no
+// piece is split.
+constexpr int kWaveKeys = kWaves * kStep;  // keys of a step of each wave
+
+// What the prefix sums leave in LDS per request: its first unit, and, for up to
+// kKeptRequests requests, what an item needs (another round trip to memory
+// otherwise).
+constexpr int kKeptRequests = 256;
+
+struct RequestRows {
+  int first, end, local;
+};
+
+__device__ __forceinline__ RequestRows load_request(const CacheFwdParams& p,
+                                                    int b) {
+  const int rows = static_cast<int>(p.rows);
+  RequestRows r;
+  const int a = p.cu[b], e = p.cu[b + 1];
+  r.local = stored_keys(p, p.lens[b]);
+  r.first = min(max(a, 0), rows);
+  r.end = min(max(e, r.first), rows);
+  return r;
+}
+
+// First units of the requests in LDS, by prefix sums over the workgroup; the
+// sums are capped at max_units, which rows that do not overlap cannot pass.
+// Returns the number of units.
+template <int kRows>
+__device__ __forceinline__ int plan_units(const CacheFwdParams& p, int* s_units,
+                                          RequestRows* s_kept, int* s_wave) {
+  const int B = p.num_requests, tid = threadIdx.x, lane = tid & 63;
+  int base = 0;
+  for (int b0 = 0; b0 < B; b0 += NT) {
+    const int b = b0 + tid;
+    int mine = 0;
+    if (b < B) {
+      const RequestRows r = load_request(p, b);
+      if (B <= kKeptRequests) s_kept[b] = r;
+      const uint32_t rr = uint32_t(r.end - r.first) * p.group;  // below 2^30
+      const uint32_t tiles = (rr + kRows - 1) / kRows;
+      const int nu =
+          p.split ? max((r.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1)
+                  : 1;
+      const int64_t n = int64_t{tiles} * nu * p.c.hkv;
+      mine = static_cast<int>(n < p.max_units ? n : p.max_units);
+    }
+    int y = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int z = __shfl_up(y, o);
+      if (lane >= o) y = min(y + z, p.max_units);
+    }
+    int before = __shfl_up(y, 1);  // every lane takes part
+    if (lane == 0) before = 0;
+    if (lane == 63) s_wave[tid >> 6] = y;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < (tid >> 6)) before = min(before + s_wave[w], p.max_units);
+    }
+    if (b < B) s_units[b] = min(base + before, p.max_units);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) base = min(base + s_wave[w], p.max_units);
+    __syncthreads();
+  }
+  if (tid == 0) s_units[B] = base;
+  __syncthreads();
+  return base;
+}
 
 template <int D, int NQ, bool OUT_F32, bool P16>
 __global__ __launch_bounds__(NT, NQ == 1 ? 4 : NQ == 2 ? 3 : 2)
@@ -447,59 +506,22 @@ void cache_fwd_kernel(CacheFwdParams p) {
   __shared__ float s_o[kWaves][16][kPad];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
   __shared__ bf16x8 s_q[kQInLds<NQ> ? NQ * (D / 32) * 64 : 1];
-  extern __shared__ int64_t s_units[];  // [B + 1] first unit of a request
+  __shared__ int s_wave[kWaves];
+  extern __shared__ int s_units[];  // [B + 1], then the kept requests
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int B = p.num_requests, hkv = p.c.hkv;
+  RequestRows* s_kept = reinterpret_cast<RequestRows*>(s_units + B + 1);
 
-  // First units of the requests: prefix sums by one wave.
-  if (wave == 0) {
-    int64_t base = 0;
-    int tiles = 0;  // so far; capped, in case rows overlap
-    for (int b0 = 0; b0 < B; b0 += 64) {
-      const int b = b0 + lane;
-      int n = 0, nu = 1;
-      if (b < B) {
-        int first, end;
-        request_rows(p, b, &first, &end);
-        const uint32_t rr = uint32_t(end - first) * p.group;  // below 2^31
-        n = min(int((rr + kRows - 1) / kRows), p.max_tiles);
-        if (p.split)
-          nu = max((stored_keys(p, p.lens[b]) + kUnit - 1) / kUnit, 1);
-      }
-      int y = n;
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) {
-        const int z = __shfl_up(y, o);
-        if (lane >= o) y = min(y + z, p.max_tiles);
-      }
-      // This request's tiles under the cap.  (Every lane takes part in the
-      // shuffle: one that does not would have nothing to give.)
-      int before = __shfl_up(y, 1);
-      if (lane == 0) before = 0;
-      n = min(tiles + y, p.max_tiles) - min(tiles + before, p.max_tiles);
-      tiles = min(tiles + __shfl(y, 63), p.max_tiles);
-      int64_t u = int64_t{n} * nu * hkv;
-      const int64_t mine = u;
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) {
-        const int64_t z = __shfl_up(u, o);
-        if (lane >= o) u += z;
-      }
-      if (b < B) s_units[b] = base + u - mine;
-      base += __shfl(u, 63);
-    }
-    if (lane == 0) s_units[B] = base;
-  }
-  __syncthreads();
-  const int64_t total = s_units[B];
-  int64_t per = 1, at = blockIdx.x, stop = total;
+  const int total = __builtin_amdgcn_readfirstlane(
+      plan_units<kRows>(p, s_units, s_kept, s_wave));
+  int per = 1, at = blockIdx.x, stop = total;
   if (p.split) {
-    per = (total + gridDim.x - 1) / gridDim.x;
-    per = per > p.min_units ? per : p.min_units;
-    at = per * blockIdx.x;
-    stop = at + per < total ? at + per : total;
+    per = max((total + int(gridDim.x) - 1) / int(gridDim.x), p.min_units);
+    // Below 2^31: per * gridDim < total + gridDim * min_units.
+    at = per * int(blockIdx.x);
+    stop = min(at + per, total);
     if (tid == 0) p.fold[blockIdx.x].parts = 0;
   }
 
@@ -513,22 +535,18 @@ void cache_fwd_kernel(CacheFwdParams p) {
         hi = mid;
     }
     const int b = __builtin_amdgcn_readfirstlane(lo);
-    int first, end;
-    request_rows(p, b, &first, &end);
-    const int rr_end = (end - first) * p.group;
+    RequestRows req = B <= kKeptRequests ? s_kept[b] : load_request(p, b);
+    const int first = __builtin_amdgcn_readfirstlane(req.first);
+    const int rr_end =
+        __builtin_amdgcn_readfirstlane(req.end - req.first) * p.group;
     Keys h;
-    h.local = stored_keys(p, load_const(p.lens, b));
-    const int nu = p.split ? max((h.local + kUnit - 1) / kUnit, 1) : 1;
-    const int64_t off = at - s_units[b];
-    const int seq = __builtin_amdgcn_readfirstlane(int(off / nu));
-    const int u0 =
-        __builtin_amdgcn_readfirstlane(int(off - int64_t{seq} * nu));
-    const int64_t left = stop - at;
-    const int u1 = p.split ? __builtin_amdgcn_readfirstlane(
-                                 int(u0 + left < nu ? u0 + left : nu))
-                           : 1;
-    const int rr0 = __builtin_amdgcn_readfirstlane(seq / hkv) * kRows;
-    const int kvh = seq - rr0 / kRows * hkv;
+    h.local = __builtin_amdgcn_readfirstlane(req.local);
+    const int nu =
+        p.split ? max((h.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1) : 1;
+    const int off = at - __builtin_amdgcn_readfirstlane(s_units[b]);
+    const int seq = off / nu, u0 = off - seq * nu;
+    const int u1 = p.split ? min(u0 + (stop - at), nu) : 1;
+    const int tile = seq / hkv, kvh = seq - tile * hkv, rr0 = tile * kRows;
 
     h.lg = p.c.page_log2;
     h.num_pages = p.c.num_pages;
@@ -538,18 +556,26 @@ void cache_fwd_kernel(CacheFwdParams p) {
     h.base = p.data + int64_t{kvh} * p.c.block_bytes();
     lane_offsets<D>(&h, r, g);
 
+    // First key of the wave, end of the piece.  The first step's loads go out
+    // with those of Q and the positions.
+    int kb = (p.split ? u0 << p.unit_log2 : 0) + wave * kStep;
+    const int piece_end =
+        p.split ? min(int64_t{u1} << p.unit_log2, int64_t{h.local}) : h.local;
+    StepPages pg = load_pages<P16>(h, kb);
+
     State<D, NQ> st;
-    int most_seen = 0, all_see = INT32_MAX;
+    int pos[NQ];
     if (kQInLds<NQ>) __syncthreads();  // the last item's Q has been read
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      const bool valid = rr0 + 16 * q + r < rr_end;
-      const uint32_t rr = valid ? rr0 + 16 * q + r : rr0;
+      const int mine = rr0 + 16 * q + r;
+      const uint32_t rr = mine < rr_end ? mine : rr0;
       const uint32_t tok = rr / uint32_t(p.group);
       const int64_t row = first + int64_t{tok};
       const int head = kvh * p.group + int(rr - tok * p.group);
       const uint16_t* src =
           p.q + row * p.q_stride + int64_t{head} * D + g * (D / 4);
+      pos[q] = p.positions[row];
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         if constexpr (!kQInLds<NQ>)
@@ -558,9 +584,19 @@ void cache_fwd_kernel(CacheFwdParams p) {
           s_q[(q * (D / 32) + c) * 64 + lane] =
               *reinterpret_cast<const bf16x8*>(src + 8 * c);
       }
-      const int64_t pos = p.positions[row];
-      st.vis[q] =
-          valid ? min(p.c.share.below(pos < 0 ? 0 : pos + 1), h.local) : 0;
+    }
+    StepData<D> s;
+    if (kb < piece_end) {
+      load_k<D, P16>(h, pg, kb, r, &s);
+      load_v<D, P16>(h, pg, kb, g, &s);
+    }
+    int most_seen = 0, all_see = INT32_MAX;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const bool valid = rr0 + 16 * q + r < rr_end;
+      st.vis[q] = valid ? min(p.c.share.below(int64_t{max(pos[q], -1)} + 1),
+                              h.local)
+                        : 0;
       most_seen = max(most_seen, st.vis[q]);
       if (valid) all_see = min(all_see, st.vis[q]);
       st.m[q] = -INFINITY;
@@ -580,17 +616,14 @@ void cache_fwd_kernel(CacheFwdParams p) {
     // The next step's K is loaded into the registers of this one's as soon as
     // the first product has read them, its V after the second: each is in
     // flight for about half a step, without registers of its own.
-    const int kend = p.split ? min(u1 * kUnit, most_seen) : most_seen;
-    int kb = u0 * kUnit + wave * kStep;
+    const int kend = min(piece_end, most_seen);
     if (kb < kend) {
-      StepData<D> s;
-      StepPages pg = load_pages<P16>(h, kb);
-      load_k<D, P16>(h, pg, kb, r, &s);
-      load_v<D, P16>(h, pg, kb, g, &s);
       for (;;) {
-        const int next = kb + kUnit;
+        const int next = kb + kWaveKeys;
         const bool more = next < kend;
         const StepPages pn = load_pages<P16>(h, next);
+        // Q's LDS reads stay in the loop (its registers are needed).
+        if constexpr (kQInLds<NQ>) asm volatile("" ::: "memory");
         f32x4 x[NQ][2];
         score_step<D, NQ>(st, s_q, s, lane, x);
         if (more) load_k<D, P16>(h, pn, next, r, &s);
@@ -615,7 +648,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
       f.rr_end = rr_end;
       f.kvh = kvh;
       // Runs that the sequence's units lie in.
-      f.parts = static_cast<int32_t>((at + nu - 1) / per - blockIdx.x + 1);
+      f.parts = min((at + nu - 1) / per, int(gridDim.x) - 1) - int(blockIdx.x) +
+                1;
       p.fold[blockIdx.x] = f;
     }
     // Fold the waves, 16 rows at a time.
@@ -659,17 +693,17 @@ void cache_fwd_kernel(CacheFwdParams p) {
                                 dim0, acc, ref, L);
         } else {
           const int64_t pr = int64_t{slot} * kRows + 16 * q + row16;
-          f32x4* dst = reinterpret_cast<f32x4*>(p.part_o + pr * D + dim0);
-          dst[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
-          dst[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
           if (dim0 == 0) {
             p.part_ml[2 * pr] = M;
             p.part_ml[2 * pr + 1] = L;
           }
+          f32x4* dst = reinterpret_cast<f32x4*>(p.part_o + pr * D + dim0);
+          dst[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+          dst[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
         }
       }
     }
-    at += p.split ? u1 - u0 : int64_t{gridDim.x};
+    at += p.split ? u1 - u0 : int(gridDim.x);
   }
 }
 
@@ -748,9 +782,8 @@ void cache_fold_kernel(CacheFwdParams p) {
 // How a call is launched, from its sizes alone.
 struct Shape {
   int nq;          // 16-row columns per tile
-  int64_t tiles;   // most tiles of all requests together
   bool split;
-  int grid;
+  int grid, unit_log2, max_units;
 };
 
 Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
@@ -760,11 +793,18 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   // Rows of a request, were they all alike.
   const int64_t each = (rows + num_requests - 1) / num_requests * group;
   s.nq = each <= 16 ? 1 : each <= 32 ? 2 : 4;
-  s.tiles = rows * group / (16 * s.nq) + num_requests;
-  if (s.tiles > 1 << 29) s.tiles = 1 << 29;  // sums of two fit 32 bits
-  const int64_t seqs = s.tiles * c.hkv;
+  // Most sequences that rows which do not overlap make.
+  const int64_t seqs = (rows * group / (16 * s.nq) + num_requests) * c.hkv;
   const int slots = s.nq == 1 ? 1024 : s.nq == 2 ? 768 : 512;
-  s.split = (int64_t{c.max_pages} << c.page_log2) > kUnit && seqs < 4 * slots;
+  const int64_t keys = int64_t{c.max_pages} << c.page_log2;
+  s.split = keys > kWaveKeys && seqs < 4 * slots;
+  s.unit_log2 = 7;
+  static_assert(kWaveKeys == 1 << 7, "least unit");
+  // Units are counted in 32 bits.
+  const int64_t most = int64_t{1} << 30;
+  while (s.split && seqs * ((keys >> s.unit_log2) + 1) >= most) ++s.unit_log2;
+  const int64_t units = s.split ? seqs * ((keys >> s.unit_log2) + 1) : seqs;
+  s.max_units = static_cast<int>(units < most ? units : most - 1);
   const int64_t grid = s.split ? slots : seqs;
   s.grid = static_cast<int>(grid < 65536 ? grid : 65536);
   return s;
@@ -777,7 +817,9 @@ size_t part_rows(const Shape& s) { return size_t{32} * s.nq * s.grid; }
 
 template <int D, int NQ, bool OUT_F32>
 hipError_t launch(const CacheFwdParams& p, const Shape& s, hipStream_t stream) {
-  const size_t lds = (static_cast<size_t>(p.num_requests) + 1) * 8;
+  const size_t n = static_cast<size_t>(p.num_requests);
+  const size_t lds =
+      (n + 1) * 4 + (n <= kKeptRequests ? n * sizeof(RequestRows) : 0);
   const dim3 grid(static_cast<unsigned>(s.grid));
   if (p.c.page_log2 == 4)
     hipLaunchKernelGGL((cache_fwd_kernel<D, NQ, OUT_F32, true>), grid, dim3(NT),
@@ -822,8 +864,9 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
   const Shape s = shape_of(params.c, params.hq, params.num_requests,
                            params.rows);
   CacheFwdParams p = params;
-  p.max_tiles = static_cast<int32_t>(s.tiles);
   p.split = s.split;
+  p.unit_log2 = s.unit_log2;
+  p.max_units = s.max_units;
   p.min_units = 1;
   p.fold = static_cast<CacheFold*>(ws);
   p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + fold_bytes(s));
