@@ -27,6 +27,7 @@
 #include <stdint.h>
 
 #include "cache_codes.h"
+#include "tile_common.h"
 
 namespace mesh_attn {
 namespace {
@@ -36,20 +37,6 @@ using namespace dev;
 constexpr int NT = 256;
 constexpr int kWaves = NT / 64;
 constexpr int kStep = 32;  // keys of a wave's step
-
-// Read-only data through the constant address space: uniform addresses become
-// scalar loads.
-template <typename T>
-__device__ __forceinline__ T load_const(const T* p, int64_t i) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  typedef const __attribute__((address_space(4))) T* cptr;
-  T v;
-  __builtin_memcpy(&v, (cptr)(p) + i, sizeof(T));
-  return v;
-#else
-  return p[i];
-#endif
-}
 
 __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b,
                                         const f32x4& c) {
@@ -139,7 +126,8 @@ __device__ __forceinline__ void load_k(const Keys& h, const StepPages& pages,
   const uint32_t t0 = kb & ((1 << h.lg) - 1);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const uint8_t* at = kp + t0 * (D / 2) + h.kc + t * (4 * (D / 2));
+    // Offsets are summed in 32 bits: a scalar base and one register.
+    const uint8_t* at = kp + (t0 * (D / 2) + h.kc + t * (4 * (D / 2)));
     if constexpr (D == 128) {
       const u32x4 w = load_at<u32x4>(at);
 #pragma unroll
@@ -160,11 +148,11 @@ __device__ __forceinline__ void load_v(const Keys& h, const StepPages& pages,
   const uint32_t t0 = kb & ((1 << h.lg) - 1);
 #pragma unroll
   for (int j = 0; j < D / 64; ++j) {
-    const u32x4 w = load_at<u32x4>(vp + t0 * (D / 2) + h.vc + 16 * j);
+    const u32x4 w = load_at<u32x4>(vp + (t0 * (D / 2) + h.vc + 16 * j));
 #pragma unroll
     for (int i = 0; i < 4; ++i) s->vc[4 * j + i] = w[i];
   }
-  s->vs = load_at<u32x2>(vp + t0 + h.vs);
+  s->vs = load_at<u32x2>(vp + (t0 + h.vs));
 }
 
 // The lane's offsets for pages of 2^lg tokens.
@@ -425,7 +413,8 @@ __device__ __forceinline__ int32_t stored_keys(const CacheFwdParams& p,
 // one unit, which writes the results of rows without keys).  All sequences'
 // units in a row are dealt to the workgroups in equal runs of `per`, so every
 // workgroup has the same work whatever the lengths, which only the device
-// knows.  A sequence that lies in several runs leaves partial results, two slots
+// knows.  What a sequence costs beside its keys (finding it, the first loads, the
+// fold) counts as seq_units units in front of them.  A sequence that lies in several runs leaves partial results, two slots
 // a workgroup at most: slot 2 w for the piece that goes on from an earlier run,
 // slot 2 w + 1 for the one that starts in run w and goes on after it;
 // cache_fold_kernel joins them.  p.split 0: every sequence is one unit, and no
@@ -471,7 +460,7 @@ __device__ __forceinline__ int plan_units(const CacheFwdParams& p, int* s_units,
       const int nu =
           p.split ? max((r.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1)
                   : 1;
-      const int64_t n = int64_t{tiles} * nu * p.c.hkv;
+      const int64_t n = int64_t{tiles} * (nu + p.seq_units) * p.c.hkv;
       mine = static_cast<int>(n < p.max_units ? n : p.max_units);
     }
     int y = mine;
@@ -498,8 +487,76 @@ __device__ __forceinline__ int plan_units(const CacheFwdParams& p, int* s_units,
   return base;
 }
 
+// The thread's index, not known to be the same from call to call: what is
+// derived from it is computed where it is used instead of being held in
+// registers through the loop over the keys.
+__device__ __forceinline__ int fresh_tid() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
+// Waves per SIMD: as many as the registers allow with few spills.  Head dim 128,
+// 16 rows: 3 (768 workgroups) read 1.1 GB in 209 us, 4 with spills 239; 32 rows:
+// 2 take 80 us for 16 requests of 8 rows each over 16K tokens, 3 with spills 127.
+template <int D, int NQ>
+constexpr int kWavesPerSimd = D == 64 ? (NQ == 1 ? 4 : NQ == 2 ? 3 : 2)
+                                      : (NQ == 1 ? 3 : 2);
+
+// An item of a workgroup: units [u0, u1) of the nu of a sequence (none if the
+// run ends before the keys), the last of them before `end` in all units.
+struct Item {
+  int b, first, rr0, rr_end, kvh, u0, u1, nu, local, end;
+};
+
+// The item at unit `at` of a run that ends at `stop`.
+template <int kRows>
+__device__ __forceinline__ Item locate(const CacheFwdParams& p,
+                                       const int* s_units,
+                                       const RequestRows* s_kept, int at,
+                                       int stop) {
+  const int B = p.num_requests, hkv = p.c.hkv;
+  int lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (s_units[mid] <= at)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  Item it;
+  it.b = __builtin_amdgcn_readfirstlane(lo);
+  const RequestRows req =
+      B <= kKeptRequests ? s_kept[it.b] : load_request(p, it.b);
+  it.first = __builtin_amdgcn_readfirstlane(req.first);
+  it.rr_end = __builtin_amdgcn_readfirstlane(req.end - req.first) * p.group;
+  it.local = __builtin_amdgcn_readfirstlane(req.local);
+  it.nu =
+      p.split ? max((it.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1) : 1;
+  const int off = at - __builtin_amdgcn_readfirstlane(s_units[it.b]);
+  const int len = it.nu + p.seq_units, seq = off / len;
+  const int v0 = off - seq * len;  // of the sequence's units with its cost
+  it.u0 = max(v0 - p.seq_units, 0);
+  it.u1 = p.split ? min(v0 + (stop - at) - p.seq_units, it.nu) : 1;
+  it.end = p.split ? min(at - v0 + len, stop) : at + int(gridDim.x);
+  int tile;
+  if (p.split) {
+    // Runs of neighbouring tiles of a head read the same keys.
+    const int tiles = (it.rr_end + kRows - 1) / kRows;
+    it.kvh = seq / tiles;
+    tile = seq - it.kvh * tiles;
+  } else {
+    // Workgroup i runs on XCD i % 8: with a multiple of 8 heads, a head's keys
+    // are read through one L2.
+    tile = seq / hkv;
+    it.kvh = seq - tile * hkv;
+  }
+  it.rr0 = tile * kRows;
+  return it;
+}
+
 template <int D, int NQ, bool OUT_F32, bool P16>
-__global__ __launch_bounds__(NT, NQ == 1 ? 4 : NQ == 2 ? 3 : 2)
+__global__ __launch_bounds__(NT, (kWavesPerSimd<D, NQ>))
 void cache_fwd_kernel(CacheFwdParams p) {
   constexpr int kRows = 16 * NQ;
   constexpr int kPad = D + 4;  // row stride of the fold, in floats
@@ -511,91 +568,151 @@ void cache_fwd_kernel(CacheFwdParams p) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int B = p.num_requests, hkv = p.c.hkv;
-  RequestRows* s_kept = reinterpret_cast<RequestRows*>(s_units + B + 1);
+  RequestRows* s_kept =
+      reinterpret_cast<RequestRows*>(s_units + p.num_requests + 1);
 
   const int total = __builtin_amdgcn_readfirstlane(
       plan_units<kRows>(p, s_units, s_kept, s_wave));
-  int per = 1, at = blockIdx.x, stop = total;
+  // Split: this workgroup's run.  Workgroup i runs on XCD i % 8; neighbouring
+  // runs go to one XCD (the grid is a multiple of 8), whose L2 then serves the
+  // tiles of a head, and the runs with work spread over all of them.
+  int run = blockIdx.x, per = 1, at = run, stop = total;
   if (p.split) {
     per = max((total + int(gridDim.x) - 1) / int(gridDim.x), p.min_units);
+    const int active = (total + per - 1) / per;
+    const int each = (active + 7) / 8;  // of an XCD
+    const int x = blockIdx.x % 8, y = blockIdx.x / 8;
+    // The others take the runs behind the active ones, without work.
+    run = y < each ? x * each + y
+                   : 8 * each + x * (int(gridDim.x / 8) - each) + y - each;
     // Below 2^31: per * gridDim < total + gridDim * min_units.
-    at = per * int(blockIdx.x);
+    at = per * run;
     stop = min(at + per, total);
-    if (tid == 0) p.fold[blockIdx.x].parts = 0;
+    if (tid == 0) p.fold[run].parts = 0;
   }
 
-  while (at < stop) {
-    int lo = 0, hi = B;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (s_units[mid] <= at)
-        lo = mid;
-      else
-        hi = mid;
+  State<D, NQ> st;
+  Item it, prev;
+  bool have_prev = false;
+  for (;;) {
+    bool more = false;
+    while (at < stop && !more) {
+      it = locate<kRows>(p, s_units, s_kept, at, stop);
+      at = it.end;
+      more = it.u0 < it.u1;
     }
-    const int b = __builtin_amdgcn_readfirstlane(lo);
-    RequestRows req = B <= kKeptRequests ? s_kept[b] : load_request(p, b);
-    const int first = __builtin_amdgcn_readfirstlane(req.first);
-    const int rr_end =
-        __builtin_amdgcn_readfirstlane(req.end - req.first) * p.group;
     Keys h;
-    h.local = __builtin_amdgcn_readfirstlane(req.local);
-    const int nu =
-        p.split ? max((h.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1) : 1;
-    const int off = at - __builtin_amdgcn_readfirstlane(s_units[b]);
-    const int seq = off / nu, u0 = off - seq * nu;
-    const int u1 = p.split ? min(u0 + (stop - at), nu) : 1;
-    const int tile = seq / hkv, kvh = seq - tile * hkv, rr0 = tile * kRows;
-
-    h.lg = p.c.page_log2;
-    h.num_pages = p.c.num_pages;
-    h.table = p.block_table + int64_t{b} * p.c.max_pages;
-    h.last_page = max((h.local - 1) >> h.lg, 0);
-    h.page_bytes = int64_t{hkv} * p.c.block_bytes();
-    h.base = p.data + int64_t{kvh} * p.c.block_bytes();
-    lane_offsets<D>(&h, r, g);
-
-    // First key of the wave, end of the piece.  The first step's loads go out
-    // with those of Q and the positions.
-    int kb = (p.split ? u0 << p.unit_log2 : 0) + wave * kStep;
-    const int piece_end =
-        p.split ? min(int64_t{u1} << p.unit_log2, int64_t{h.local}) : h.local;
-    StepPages pg = load_pages<P16>(h, kb);
-
-    State<D, NQ> st;
-    int pos[NQ];
-    if (kQInLds<NQ>) __syncthreads();  // the last item's Q has been read
+    StepPages pg;
+    StepData<D> s;
+    int pos[NQ], kb = 0, piece_end = 0;
+    if (more) {
+      // The first step's loads go out with those of Q and the positions, and
+      // all of them before the last item's fold.
+      h.lg = p.c.page_log2;
+      h.num_pages = p.c.num_pages;
+      h.table = p.block_table + int64_t{it.b} * p.c.max_pages;
+      h.local = it.local;
+      h.last_page = max((it.local - 1) >> h.lg, 0);
+      h.page_bytes = int64_t{p.c.hkv} * p.c.block_bytes();
+      h.base = p.data + int64_t{it.kvh} * p.c.block_bytes();
+      lane_offsets<D>(&h, r, g);
+      kb = (p.split ? it.u0 << p.unit_log2 : 0) + wave * kStep;
+      piece_end = p.split ? min(int64_t{it.u1} << p.unit_log2,
+                                int64_t{it.local})
+                          : it.local;
+      pg = load_pages<P16>(h, kb);
+      if (kQInLds<NQ>) lds_barrier();  // the last item's Q has been read
+      const int t = fresh_tid(), r = t & 15, g = (t & 63) >> 4, lane = t & 63;
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      const int mine = rr0 + 16 * q + r;
-      const uint32_t rr = mine < rr_end ? mine : rr0;
-      const uint32_t tok = rr / uint32_t(p.group);
-      const int64_t row = first + int64_t{tok};
-      const int head = kvh * p.group + int(rr - tok * p.group);
-      const uint16_t* src =
-          p.q + row * p.q_stride + int64_t{head} * D + g * (D / 4);
-      pos[q] = p.positions[row];
+      for (int q = 0; q < NQ; ++q) {
+        const int mine = it.rr0 + 16 * q + r;
+        const uint32_t rr = mine < it.rr_end ? mine : it.rr0;
+        const uint32_t tok = rr / uint32_t(p.group);
+        const int64_t row = it.first + int64_t{tok};
+        const int head = it.kvh * p.group + int(rr - tok * p.group);
+        const uint16_t* src =
+            p.q + row * p.q_stride + int64_t{head} * D + g * (D / 4);
+        pos[q] = p.positions[row];
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        if constexpr (!kQInLds<NQ>)
-          st.q[q][c] = *reinterpret_cast<const bf16x8*>(src + 8 * c);
-        else if (q % kWaves == wave)
-          s_q[(q * (D / 32) + c) * 64 + lane] =
-              *reinterpret_cast<const bf16x8*>(src + 8 * c);
+        for (int c = 0; c < D / 32; ++c) {
+          if constexpr (!kQInLds<NQ>)
+            st.q[q][c] = *reinterpret_cast<const bf16x8*>(src + 8 * c);
+          else if (q % kWaves == wave)
+            s_q[(q * (D / 32) + c) * 64 + lane] =
+                *reinterpret_cast<const bf16x8*>(src + 8 * c);
+        }
+      }
+      if (kb < piece_end) {
+        load_k<D, P16>(h, pg, kb, r, &s);
+        load_v<D, P16>(h, pg, kb, g, &s);
       }
     }
-    StepData<D> s;
-    if (kb < piece_end) {
-      load_k<D, P16>(h, pg, kb, r, &s);
-      load_v<D, P16>(h, pg, kb, g, &s);
+
+    if (have_prev) {
+      // Fold the waves, 16 rows at a time.
+      const bool whole = prev.u0 == 0 && prev.u1 == prev.nu;
+      const int slot = 2 * run + (prev.u0 == 0 ? 1 : 0);
+      const int tid = fresh_tid(), r = tid & 15, g = (tid & 63) >> 4;
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        if (prev.rr0 + 16 * q >= prev.rr_end) break;
+        const float l = across_quarters(
+            st.l[q], [](float a, float b) { return a + b; });
+        lds_barrier();
+        if (g == 0) {
+          s_m[wave][r] = st.m[q];
+          s_l[wave][r] = l;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int m = 0; m < D / 16; ++m)
+            s_o[wave][r][g * (D / 4) + i * (D / 16) + m] = st.o[q][m][i];
+        lds_barrier();
+        const int row16 = tid / (D / 8), dim0 = tid % (D / 8) * 8;
+        const int rr = prev.rr0 + 16 * q + row16;
+        if (row16 < 16 && rr < prev.rr_end) {
+          float M = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][row16]);
+          const float ref = M == -INFINITY ? 0.f : M;
+          float L = 0.f, acc[8] = {};
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) {
+            // A wave without a maximum has sums of 0, or of NaN.
+            const float sm = s_m[w][row16] == -INFINITY
+                                 ? 1.f
+                                 : __builtin_amdgcn_exp2f(s_m[w][row16] - ref);
+            L += s_l[w][row16] * sm;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += s_o[w][row16][dim0 + i] * sm;
+          }
+          if (whole) {
+            store_row<D, OUT_F32>(p, prev.first + rr / p.group,
+                                  prev.kvh * p.group + rr % p.group, dim0, acc,
+                                  ref, L);
+          } else {
+            const int64_t pr = int64_t{slot} * kRows + 16 * q + row16;
+            if (dim0 == 0) {
+              p.part_ml[2 * pr] = M;
+              p.part_ml[2 * pr + 1] = L;
+            }
+            f32x4* dst = reinterpret_cast<f32x4*>(p.part_o + pr * D + dim0);
+            dst[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+            dst[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
+          }
+        }
+      }
     }
+    if (!more) break;
+
     int most_seen = 0, all_see = INT32_MAX;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      const bool valid = rr0 + 16 * q + r < rr_end;
+      const int r = fresh_tid() & 15;
+      const bool valid = it.rr0 + 16 * q + r < it.rr_end;
       st.vis[q] = valid ? min(p.c.share.below(int64_t{max(pos[q], -1)} + 1),
-                              h.local)
+                              it.local)
                         : 0;
       most_seen = max(most_seen, st.vis[q]);
       if (valid) all_see = min(all_see, st.vis[q]);
@@ -611,7 +728,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
     }
     most_seen = __builtin_amdgcn_readfirstlane(most_seen);
     all_see = __builtin_amdgcn_readfirstlane(all_see);
-    if (kQInLds<NQ>) __syncthreads();
+    if (kQInLds<NQ>) lds_barrier();
 
     // The next step's K is loaded into the registers of this one's as soon as
     // the first product has read them, its V after the second: each is in
@@ -620,116 +737,76 @@ void cache_fwd_kernel(CacheFwdParams p) {
     if (kb < kend) {
       for (;;) {
         const int next = kb + kWaveKeys;
-        const bool more = next < kend;
+        const bool more_keys = next < kend;
         const StepPages pn = load_pages<P16>(h, next);
         // Q's LDS reads stay in the loop (its registers are needed).
         if constexpr (kQInLds<NQ>) asm volatile("" ::: "memory");
         f32x4 x[NQ][2];
+        // The wave with matrix instructions to issue goes first: the other
+        // waves' vector work fits between them.
+        __builtin_amdgcn_s_setprio(1);
         score_step<D, NQ>(st, s_q, s, lane, x);
-        if (more) load_k<D, P16>(h, pn, next, r, &s);
+        __builtin_amdgcn_s_setprio(0);
+        if (more_keys) load_k<D, P16>(h, pn, next, r, &s);
         u32x2 vs = s.vs;
         const bool ok = lane_ok<P16>(h, pg, g);
         if (kb + kStep > all_see || !__all(ok))
           vs = mask_step<D, NQ>(st, x, s, ok, kb, h.local, g);
         finish_step<D, NQ, OUT_F32>(st, x, s, p.scale_log2, vs);
-        if (!more) break;
+        if (!more_keys) break;
         load_v<D, P16>(h, pn, next, g, &s);
         pg = pn;
         kb = next;
       }
     }
 
-    const bool whole = u0 == 0 && u1 == nu;
-    const int slot = 2 * blockIdx.x + (u0 == 0 ? 1 : 0);
-    if (p.split && u0 == 0 && !whole && tid == 0) {
+    if (p.split && it.u0 == 0 && it.u1 < it.nu && tid == 0) {
       CacheFold f;
-      f.first = first;
-      f.rr0 = rr0;
-      f.rr_end = rr_end;
-      f.kvh = kvh;
-      // Runs that the sequence's units lie in.
-      f.parts = min((at + nu - 1) / per, int(gridDim.x) - 1) - int(blockIdx.x) +
-                1;
-      p.fold[blockIdx.x] = f;
+      f.first = it.first;
+      f.rr0 = it.rr0;
+      f.rr_end = it.rr_end;
+      f.kvh = it.kvh;
+      // Runs that the sequence's keys lie in: this one, which ends at `stop`
+      // after u1 of them, and those of the rest.
+      f.parts = min((it.nu - it.u1 + per - 1) / per,
+                    int(gridDim.x) - 1 - run) + 1;
+      p.fold[run] = f;
     }
-    // Fold the waves, 16 rows at a time.
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      if (rr0 + 16 * q >= rr_end) break;
-      const float l = across_quarters(
-          st.l[q], [](float a, float b) { return a + b; });
-      __syncthreads();
-      if (g == 0) {
-        s_m[wave][r] = st.m[q];
-        s_l[wave][r] = l;
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int m = 0; m < D / 16; ++m)
-          s_o[wave][r][g * (D / 4) + i * (D / 16) + m] = st.o[q][m][i];
-      __syncthreads();
-      const int row16 = tid / (D / 8), dim0 = tid % (D / 8) * 8;
-      const int rr = rr0 + 16 * q + row16;
-      if (row16 < 16 && rr < rr_end) {
-        float M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][row16]);
-        const float ref = M == -INFINITY ? 0.f : M;
-        float L = 0.f, acc[8] = {};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          // A wave without a maximum has sums of 0, or of NaN.
-          const float sm = s_m[w][row16] == -INFINITY
-                               ? 1.f
-                               : __builtin_amdgcn_exp2f(s_m[w][row16] - ref);
-          L += s_l[w][row16] * sm;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) acc[i] += s_o[w][row16][dim0 + i] * sm;
-        }
-        if (whole) {
-          store_row<D, OUT_F32>(p, first + rr / p.group,
-                                kvh * p.group + rr % p.group,
-                                dim0, acc, ref, L);
-        } else {
-          const int64_t pr = int64_t{slot} * kRows + 16 * q + row16;
-          if (dim0 == 0) {
-            p.part_ml[2 * pr] = M;
-            p.part_ml[2 * pr + 1] = L;
-          }
-          f32x4* dst = reinterpret_cast<f32x4*>(p.part_o + pr * D + dim0);
-          dst[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
-          dst[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
-        }
-      }
-    }
-    at += p.split ? u1 - u0 : int(gridDim.x);
+    prev = it;
+    have_prev = true;
   }
 }
 
 // Joins the partial results of the sequence that starts in run blockIdx.x and
 // goes on after it: slots 2 w + 1, 2 (w + 1), 2 (w + 2), .. in that order,
-// whatever order they were made in.  Eight dims per thread, kFoldRows rows at a
-// time, the pieces dealt to kFoldParts threads.
-constexpr int kFoldRows = 4, kFoldParts = 8;
+// whatever order they were made in.  Eight dims per thread; a few pieces are
+// walked by one thread, many by kFoldParts threads, whose results are joined
+// through LDS.
+constexpr int kFoldThreads = 512, kFoldParts = 8;
 
 template <int D, int NQ, bool OUT_F32>
-__global__ __launch_bounds__(kFoldRows * kFoldParts * (D / 8))
+__global__ __launch_bounds__(kFoldThreads)
 void cache_fold_kernel(CacheFwdParams p) {
   constexpr int kRows = 16 * NQ, kDimThreads = D / 8;
-  __shared__ float s_acc[kFoldParts][kFoldRows][D];
-  __shared__ float s_m[kFoldParts][kFoldRows], s_l[kFoldParts][kFoldRows];
+  constexpr int kRowThreads = kFoldThreads / kDimThreads;
+  constexpr int kManyRows = kRowThreads / kFoldParts;
+  __shared__ float s_acc[kFoldParts][kManyRows][D];
+  __shared__ float s_m[kFoldParts][kManyRows], s_l[kFoldParts][kManyRows];
   const int w = blockIdx.x;
   const CacheFold f = load_const(p.fold, w);
   if (f.parts < 2) return;
   const int dim0 = threadIdx.x % kDimThreads * 8;
-  const int row4 = threadIdx.x / kDimThreads % kFoldRows;
-  const int pg = threadIdx.x / (kDimThreads * kFoldRows);
-  for (int q0 = 0; q0 < kRows; q0 += kFoldRows) {
+  const int t = threadIdx.x / kDimThreads;
+  const bool many = f.parts > 4;
+  const int at_once = many ? kManyRows : kRowThreads;
+  const int pg = many ? t / kManyRows : 0;
+  const int step = many ? kFoldParts : 1;
+  const int my_row = many ? t % kManyRows : t;
+  for (int q0 = 0; q0 < kRows; q0 += at_once) {
     if (f.rr0 + q0 >= f.rr_end) return;
-    const int row = q0 + row4;
+    const int row = q0 + my_row;
     const int rr = f.rr0 + row;
-    const bool valid = rr < f.rr_end;
+    const bool valid = row < kRows && rr < f.rr_end;
     float M = -INFINITY, L = 0.f, acc[8] = {};
     auto fold = [&](float m, float l, const float* x) {
       const float mn = fmaxf(M, m);
@@ -742,7 +819,8 @@ void cache_fold_kernel(CacheFwdParams p) {
       M = mn;
     };
     if (valid)
-      for (int i = pg; i < f.parts; i += kFoldParts) {
+#pragma unroll 4
+      for (int i = pg; i < f.parts; i += step) {
         const int64_t slot = i == 0 ? 2 * int64_t{w} + 1 : 2 * (int64_t{w} + i);
         const int64_t pr = slot * kRows + row;
         float x[8];
@@ -756,26 +834,26 @@ void cache_fold_kernel(CacheFwdParams p) {
         }
         fold(p.part_ml[2 * pr], p.part_ml[2 * pr + 1], x);
       }
-    __syncthreads();
+    if (many) {
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s_acc[pg][row4][dim0 + i] = acc[i];
-    if (dim0 == 0) {
-      s_m[pg][row4] = M;
-      s_l[pg][row4] = L;
-    }
-    __syncthreads();
-    if (pg == 0 && valid) {
+      for (int i = 0; i < 8; ++i) s_acc[pg][my_row][dim0 + i] = acc[i];
+      if (dim0 == 0) {
+        s_m[pg][my_row] = M;
+        s_l[pg][my_row] = L;
+      }
+      __syncthreads();
       M = -INFINITY;
       L = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-#pragma unroll
       for (int j = 0; j < kFoldParts; ++j)
-        fold(s_m[j][row4], s_l[j][row4], &s_acc[j][row4][dim0]);
-      store_row<D, OUT_F32>(p, f.first + rr / p.group,
-                            f.kvh * p.group + rr % p.group,
-                            dim0, acc, M == -INFINITY ? 0.f : M, L);
+        fold(s_m[j][my_row], s_l[j][my_row], &s_acc[j][my_row][dim0]);
     }
+    if (pg == 0 && valid)
+      store_row<D, OUT_F32>(p, f.first + rr / p.group,
+                            f.kvh * p.group + rr % p.group, dim0, acc,
+                            M == -INFINITY ? 0.f : M, L);
   }
 }
 
@@ -783,8 +861,13 @@ void cache_fold_kernel(CacheFwdParams p) {
 struct Shape {
   int nq;          // 16-row columns per tile
   bool split;
-  int grid, unit_log2, max_units;
+  int grid, unit_log2, max_units, seq_units;
 };
+
+// Units that a sequence counts beside its keys.  128 requests of 1 to 16384
+// tokens (half of them shorter than a unit), 8 KV heads: 82 us with 0, 58 with
+// 1, 50 with 2, 48 with 4; requests of one length take the same within 4 %.
+constexpr int kSeqUnits = 4;
 
 Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
                int64_t rows) {
@@ -795,15 +878,26 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   s.nq = each <= 16 ? 1 : each <= 32 ? 2 : 4;
   // Most sequences that rows which do not overlap make.
   const int64_t seqs = (rows * group / (16 * s.nq) + num_requests) * c.hkv;
-  const int slots = s.nq == 1 ? 1024 : s.nq == 2 ? 768 : 512;
+  const int per_simd = c.d == 64
+                           ? (s.nq == 1   ? kWavesPerSimd<64, 1>
+                              : s.nq == 2 ? kWavesPerSimd<64, 2>
+                                          : kWavesPerSimd<64, 4>)
+                           : (s.nq == 1   ? kWavesPerSimd<128, 1>
+                              : s.nq == 2 ? kWavesPerSimd<128, 2>
+                                          : kWavesPerSimd<128, 4>);
+  const int slots = 256 * per_simd;  // a wave on each SIMD per workgroup
   const int64_t keys = int64_t{c.max_pages} << c.page_log2;
   s.split = keys > kWaveKeys && seqs < 4 * slots;
   s.unit_log2 = 7;
   static_assert(kWaveKeys == 1 << 7, "least unit");
   // Units are counted in 32 bits.
   const int64_t most = int64_t{1} << 30;
-  while (s.split && seqs * ((keys >> s.unit_log2) + 1) >= most) ++s.unit_log2;
-  const int64_t units = s.split ? seqs * ((keys >> s.unit_log2) + 1) : seqs;
+  s.seq_units = s.split ? kSeqUnits : 0;
+  auto units_of = [&] {
+    return s.split ? seqs * ((keys >> s.unit_log2) + 1 + s.seq_units) : seqs;
+  };
+  while (s.split && units_of() >= most && s.unit_log2 < 30) ++s.unit_log2;
+  const int64_t units = units_of();
   s.max_units = static_cast<int>(units < most ? units : most - 1);
   const int64_t grid = s.split ? slots : seqs;
   s.grid = static_cast<int>(grid < 65536 ? grid : 65536);
@@ -830,7 +924,7 @@ hipError_t launch(const CacheFwdParams& p, const Shape& s, hipStream_t stream) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !s.split) return e;
   hipLaunchKernelGGL((cache_fold_kernel<D, NQ, OUT_F32>), grid,
-                     dim3(kFoldRows * kFoldParts * (D / 8)), 0, stream, p);
+                     dim3(kFoldThreads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -866,6 +960,7 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
   CacheFwdParams p = params;
   p.split = s.split;
   p.unit_log2 = s.unit_log2;
+  p.seq_units = s.seq_units;
   p.max_units = s.max_units;
   p.min_units = 1;
   p.fold = static_cast<CacheFold*>(ws);
