@@ -602,24 +602,37 @@ def mesh_attn_goo_plan(k_q, k_kv, t_ag_q, t_ag_kv, t_rs_q, t_c, gamma=1.05):
 # Paged key/value cache in 4 bits
 # ---------------------------------------------------------------------------
 
-def _one_device(stream, *tensors):
+def _device_index(stream, t, name):
     # Launches go to the current device (or the stream's): a tensor of another
     # one would be an address it may not know.
-    index = (_torch()._C._cuda_getDevice() if stream is None
-             else stream.device.index)
-    for t in tensors:
-        if t.get_device() != index:
-            raise ValueError(f"tensor on {t.device}, the call on cuda:{index}")
-
-
-def _heads(t, name, rows, heads, d, dtypes):
-    """Pointer and row stride of [rows, heads, d] whose heads are dense."""
     if not isinstance(t, _torch().Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a GPU, got {t.device}")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name} dtype {t.dtype} not in {dtypes}")
+    return (_torch_module._C._cuda_getDevice() if stream is None
+            else stream.device.index)
+
+
+def _arg(t, name, shape, dtype, dev):
+    """Pointer of a dense tensor of the call's device."""
+    if (isinstance(t, _torch_module.Tensor) and t.dtype is dtype
+            and t.get_device() == dev and t.shape == shape
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _dev(t, name, shape, (dtype,))
+    raise ValueError(f"{name} on {t.device}, the call on cuda:{dev}")
+
+
+def _heads(t, name, rows, heads, d, dtype, dev):
+    """Pointer and row stride of [rows, heads, d] whose heads are dense."""
+    if not isinstance(t, _torch_module.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.get_device() != dev:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be on a GPU, got {t.device}")
+        raise ValueError(f"{name} on {t.device}, the call on cuda:{dev}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} dtype {t.dtype} is not {dtype}")
     if t.shape != (rows, heads, d):
         raise ValueError(f"{name} shape {tuple(t.shape)} != "
                          f"{(rows, heads, d)}")
@@ -633,10 +646,11 @@ def _heads(t, name, rows, heads, d, dtypes):
     return t.data_ptr(), row
 
 
-def _cache_data(c, data):
-    shape = (c.num_pages, c.num_kv_heads,
-             c.page_size * (c.head_dim + c.head_dim // 16))
-    return _dev(data, "data", shape, (_torch().uint8,))
+def _cache_data(c, data, dev):
+    d = c.head_dim
+    return _arg(data, "data", (c.num_pages, c.num_kv_heads,
+                               c.page_size * (d + d // 16)),
+                _torch_module.uint8, dev)
 
 
 def mesh_attn_cache_bytes(cache):
@@ -656,25 +670,21 @@ def mesh_attn_cache_tables(cache, lens, new_lens, free_pages, free_range,
     """Block table, slots and positions of a step from the requests' lengths;
     all int32 but ``slots`` (int64).  Returns ``(block_table, lens_out, cu_new,
     slots, positions, free_range_out, refused)``."""
-    torch = _torch()
-    c = Cache.make(cache)
-    i32 = (torch.int32,)
+    dev, torch = _device_index(stream, lens, "lens"), _torch_module
+    c, i32 = Cache.make(cache), torch.int32
     b, rows, num_free = lens.numel(), slots.numel(), free_pages.numel()
-    a = [_dev(lens, "lens", (b,), i32),
-         _dev(new_lens, "new_lens", (b,), i32),
-         _dev(free_pages, "free_pages", (num_free,), i32), num_free,
-         _dev(free_range, "free_range", (2,), i32),
-         _dev(block_table, "block_table", (b, c.max_pages), i32),
-         _dev(lens_out, "lens_out", (b,), i32),
-         _dev(cu_new, "cu_new", (b + 1,), i32), rows,
-         _dev(slots, "slots", (rows,), (torch.int64,)),
-         _dev(positions, "positions", (rows,), i32),
-         _dev(free_range_out, "free_range_out", (2,), i32),
-         _dev(refused, "refused", (1,), i32)]
-    _one_device(stream, lens, new_lens, free_pages, free_range, block_table,
-                lens_out, cu_new, slots, positions, free_range_out, refused)
-    st = load_library().mesh_attn_cache_tables(ctypes.byref(c), b, *a,
-                                               _stream_ptr(stream))
+    st = load_library().mesh_attn_cache_tables(
+        c, b, _arg(lens, "lens", (b,), i32, dev),
+        _arg(new_lens, "new_lens", (b,), i32, dev),
+        _arg(free_pages, "free_pages", (num_free,), i32, dev), num_free,
+        _arg(free_range, "free_range", (2,), i32, dev),
+        _arg(block_table, "block_table", (b, c.max_pages), i32, dev),
+        _arg(lens_out, "lens_out", (b,), i32, dev),
+        _arg(cu_new, "cu_new", (b + 1,), i32, dev), rows,
+        _arg(slots, "slots", (rows,), torch.int64, dev),
+        _arg(positions, "positions", (rows,), i32, dev),
+        _arg(free_range_out, "free_range_out", (2,), i32, dev),
+        _arg(refused, "refused", (1,), i32, dev), _stream_ptr(stream))
     _check("mesh_attn_cache_tables", st)
     return (block_table, lens_out, cu_new, slots, positions, free_range_out,
             refused)
@@ -683,17 +693,15 @@ def mesh_attn_cache_tables(cache, lens, new_lens, free_pages, free_range,
 def mesh_attn_cache_append(cache, k, v, slots, data, stream=None):
     """Stores rows ``k, v [rows, Hkv, d]`` (bf16; row strides as they are) in 4
     bits at ``slots [rows]`` (int64; out of range: not stored)."""
-    torch = _torch()
-    c = Cache.make(cache)
-    rows = slots.numel()
-    bf = (torch.bfloat16,)
-    kp, ks = _heads(k, "k", rows, c.num_kv_heads, c.head_dim, bf)
-    vp, vs = _heads(v, "v", rows, c.num_kv_heads, c.head_dim, bf)
-    sp = _dev(slots, "slots", (rows,), (torch.int64,))
-    dp = _cache_data(c, data)
-    _one_device(stream, k, v, slots, data)
+    dev, torch = _device_index(stream, k, "k"), _torch_module
+    c, bf = Cache.make(cache), torch.bfloat16
+    rows, heads, d = slots.numel(), c.num_kv_heads, c.head_dim
+    kp, ks = _heads(k, "k", rows, heads, d, bf, dev)
+    vp, vs = _heads(v, "v", rows, heads, d, bf, dev)
     st = load_library().mesh_attn_cache_append(
-        ctypes.byref(c), rows, kp, ks, vp, vs, sp, dp, _stream_ptr(stream))
+        c, rows, kp, ks, vp, vs,
+        _arg(slots, "slots", (rows,), torch.int64, dev),
+        _cache_data(c, data, dev), _stream_ptr(stream))
     _check("mesh_attn_cache_append", st)
     return data
 
@@ -701,15 +709,14 @@ def mesh_attn_cache_append(cache, k, v, slots, data, stream=None):
 def mesh_attn_cache_read(cache, slots, data, k, v, stream=None):
     """The stored rows at ``slots`` as bf16 ``k, v [rows, Hkv, d]``, the KV
     buffer of the tile calls."""
-    torch = _torch()
-    c = Cache.make(cache)
+    dev, torch = _device_index(stream, slots, "slots"), _torch_module
+    c, bf = Cache.make(cache), torch.bfloat16
     rows = slots.numel()
-    shape, bf = (rows, c.num_kv_heads, c.head_dim), (torch.bfloat16,)
-    a = [_dev(slots, "slots", (rows,), (torch.int64,)), _cache_data(c, data),
-         _dev(k, "k", shape, bf), _dev(v, "v", shape, bf)]
-    _one_device(stream, slots, data, k, v)
-    st = load_library().mesh_attn_cache_read(ctypes.byref(c), rows, *a,
-                                             _stream_ptr(stream))
+    shape = (rows, c.num_kv_heads, c.head_dim)
+    st = load_library().mesh_attn_cache_read(
+        c, rows, _arg(slots, "slots", (rows,), torch.int64, dev),
+        _cache_data(c, data, dev), _arg(k, "k", shape, bf, dev),
+        _arg(v, "v", shape, bf, dev), _stream_ptr(stream))
     _check("mesh_attn_cache_read", st)
     return k, v
 
@@ -726,32 +733,34 @@ def mesh_attn_cache_fwd(cache, softmax_scale, q, positions, cu_new, lens,
     is) over the stored keys of their requests.  ``o`` bf16 (final) or float32
     (partial) ``[rows, Hq, d]``, ``lse [Hq, rows]``; rows of no request stay as
     they were."""
-    torch = _torch()
-    c = Cache.make(cache)
+    dev, torch = _device_index(stream, q, "q"), _torch_module
+    c, i32 = Cache.make(cache), torch.int32
     if q.dim() != 3:
         raise ValueError("q must be [rows, heads, head_dim]")
-    rows, hq, _ = q.shape
+    rows, hq, d = q.shape[0], q.shape[1], c.head_dim
     b = lens.numel()
-    i32 = (torch.int32,)
-    qp, qs = _heads(q, "q", rows, hq, c.head_dim, (torch.bfloat16,))
-    a = [_dev(positions, "positions", (rows,), i32),
-         _dev(cu_new, "cu_new", (b + 1,), i32), _dev(lens, "lens", (b,), i32),
-         _dev(block_table, "block_table", (b, c.max_pages), i32),
-         _cache_data(c, data),
-         _dev(o, "o", (rows, hq, c.head_dim), (torch.bfloat16, torch.float32)),
-         _dtype_code(o), _dev(lse, "lse", (hq, rows), (torch.float32,))]
-    _one_device(stream, q, positions, cu_new, lens, block_table, data, o, lse)
+    qp, qs = _heads(q, "q", rows, hq, d, torch.bfloat16, dev)
+    f32 = o.dtype is torch.float32
     if ws is None:
         n = mesh_attn_cache_fwd_workspace_size(c, hq, b, rows)
         ws = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
         if stream is not None:
             ws.record_stream(stream)
-    elif not ws.is_cuda or not ws.is_contiguous():
-        raise ValueError("workspace must be a contiguous GPU tensor")
-    _one_device(stream, ws)
+    elif ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor of the call's "
+                         "GPU")
     st = load_library().mesh_attn_cache_fwd(
-        ctypes.byref(c), hq, float(softmax_scale), b, rows, qp, qs, *a,
-        ws.data_ptr(), ws.numel() * ws.element_size(), _stream_ptr(stream))
+        c, hq, softmax_scale, b, rows, qp, qs,
+        _arg(positions, "positions", (rows,), i32, dev),
+        _arg(cu_new, "cu_new", (b + 1,), i32, dev),
+        _arg(lens, "lens", (b,), i32, dev),
+        _arg(block_table, "block_table", (b, c.max_pages), i32, dev),
+        _cache_data(c, data, dev),
+        _arg(o, "o", (rows, hq, d), torch.float32 if f32 else torch.bfloat16,
+             dev),
+        MA_FP32 if f32 else MA_BF16,
+        _arg(lse, "lse", (hq, rows), torch.float32, dev), ws.data_ptr(),
+        ws.nbytes, _stream_ptr(stream))
     _check("mesh_attn_cache_fwd", st)
     return o, lse
 
@@ -766,31 +775,30 @@ def mesh_attn_rope(rope, positions, q, q_out, k=None, k_out=None, inverse=0,
     ``positions [num_axes, rows]`` (int32; ``[rows]`` does for one axis) into ``q_out``, ``k_out`` (the same
     tensors for in place); bf16 or float32, row strides as they are.
     ``inverse=1`` turns back: the gradient."""
-    torch = _torch()
     r = Rope.make(rope)
-    if q.dim() != 3 or (k is not None and k.dim() != 3):
-        raise ValueError("q and k must be [rows, heads, head_dim]")
     if (k is None) != (k_out is None):
         raise ValueError("k and k_out go together")
-    rows, hq, _ = q.shape
-    d, dtypes = r.head_dim, (q.dtype,)
-    if q.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"q dtype {q.dtype} is not bfloat16 or float32")
+    dev, torch = _device_index(stream, q, "q"), _torch_module
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise ValueError("q and k must be [rows, heads, head_dim]")
+    rows, hq, d, dt = q.shape[0], q.shape[1], r.head_dim, q.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise ValueError(f"q dtype {dt} is not bfloat16 or float32")
     shape = (r.num_axes, rows)
     if r.num_axes == 1 and positions.dim() == 1:
         shape = (rows,)
-    pp = _dev(positions, "positions", shape, (torch.int32,))
-    qp, qs = _heads(q, "q", rows, hq, d, dtypes)
-    qo, qos = _heads(q_out, "q_out", rows, hq, d, dtypes)
-    _one_device(stream, positions, q, q_out)
-    hk = kp = ks = ko = kos = 0
+    pp = _arg(positions, "positions", shape, torch.int32, dev)
+    qp, qs = _heads(q, "q", rows, hq, d, dt, dev)
+    qo, qos = _heads(q_out, "q_out", rows, hq, d, dt, dev)
+    hk = ks = kos = 0
+    kp = ko = None
     if k is not None:
         hk = k.shape[1]
-        kp, ks = _heads(k, "k", rows, hk, d, dtypes)
-        ko, kos = _heads(k_out, "k_out", rows, hk, d, dtypes)
-        _one_device(stream, k, k_out)
+        kp, ks = _heads(k, "k", rows, hk, d, dt, dev)
+        ko, kos = _heads(k_out, "k_out", rows, hk, d, dt, dev)
     st = load_library().mesh_attn_rope(
-        ctypes.byref(r), rows, pp, hq, qp, qs, qo, qos, hk, kp or None, ks,
-        ko or None, kos, _dtype_code(q), int(inverse), _stream_ptr(stream))
+        r, rows, pp, hq, qp, qs, qo, qos, hk, kp, ks, ko, kos,
+        MA_BF16 if dt is torch.bfloat16 else MA_FP32, inverse,
+        _stream_ptr(stream))
     _check("mesh_attn_rope", st)
     return q_out, k_out

@@ -332,16 +332,15 @@ ma_status_t mesh_attn_rope(const ma_rope_t* rope, int64_t rows,
     p.t.axis[i] = 0;
   }
   // Turns per position modulo 1, in 2^-64: the extended type's 64-bit fraction
-  // holds the quotient of a double to half a unit of that for frequencies up to
-  // 2 pi, and the kernel's product with the position wraps as turns do.
-  const long double kTwoPi = 6.283185307179586476925286766559L;
+  // holds the product to about a unit of that for frequencies up to 2 pi, and the kernel's product with the position wraps as turns do.
+  const long double kPerRadian = 0.159154943091895335768883763372514362L;
   for (int i = 0; i < rot / 2; ++i) {
     const double f = rope->inv_freq[i];
     if (!(std::fabs(f) < 2147483648.0))
       return fail(MA_ERR_INVALID_ARG, "inv_freq[%d] = %g", i, f);
-    const long double t = static_cast<long double>(std::fabs(f)) / kTwoPi;
-    const long double frac = t - std::floor(t);
-    const long double scaled = std::floor(frac * 0x1p64L + 0.5L);
+    const long double t = static_cast<long double>(std::fabs(f)) * kPerRadian;
+    const long double frac = t - static_cast<uint32_t>(t);
+    const long double scaled = frac * 0x1p64L + 0.5L;
     const uint64_t u =
         scaled >= 0x1p64L ? 0 : static_cast<uint64_t>(scaled);
     p.t.turn[i] = f < 0 ? uint64_t{0} - u : u;

@@ -7,9 +7,9 @@
 // fraction's top two bits after rounding are the quadrant, the rest (at most an
 // eighth of a turn) goes to sincospi in float32.
 //
-// Streaming: every element is read and written once, the angles are made once
-// per (row, pair) and used for all heads of Q and K.  A thread owns one
-// 16-byte unit's worth of pairs of a row and walks over the heads.
+// Streaming: every element is read and written once.  A thread owns one 16-byte
+// unit's worth of pairs of a row, makes their angles once and walks over heads of
+// Q and K, four at a time with all their loads in flight.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -61,86 +61,120 @@ struct Unit<false> {
   }
 };
 
+// cos and sin of a turn by per * pos (2^-64 turns, modulo 1).
 __device__ __forceinline__ void turn_of(uint64_t per, int32_t pos, float* c,
                                         float* s) {
   const uint64_t frac = per * static_cast<uint64_t>(int64_t{pos});
-  // Quadrant, and the signed rest in 2^-64 turns.
+  // Quadrant, and the signed rest in 2^-64 turns: at most an eighth.
   const uint64_t near = frac + (uint64_t{1} << 61);
   const uint32_t quad = static_cast<uint32_t>(near >> 62);
   const int64_t rest =
       static_cast<int64_t>(frac - (static_cast<uint64_t>(quad) << 62));
-  // Half turns: rest * 2^-63, |.| <= 1/4.
-  const float x = static_cast<float>(static_cast<int32_t>(rest >> 30)) *
-                  0x1p-33f;
-  float sn, cs;
-  sincospif(x, &sn, &cs);
+  // Radians, |t| <= pi / 4: 2 pi 2^-34 a unit of the rest's upper bits.
+  const float t = static_cast<float>(static_cast<int32_t>(rest >> 30)) *
+                  static_cast<float>(6.283185307179586 * 0x1p-34);
+  // Taylor: the first terms left out are below 2^-29 of sin and 2^-33 of cos.
+  const float z = t * t;
+  float sn = fmaf(z, 1.f / 362880, -1.f / 5040);
+  sn = fmaf(sn, z, 1.f / 120);
+  sn = fmaf(sn, z, -1.f / 6);
+  sn = fmaf(sn * z, t, t);
+  float cs = fmaf(z, -1.f / 3628800, 1.f / 40320);
+  cs = fmaf(cs, z, -1.f / 720);
+  cs = fmaf(cs, z, 1.f / 24);
+  cs = fmaf(cs, z, -0.5f);
+  cs = fmaf(cs, z, 1.f);
   const float a = (quad & 1) ? sn : cs, b = (quad & 1) ? cs : sn;
   *c = (quad == 1 || quad == 2) ? -a : a;
   *s = (quad & 2) ? -b : b;
 }
 
-// The units of a head are rotated ones (two per thread and step: the halves'
-// units i and i + rot/2, or, interleaved, two neighbours), then copied ones.
+// Heads loaded together.
+constexpr int kBatch = 4;
+
+// The units of a head are rotated ones (two per thread and head: units i and
+// i + rot/2 of the halves, or, interleaved, two neighbours), then copied ones.
+// blockIdx.y: p.batches * kBatch heads of Q's, then K's.
 template <bool F32, bool INTER>
 __global__ __launch_bounds__(NT) void rope_kernel(RopeParams p) {
   constexpr int N = Unit<F32>::N;
   const int half = p.rot / 2;
-  const int rot_units = half / N, units = rot_units + (p.d - p.rot) / N;
+  const uint32_t rot_units = half / N,
+                 units = rot_units + (p.d - p.rot) / N;
   const int64_t total = p.rows * units;
   const int64_t idx = int64_t{blockIdx.x} * NT + threadIdx.x;
   if (idx >= total) return;
-  const int64_t row = idx / units;
-  const int u = static_cast<int>(idx - row * units);
-  if (u >= rot_units) {
-    const int at = p.rot + (u - rot_units) * N;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (p.x[t] == p.y[t]) continue;
-      for (int h = 0; h < p.heads[t]; ++h) {
-        float x[N];
-        Unit<F32>::load(p.x[t], row * p.x_stride[t] + h * p.d + at, x);
-        Unit<F32>::store(p.y[t], row * p.y_stride[t] + h * p.d + at, x);
-      }
-    }
-    return;
-  }
+  const int64_t row = total < (int64_t{1} << 32)
+                          ? int64_t{uint32_t(idx) / units}
+                          : idx / units;
+  const uint32_t u = static_cast<uint32_t>(idx - row * units);
+  const bool turns = u < rot_units;
   float c[N], s[N];
+  int at0, at1;
+  if (turns) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int pair = u * N + j;
-    turn_of(p.t.turn[pair], p.positions[p.t.axis[pair] * p.rows + row], &c[j],
-            &s[j]);
-    if (p.inverse) s[j] = -s[j];
+    for (int j = 0; j < N; ++j) {
+      const int pair = u * N + j;
+      turn_of(p.t.turn[pair], p.positions[p.t.axis[pair] * p.rows + row], &c[j],
+              &s[j]);
+      if (p.inverse) s[j] = -s[j];
+    }
+    at0 = INTER ? 2 * u * N : u * N;
+    at1 = INTER ? at0 + N : at0 + half;
+  } else {
+    at0 = at1 = p.rot + (u - rot_units) * N;
   }
-  const int at0 = INTER ? 2 * u * N : u * N;
-  const int at1 = INTER ? at0 + N : at0 + half;
+  const int heads = p.heads[0] + p.heads[1];
+  int h0 = blockIdx.y * (p.batches * kBatch);
+  for (int b = 0; b < p.batches && h0 < heads; ++b, h0 += kBatch) {
+    float x[kBatch][2 * N];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    for (int h = 0; h < p.heads[t]; ++h) {
-      float x[2 * N], y[2 * N];
-      const int64_t in = row * p.x_stride[t] + h * p.d;
-      const int64_t out = row * p.y_stride[t] + h * p.d;
-      Unit<F32>::load(p.x[t], in + at0, x);
-      Unit<F32>::load(p.x[t], in + at1, x + N);
+    for (int i = 0; i < kBatch; ++i) {
+      const int h = min(h0 + i, heads - 1), t = h < p.heads[0] ? 0 : 1;
+      const int64_t in = row * p.x_stride[t] +
+                         int64_t{t ? h - p.heads[0] : h} * p.d;
+      Unit<F32>::load(p.x[t], in + at0, x[i]);
+      if (turns) Unit<F32>::load(p.x[t], in + at1, x[i] + N);
+    }
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int a = INTER ? 2 * j : j, b = INTER ? 2 * j + 1 : j + N;
-        y[a] = x[a] * c[j] - x[b] * s[j];
-        y[b] = x[b] * c[j] + x[a] * s[j];
+    for (int i = 0; i < kBatch; ++i) {
+      const int h = h0 + i, t = h < p.heads[0] ? 0 : 1;
+      if (h >= heads) break;
+      const int64_t out = row * p.y_stride[t] +
+                          int64_t{t ? h - p.heads[0] : h} * p.d;
+      if (turns) {
+        float y[2 * N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const int a = INTER ? 2 * j : j, e = INTER ? 2 * j + 1 : j + N;
+          y[a] = x[i][a] * c[j] - x[i][e] * s[j];
+          y[e] = x[i][e] * c[j] + x[i][a] * s[j];
+        }
+        Unit<F32>::store(p.y[t], out + at0, y);
+        Unit<F32>::store(p.y[t], out + at1, y + N);
+      } else if (p.x[t] != p.y[t]) {
+        Unit<F32>::store(p.y[t], out + at0, x[i]);
       }
-      Unit<F32>::store(p.y[t], out + at0, y);
-      Unit<F32>::store(p.y[t], out + at1, y + N);
     }
   }
 }
 
 }  // namespace
 
-hipError_t launch_rope(const RopeParams& p, bool f32, hipStream_t stream) {
+hipError_t launch_rope(const RopeParams& params, bool f32,
+                       hipStream_t stream) {
+  RopeParams p = params;
   const int n = f32 ? 4 : 8;
   const int units = p.rot / 2 / n + (p.d - p.rot) / n;
   const int64_t grid = (p.rows * units + NT - 1) / NT;
-  const dim3 g(static_cast<unsigned>(grid));
+  // Angles are made once for all the heads of a thread, of which more threads
+  // have fewer.
+  const int batches = (p.heads[0] + p.heads[1] + kBatch - 1) / kBatch;
+  p.batches = 1;
+  while (p.batches < 4 && grid * (batches / (2 * p.batches)) >= 2048)
+    p.batches *= 2;
+  const dim3 g(static_cast<unsigned>(grid),
+               (batches + p.batches - 1) / p.batches);
   if (f32) {
     if (p.interleaved)
       hipLaunchKernelGGL((rope_kernel<true, true>), g, dim3(NT), 0, stream, p);

@@ -256,8 +256,10 @@ def test_binding_refuses_cpu_tensors_and_bad_mappings():
         ma.mesh_attn_cache_fwd(c, 0.1, x, slots, slots, slots, slots, data, x,
                                x)
     rope = dict(head_dim=64, rotary_dim=32, inv_freq=[1.0] * 16)
-    with pytest.raises(ValueError, match="positions must be on a GPU"):
+    with pytest.raises(ValueError, match="q must be on a GPU"):
         ma.mesh_attn_rope(rope, slots, x, x)
+    with pytest.raises(TypeError, match="lens must be a torch.Tensor"):
+        ma.mesh_attn_cache_tables(c, [3], *[slots] * 10)
     with pytest.raises(ValueError, match="rotary_dim / 2"):
         ma.Rope.make(dict(rope, inv_freq=[1.0]))
     with pytest.raises(ValueError, match="rotary_dim / 2"):
