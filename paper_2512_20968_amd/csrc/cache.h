@@ -127,7 +127,7 @@ struct RopeParams {
   int64_t rows;
   int32_t heads[2];
   int32_t d, rot, interleaved, inverse;
-  int32_t batches;  // of heads that a thread walks over
+  int32_t group_rows;  // rows of a workgroup
 };
 static_assert(sizeof(RopeParams) <= 4096, "kernel arguments");
 hipError_t launch_rope(const RopeParams& p, bool f32, hipStream_t stream);

@@ -7,22 +7,25 @@
 // fraction's top two bits after rounding are the quadrant, the rest (at most an
 // eighth of a turn) goes to sincospi in float32.
 //
-// Streaming: every element is read and written once.  A thread owns one 16-byte
-// unit's worth of pairs of a row, makes their angles once and walks over heads of
-// Q and K, four at a time with all their loads in flight.
+// Streaming: every element is read and written once.  A workgroup takes a few
+// rows, makes each of their angles once, in LDS, and then walks over the 16-byte
+// units of their heads in the order in which they lie in memory, two units
+// per thread in flight.  16384 rows of 40 bf16 heads of 128 (336 MB): 64.9 us,
+// 5.2 TB/s, as a large copy; with the angles made by every thread that walks
+// over heads it took 72 to 79 us.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include "cache.h"
+#include "tile_common.h"
 
 namespace mesh_attn {
 namespace {
 
-constexpr int NT = 256;
+using namespace dev;
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr int NT = 256;
 
 // 16 bytes of a head as float32.
 template <bool F32>
@@ -40,7 +43,8 @@ struct Unit<true> {
     f32x4 v;
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = x[j];
-    *reinterpret_cast<f32x4*>(static_cast<float*>(base) + i) = v;
+    __builtin_nontemporal_store(
+        v, reinterpret_cast<f32x4*>(static_cast<float*>(base) + i));
   }
 };
 template <>
@@ -57,7 +61,8 @@ struct Unit<false> {
     bf16x8 v;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = static_cast<__bf16>(x[j]);
-    *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(base) + i) = v;
+    __builtin_nontemporal_store(
+        v, reinterpret_cast<bf16x8*>(static_cast<__bf16*>(base) + i));
   }
 };
 
@@ -89,71 +94,93 @@ __device__ __forceinline__ void turn_of(uint64_t per, int32_t pos, float* c,
   *s = (quad & 2) ? -b : b;
 }
 
-// Heads loaded together.
-constexpr int kBatch = 4;
+// Units of a thread that are loaded together.
+constexpr int kBatch = 2;
+
+// Angles of a workgroup's rows: rows_per_group * pairs of them at most (one per
+// thread, or one row's).
+constexpr int kAngles = NT > kRopeMaxPairs ? NT : kRopeMaxPairs;
 
 // The units of a head are rotated ones (two per thread and head: units i and
 // i + rot/2 of the halves, or, interleaved, two neighbours), then copied ones.
-// blockIdx.y: p.batches * kBatch heads of Q's, then K's.
 template <bool F32, bool INTER>
 __global__ __launch_bounds__(NT) void rope_kernel(RopeParams p) {
   constexpr int N = Unit<F32>::N;
-  const int half = p.rot / 2;
+  __shared__ alignas(16) float s_cos[kAngles], s_sin[kAngles];
+  const uint32_t half = p.rot / 2;
   const uint32_t rot_units = half / N,
                  units = rot_units + (p.d - p.rot) / N;
-  const int64_t total = p.rows * units;
-  const int64_t idx = int64_t{blockIdx.x} * NT + threadIdx.x;
-  if (idx >= total) return;
-  const int64_t row = total < (int64_t{1} << 32)
-                          ? int64_t{uint32_t(idx) / units}
-                          : idx / units;
-  const uint32_t u = static_cast<uint32_t>(idx - row * units);
-  const bool turns = u < rot_units;
-  float c[N], s[N];
-  int at0, at1;
-  if (turns) {
+  const uint32_t heads = p.heads[0] + p.heads[1], of_row = heads * units;
+  const int64_t row0 = int64_t{blockIdx.x} * p.group_rows;
+  const uint32_t rows = static_cast<uint32_t>(
+      min(int64_t{p.group_rows}, p.rows - row0));
+  const uint32_t items = rows * of_row;
+
+  struct Item {
+    int64_t in, out;
+    uint32_t at0, at1, angle;
+    int t;
+    bool turns;
+  };
+  auto locate = [&](uint32_t i) {
+    Item it;
+    const uint32_t r = i / of_row, rest = i - r * of_row;
+    const uint32_t h = rest / units, u = rest - h * units;
+    it.t = h < uint32_t(p.heads[0]) ? 0 : 1;
+    const int64_t row = row0 + r;
+    const int64_t head = int64_t{it.t ? h - p.heads[0] : h} * p.d;
+    it.in = row * p.x_stride[it.t] + head;
+    it.out = row * p.y_stride[it.t] + head;
+    it.turns = u < rot_units;
+    it.at0 = !it.turns ? p.rot + (u - rot_units) * N
+             : INTER   ? 2 * u * N
+                       : u * N;
+    it.at1 = INTER ? it.at0 + N : it.at0 + half;
+    it.angle = r * half + u * N;
+    return it;
+  };
+  Item it[kBatch];
+  float x[kBatch][2 * N];
+  auto load = [&](uint32_t i0) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int pair = u * N + j;
-      turn_of(p.t.turn[pair], p.positions[p.t.axis[pair] * p.rows + row], &c[j],
-              &s[j]);
-      if (p.inverse) s[j] = -s[j];
+    for (int i = 0; i < kBatch; ++i) {
+      if (i0 + i * NT >= items) break;
+      it[i] = locate(i0 + i * NT);
+      Unit<F32>::load(p.x[it[i].t], it[i].in + it[i].at0, x[i]);
+      if (it[i].turns)
+        Unit<F32>::load(p.x[it[i].t], it[i].in + it[i].at1, x[i] + N);
     }
-    at0 = INTER ? 2 * u * N : u * N;
-    at1 = INTER ? at0 + N : at0 + half;
-  } else {
-    at0 = at1 = p.rot + (u - rot_units) * N;
+  };
+  load(threadIdx.x);  // in flight while the angles are made
+  for (uint32_t i = threadIdx.x; i < rows * half; i += NT) {
+    const uint32_t r = i / half, pair = i - r * half;
+    float c, s;
+    turn_of(p.t.turn[pair], p.positions[p.t.axis[pair] * p.rows + row0 + r], &c,
+            &s);
+    s_cos[i] = c;
+    s_sin[i] = p.inverse ? -s : s;
   }
-  const int heads = p.heads[0] + p.heads[1];
-  int h0 = blockIdx.y * (p.batches * kBatch);
-  for (int b = 0; b < p.batches && h0 < heads; ++b, h0 += kBatch) {
-    float x[kBatch][2 * N];
+  lds_barrier();
+  for (uint32_t i0 = threadIdx.x; i0 < items; i0 += kBatch * NT) {
+    if (i0 != threadIdx.x) load(i0);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int h = min(h0 + i, heads - 1), t = h < p.heads[0] ? 0 : 1;
-      const int64_t in = row * p.x_stride[t] +
-                         int64_t{t ? h - p.heads[0] : h} * p.d;
-      Unit<F32>::load(p.x[t], in + at0, x[i]);
-      if (turns) Unit<F32>::load(p.x[t], in + at1, x[i] + N);
-    }
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int h = h0 + i, t = h < p.heads[0] ? 0 : 1;
-      if (h >= heads) break;
-      const int64_t out = row * p.y_stride[t] +
-                          int64_t{t ? h - p.heads[0] : h} * p.d;
-      if (turns) {
-        float y[2 * N];
+      if (i0 + i * NT >= items) break;
+      const Item& m = it[i];
+      void* y = p.y[m.t];
+      if (m.turns) {
+        float z[2 * N];
 #pragma unroll
         for (int j = 0; j < N; ++j) {
+          const float c = s_cos[m.angle + j], s = s_sin[m.angle + j];
           const int a = INTER ? 2 * j : j, e = INTER ? 2 * j + 1 : j + N;
-          y[a] = x[i][a] * c[j] - x[i][e] * s[j];
-          y[e] = x[i][e] * c[j] + x[i][a] * s[j];
+          z[a] = x[i][a] * c - x[i][e] * s;
+          z[e] = x[i][e] * c + x[i][a] * s;
         }
-        Unit<F32>::store(p.y[t], out + at0, y);
-        Unit<F32>::store(p.y[t], out + at1, y + N);
-      } else if (p.x[t] != p.y[t]) {
-        Unit<F32>::store(p.y[t], out + at0, x[i]);
+        Unit<F32>::store(y, m.out + m.at0, z);
+        Unit<F32>::store(y, m.out + m.at1, z + N);
+      } else if (p.x[m.t] != y) {
+        Unit<F32>::store(y, m.out + m.at0, x[i]);
       }
     }
   }
@@ -161,20 +188,21 @@ __global__ __launch_bounds__(NT) void rope_kernel(RopeParams p) {
 
 }  // namespace
 
+// Workgroups before one takes more rows.  16384 float32 rows of 20 heads, 32
+// pairs: 63.7 us with 4 rows each (4096 workgroups), 69.3 with 8; 3001 rows of 16
+// heads 6.8 us with one each, 10.9 with 16.
+constexpr int kGroups = 4096;
+
 hipError_t launch_rope(const RopeParams& params, bool f32,
                        hipStream_t stream) {
   RopeParams p = params;
-  const int n = f32 ? 4 : 8;
-  const int units = p.rot / 2 / n + (p.d - p.rot) / n;
-  const int64_t grid = (p.rows * units + NT - 1) / NT;
-  // Angles are made once for all the heads of a thread, of which more threads
-  // have fewer.
-  const int batches = (p.heads[0] + p.heads[1] + kBatch - 1) / kBatch;
-  p.batches = 1;
-  while (p.batches < 4 && grid * (batches / (2 * p.batches)) >= 2048)
-    p.batches *= 2;
-  const dim3 g(static_cast<unsigned>(grid),
-               (batches + p.batches - 1) / p.batches);
+  // Up to an angle per thread, while there are enough workgroups.
+  p.group_rows = 1;
+  while (2 * p.group_rows * (p.rot / 2) <= NT &&
+         p.rows >= int64_t{2 * p.group_rows} * kGroups)
+    p.group_rows *= 2;
+  const dim3 g(static_cast<unsigned>((p.rows + p.group_rows - 1) /
+                                     p.group_rows));
   if (f32) {
     if (p.interleaved)
       hipLaunchKernelGGL((rope_kernel<true, true>), g, dim3(NT), 0, stream, p);
