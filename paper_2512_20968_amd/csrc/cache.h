@@ -100,7 +100,7 @@ struct CacheFwdParams {
   int32_t split;      // whether sequences are cut
   int32_t unit_log2;  // keys of a unit
   int32_t seq_units;  // units that a sequence costs beside its keys
-  int32_t min_units, max_units;  // least of a run; most of a launch
+  int32_t max_units;  // most of a launch
   CacheFold* fold;           // [workgroup]
   float* part_o;             // [2 * workgroups][rows of a tile][d]
   float* part_ml;            // .. [2]: reference (log2 units) and sum

@@ -578,14 +578,14 @@ void cache_fwd_kernel(CacheFwdParams p) {
   // tiles of a head, and the runs with work spread over all of them.
   int run = blockIdx.x, per = 1, at = run, stop = total;
   if (p.split) {
-    per = max((total + int(gridDim.x) - 1) / int(gridDim.x), p.min_units);
+    per = max((total + int(gridDim.x) - 1) / int(gridDim.x), 1);
     const int active = (total + per - 1) / per;
     const int each = (active + 7) / 8;  // of an XCD
     const int x = blockIdx.x % 8, y = blockIdx.x / 8;
     // The others take the runs behind the active ones, without work.
     run = y < each ? x * each + y
                    : 8 * each + x * (int(gridDim.x / 8) - each) + y - each;
-    // Below 2^31: per * gridDim < total + gridDim * min_units.
+    // Below 2^31: per * gridDim is at most total + gridDim.
     at = per * run;
     stop = min(at + per, total);
     if (tid == 0) p.fold[run].parts = 0;
@@ -887,7 +887,13 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
                                           : kWavesPerSimd<128, 4>);
   const int slots = 256 * per_simd;  // a wave on each SIMD per workgroup
   const int64_t keys = int64_t{c.max_pages} << c.page_log2;
-  s.split = keys > kWaveKeys && seqs < 4 * slots;
+  // Short tables (the lengths may be shorter still) are not worth a second
+  // launch.  Microseconds cut / whole, one row of 4 heads per KV head, 8 KV heads:
+  //   1 request of 256 tokens  9.1/6.7   64 of  512   18.3/12.1
+  //   1 of 1024               10.0/11.6  64 of 1024   22.0/17.3
+  //   1 of 2048               10.4/16.4  32 of 1..1024 13.5/11.4
+  const bool brief = keys <= 512 || (keys <= 1024 && seqs >= 256);
+  s.split = !brief && seqs < 4 * slots;
   s.unit_log2 = 7;
   static_assert(kWaveKeys == 1 << 7, "least unit");
   // Units are counted in 32 bits.
@@ -962,7 +968,6 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
   p.unit_log2 = s.unit_log2;
   p.seq_units = s.seq_units;
   p.max_units = s.max_units;
-  p.min_units = 1;
   p.fold = static_cast<CacheFold*>(ws);
   p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + fold_bytes(s));
   p.part_ml = p.part_o + part_rows(s) * p.c.d;
