@@ -488,7 +488,8 @@ ma_status_t mesh_attn_cache_read(const ma_cache_t* cache, int64_t rows,
                                  void* k, void* v, hipStream_t stream);
 
 /* Device workspace bytes of mesh_attn_cache_fwd (0 if it needs none, or for
- * invalid arguments); at most 68 MB.  Never less for more rows or requests. */
+ * invalid arguments); at most 35 MB, the same for all numbers of rows and
+ * requests. */
 size_t mesh_attn_cache_fwd_workspace_size(const ma_cache_t* cache,
                                           int32_t num_q_heads,
                                           int32_t num_requests, int64_t rows);

@@ -239,7 +239,7 @@ size_t mesh_attn_cache_fwd_workspace_size(const ma_cache_t* cache,
       check_requests(num_requests) != MA_OK || check_rows(rows) != MA_OK)
     return 0;
   ok();
-  return cache_fwd_workspace(c, num_q_heads, num_requests, rows);
+  return cache_fwd_workspace(c, num_requests, rows);
 }
 
 ma_status_t mesh_attn_cache_fwd(
@@ -272,7 +272,7 @@ ma_status_t mesh_attn_cache_fwd(
                       {"o", o, 16},
                       {"lse", lse, 4}};
   MA_TRY(check_args(args, 8));
-  const size_t need = cache_fwd_workspace(p.c, num_q_heads, num_requests, rows);
+  const size_t need = cache_fwd_workspace(p.c, num_requests, rows);
   if (need > 0) {
     if (ws_bytes < need)
       return fail(MA_ERR_WORKSPACE_TOO_SMALL,

@@ -108,8 +108,8 @@ struct CacheFwdParams {
 
 hipError_t launch_cache_fwd(const CacheFwdParams& p, bool out_f32, void* ws,
                             hipStream_t stream);
-size_t cache_fwd_workspace(const CacheDims& c, int32_t hq,
-                           int32_t num_requests, int64_t rows);
+size_t cache_fwd_workspace(const CacheDims& c, int32_t num_requests,
+                           int64_t rows);
 
 // One pair's turn per position, as a 64-bit fraction of a full turn, and its
 // axis.

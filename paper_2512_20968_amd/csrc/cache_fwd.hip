@@ -857,6 +857,18 @@ void cache_fold_kernel(CacheFwdParams p) {
   }
 }
 
+// Workgroups that fit the card at once: each has a wave on every SIMD of one of
+// 256 compute units.
+int resident_groups(int head_dim, int nq) {
+  if (head_dim == 64)
+    return 256 * (nq == 1   ? kWavesPerSimd<64, 1>
+                  : nq == 2 ? kWavesPerSimd<64, 2>
+                            : kWavesPerSimd<64, 4>);
+  return 256 * (nq == 1   ? kWavesPerSimd<128, 1>
+                : nq == 2 ? kWavesPerSimd<128, 2>
+                          : kWavesPerSimd<128, 4>);
+}
+
 // How a call is launched, from its sizes alone.
 struct Shape {
   int nq;          // 16-row columns per tile
@@ -865,9 +877,16 @@ struct Shape {
 };
 
 // Units that a sequence counts beside its keys.  128 requests of 1 to 16384
-// tokens (half of them shorter than a unit), 8 KV heads: 82 us with 0, 58 with
-// 1, 50 with 2, 48 with 4; requests of one length take the same within 4 %.
-constexpr int kSeqUnits = 4;
+// tokens (half of them shorter than a unit), 8 KV heads, keys in the last-level
+// cache / not: 82 us with 0, 50/58 with 2, 48/61 with 4, -/71 with 12; requests
+// of one length take the same within 4 %.
+constexpr int kSeqUnits = 2;
+
+// Most stored keys of a request, and how many of them are always one launch's.
+int64_t keys_of(const CacheDims& c) {
+  return int64_t{c.max_pages} << c.page_log2;
+}
+constexpr int64_t kBriefKeys = 512;
 
 Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
                int64_t rows) {
@@ -878,21 +897,14 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   s.nq = each <= 16 ? 1 : each <= 32 ? 2 : 4;
   // Most sequences that rows which do not overlap make.
   const int64_t seqs = (rows * group / (16 * s.nq) + num_requests) * c.hkv;
-  const int per_simd = c.d == 64
-                           ? (s.nq == 1   ? kWavesPerSimd<64, 1>
-                              : s.nq == 2 ? kWavesPerSimd<64, 2>
-                                          : kWavesPerSimd<64, 4>)
-                           : (s.nq == 1   ? kWavesPerSimd<128, 1>
-                              : s.nq == 2 ? kWavesPerSimd<128, 2>
-                                          : kWavesPerSimd<128, 4>);
-  const int slots = 256 * per_simd;  // a wave on each SIMD per workgroup
-  const int64_t keys = int64_t{c.max_pages} << c.page_log2;
+  const int slots = resident_groups(c.d, s.nq);
+  const int64_t keys = keys_of(c);
   // Short tables (the lengths may be shorter still) are not worth a second
   // launch.  Microseconds cut / whole, one row of 4 heads per KV head, 8 KV heads:
   //   1 request of 256 tokens  9.1/6.7   64 of  512   18.3/12.1
   //   1 of 1024               10.0/11.6  64 of 1024   22.0/17.3
   //   1 of 2048               10.4/16.4  32 of 1..1024 13.5/11.4
-  const bool brief = keys <= 512 || (keys <= 1024 && seqs >= 256);
+  const bool brief = keys <= kBriefKeys || (keys <= 1024 && seqs >= 256);
   s.split = !brief && seqs < 4 * slots;
   s.unit_log2 = 7;
   static_assert(kWaveKeys == 1 << 7, "least unit");
@@ -910,10 +922,10 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   return s;
 }
 
-// Workspace of a split launch: CacheFold per workgroup, then the partial
-// results.
-size_t fold_bytes(const Shape& s) { return sizeof(CacheFold) * s.grid; }
-size_t part_rows(const Shape& s) { return size_t{32} * s.nq * s.grid; }
+// Workspace of a split launch of `groups` workgroups: CacheFold of each, then the
+// partial results: O, reference and sum of two tiles each.
+size_t fold_bytes(int groups) { return sizeof(CacheFold) * groups; }
+size_t part_rows(int groups, int nq) { return size_t{32} * nq * groups; }
 
 template <int D, int NQ, bool OUT_F32>
 hipError_t launch(const CacheFwdParams& p, const Shape& s, hipStream_t stream) {
@@ -951,12 +963,18 @@ hipError_t launch_d(const CacheFwdParams& p, const Shape& s, bool out_f32,
 
 }  // namespace
 
-size_t cache_fwd_workspace(const CacheDims& c, int32_t hq, int32_t num_requests,
+size_t cache_fwd_workspace(const CacheDims& c, int32_t num_requests,
                            int64_t rows) {
-  if (rows == 0 || num_requests == 0) return 0;
-  // The most that a call of no more rows and requests needs: 16 rows a tile
-  // and all workgroups, or fewer of both.
-  return size_t{1024} * (sizeof(CacheFold) + 2 * 32 * size_t(c.d + 2) * 4);
+  if (rows == 0 || num_requests == 0 || keys_of(c) <= kBriefKeys) return 0;
+  // What any call over this cache needs, so that it serves smaller ones.
+  size_t most = 0;
+  for (int nq = 1; nq <= 4; nq *= 2) {
+    const int groups = resident_groups(c.d, nq);
+    const size_t n = fold_bytes(groups) +
+                     part_rows(groups, nq) * (c.d + 2) * sizeof(float);
+    most = n > most ? n : most;
+  }
+  return most;
 }
 
 hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws,
@@ -968,9 +986,14 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
   p.unit_log2 = s.unit_log2;
   p.seq_units = s.seq_units;
   p.max_units = s.max_units;
-  p.fold = static_cast<CacheFold*>(ws);
-  p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + fold_bytes(s));
-  p.part_ml = p.part_o + part_rows(s) * p.c.d;
+  p.fold = nullptr;
+  p.part_o = p.part_ml = nullptr;
+  if (s.split) {
+    p.fold = static_cast<CacheFold*>(ws);
+    p.part_o =
+        reinterpret_cast<float*>(static_cast<char*>(ws) + fold_bytes(s.grid));
+    p.part_ml = p.part_o + part_rows(s.grid, s.nq) * p.c.d;
+  }
   return p.c.d == 128 ? launch_d<128>(p, s, out_f32, stream)
                       : launch_d<64>(p, s, out_f32, stream);
 }

@@ -556,18 +556,79 @@ def test_far_pages():
     assert torch.equal(out[0][1], out[1][1])
 
 
+@pytest.mark.parametrize("b,new", [(257, 1), (1000, 1), (4096, 1), (300, 3)])
+def test_many_requests(b, new):
+    """More requests than a workgroup keeps the lengths of, up to the limit."""
+    rng = np.random.default_rng(b)
+    c = cache_of(num_pages=8000, page_size=16, num_kv_heads=1, max_pages=70)
+    lens = np.minimum(np.exp(rng.uniform(0, 4.5, b)).astype(int), 60)
+    lens[rng.integers(b)] = 1100
+    lens = np.maximum(lens, new)
+    lens[:3] = 0
+    news = np.where(lens > 0, new, 0)
+    x = Batch(c, lens.tolist(), news.tolist(), group=2, seed=b)
+    check(x.run(), x.want(), 64)
+
+
+@pytest.mark.parametrize("lens", [[2**31 - 1, 5], [192, 2**31 - 1]])
+def test_lengths_past_the_table(lens):
+    for share in SHARES:
+        c = cache_of(num_pages=60, **share)
+        b = Batch(c, lens, [2, 1], seed=14)
+        check(b.run(), b.want(), 64)
+
+
+def test_tables_for_a_billion_tokens():
+    """max_pages at its limit: units of more keys, so that they can be counted."""
+    c = cache_of(num_pages=300, page_size=256, max_pages=1 << 22)
+    lens = [700, 0, 1, 5000] + [300 + i for i in range(76)]
+    new = [1, 0, 1, 3] + [1] * 76
+    small = Batch(cache_of(num_pages=300, page_size=256, max_pages=20), lens,
+                  new, seed=15)
+    want = small.want()
+    table = torch.full((80, 1 << 22), -1, **I32)
+    table[:, :20] = i32(small.table)
+    o = torch.full((len(small.positions), 4, 64), 123.0, device="cuda")
+    lse = torch.full((4, len(small.positions)), 123.0, device="cuda")
+    ma.mesh_attn_cache_fwd(c, small.scale, small.q.cuda(),
+                           i32(small.positions), i32(small.cu),
+                           i32(small.lens), table, small.data, o, lse)
+    check((o, lse), want, 64)
+
+
+def test_far_rows():
+    """Q and O past 2^31 elements: the last rows, over a few keys."""
+    c = cache_of(head_dim=128, num_kv_heads=1, page_size=64, num_pages=4)
+    rows, hq = 140000, 128
+    q = torch.zeros(rows, hq, 128, dtype=torch.bfloat16, device="cuda")
+    assert q.numel() > 2**31
+    b = Batch(c, [40, 100], [1, 5], group=hq, seed=16)
+    q[-6:] = b.q.cuda()
+    cu = [0, rows - 5, rows]
+    positions = np.full(rows, -1)
+    positions[-6:] = b.positions
+    o = torch.full((rows, hq, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((hq, rows), 7.0, device="cuda")
+    ma.mesh_attn_cache_fwd(c, b.scale, q, i32(positions), i32(cu),
+                           i32(b.lens), i32(b.table), b.data, o, lse)
+    check((o[-6:], lse[:, -6:].contiguous()), b.want(), 128)
+    assert not o[:-6].any() and torch.all(lse[:, :-6] == -float("inf"))
+
+
 def test_fewer_bytes_of_workspace_are_refused():
     c = cache_of(num_pages=300, max_pages=256, page_size=64)
     need = ma.mesh_attn_cache_fwd_workspace_size(c, 4, 1, 1)
+    assert 0 < need <= 35 << 20
     b = Batch(c, [5000], [1], seed=13)
-    if need:
-        ws = torch.empty(need - 1, dtype=torch.uint8, device="cuda")
-        with pytest.raises(ma.MeshAttnError, match="workspace"):
-            b.run(ws=ws)
-    ws = torch.full((max(need, 16) + 256,), 0xAB, dtype=torch.uint8,
-                    device="cuda")
-    check(b.run(ws=ws[:max(need, 16)]), b.want(), 64)
-    assert torch.all(ws[max(need, 16):] == 0xAB)
+    ws = torch.empty(need - 1, dtype=torch.uint8, device="cuda")
+    with pytest.raises(ma.MeshAttnError, match="workspace"):
+        b.run(ws=ws)
+    # Whatever it held, and nothing behind it is written.
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    check(b.run(ws=ws[:need]), b.want(), 64)
+    assert torch.all(ws[need:] == 0xFF)
+    brief = cache_of(max_pages=32)
+    assert ma.mesh_attn_cache_fwd_workspace_size(brief, 4, 1, 1) == 0
 
 
 # -- together -----------------------------------------------------------------

@@ -165,11 +165,11 @@ def _size(c, hq, n, rows):
 def test_fwd_workspace():
     c = _cache(num_pages=4096, max_pages=4096)
     need = _size(c, 4, 3, 5)
-    assert need <= 68 << 20
-    if need:
-        assert _fwd(c, ws_bytes=need - 1) == TOO_SMALL
-        assert _fwd(c, ws=None, ws_bytes=need) == INVALID
-        assert _fwd(c, ws=A + 8, ws_bytes=need) == INVALID
+    assert 0 < need <= 35 << 20
+    assert _fwd(c, ws_bytes=need - 1) == TOO_SMALL
+    assert _fwd(c, ws=None, ws_bytes=need) == INVALID
+    assert _fwd(c, ws=A + 8, ws_bytes=need) == INVALID
+    assert _size(_cache(), 4, 3, 5) == 0
     assert _size(c, 3, 3, 5) == _size(c, 4, -1, 5) == _size(c, 4, 3, -1) == 0
     assert _size(_cache(page_size=5), 4, 3, 5) == 0
 
@@ -182,7 +182,7 @@ def test_fwd_workspace_never_shrinks(d, group):
              for n in (1, 2, 3, 7, 16, 64, 300, 4096)
              for r in (1, 2, 3, 8, 17, 64, 1000, 4096, 100000)}
     for (n, r), s in sizes.items():
-        assert s <= 68 << 20
+        assert 0 < s <= 35 << 20
         for (n2, r2), s2 in sizes.items():
             if n2 >= n and r2 >= r:
                 assert s2 >= s
