@@ -294,6 +294,7 @@ ma_status_t mesh_attn_cache_fwd(
   p.group = num_q_heads / p.c.hkv;
   p.num_requests = num_requests;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
+  p.inv_scale_log2 = 1.f / p.scale_log2;
   return launched(launch_cache_fwd(p, o_dtype == MA_FP32, ws, stream),
                   "cache_fwd launch");
 }

@@ -96,7 +96,7 @@ struct CacheFwdParams {
   float* lse;
   int64_t rows;
   int32_t hq, group, num_requests;
-  float scale_log2;
+  float scale_log2, inv_scale_log2;
   int32_t split;      // whether sequences are cut
   int32_t unit_log2;  // keys of a unit
   int32_t seq_units;  // units that a sequence costs beside its keys

@@ -178,15 +178,18 @@ template <int D, int NQ>
 struct State {
   bf16x8 q[kQInLds<NQ> ? 1 : NQ][D / 32];
   f32x4 o[NQ][D / 16];  // O^T, MFMA m of the lane's D/4 dims
-  float m[NQ], l[NQ];   // running maximum (log2 units); this lane's share of
-                        // the sum
+  // Probabilities are 2^(score * scale - ref), with the reference at most kLag
+  // below the row's running maximum; a score above `limit` moves it.  A row
+  // without a finite score so far: limit -inf, neg_ref 0.
+  float limit[NQ], neg_ref[NQ];
+  float l[NQ];          // this lane's share of the sum
   int vis[NQ];          // stored keys that the column's row sees
 };
 
-// The running maximum may lag behind by this much (log2 units): probabilities
-// stay below 2^kLag, as exact relative to each other as below 1, and the
-// accumulators are rescaled a few times per item instead of whenever a row's
-// maximum grows.
+// The reference may lag behind the maximum by this much (log2 units):
+// probabilities stay below 2^kLag, as exact relative to each other as below 1,
+// and the accumulators are rescaled a few times per item instead of whenever a
+// row's maximum grows.
 constexpr float kLag = 8.f;
 
 // Probabilities as the second product's operand.  For a bf16 O: rounded to
@@ -229,31 +232,46 @@ template <int D, int NQ, bool EXACT>
 __device__ __forceinline__ void finish_step(State<D, NQ>& st,
                                             f32x4 (&x)[NQ][2],
                                             const StepData<D>& s,
-                                            float scale_log2, u32x2 vs) {
+                                            float scale_log2,
+                                            float inv_scale_log2, u32x2 vs) {
   Probs<EXACT> ph[NQ];
+  // One branch for all rows: it is rarely taken.
+  float top[NQ];
+  bool above = false;
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
-    float top = x[q][0][0];
+    top[q] = x[q][0][0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[q][i >> 2][i & 3]);
-    top *= scale_log2;
-    if (__any(top > st.m[q] + kLag)) {
-      const float mn = fmaxf(
-          st.m[q],
-          across_quarters(top, [](float a, float b) { return fmaxf(a, b); }));
+    for (int i = 1; i < 8; ++i) top[q] = fmaxf(top[q], x[q][i >> 2][i & 3]);
+    above |= top[q] > st.limit[q];
+  }
+  if (__any(above)) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const float t =
+          across_quarters(top[q], [](float a, float b) { return fmaxf(a, b); }) *
+          scale_log2;
+      const bool none = st.limit[q] == -INFINITY;
+      const float m = none ? t : fmaxf(-st.neg_ref[q], t);
+      const bool still = !(m > -INFINITY);  // also for a NaN
+      // Sums without a finite score so far are 0, or NaN.
       const float f =
-          mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[q] - mn);
-      st.m[q] = mn;
+          still || none ? 1.f : __builtin_amdgcn_exp2f(-st.neg_ref[q] - m);
+      st.limit[q] = still ? -INFINITY
+                          : fmaxf((m + kLag) * inv_scale_log2, -3e38f);
+      st.neg_ref[q] = still ? 0.f : -m;
       st.l[q] *= f;
 #pragma unroll
-      for (int m = 0; m < D / 16; ++m) st.o[q][m] *= f;
+      for (int m16 = 0; m16 < D / 16; ++m16) st.o[q][m16] *= f;
     }
-    const float ref = st.m[q] == -INFINITY ? 0.f : st.m[q];
+  }
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
     float p[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       p[i] = __builtin_amdgcn_exp2f(
-          fmaf(x[q][i >> 2][i & 3], scale_log2, -ref));
+          fmaf(x[q][i >> 2][i & 3], scale_log2, st.neg_ref[q]));
     st.l[q] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     split_probs<EXACT>(p, &ph[q]);
   }
@@ -660,7 +678,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
             st.l[q], [](float a, float b) { return a + b; });
         lds_barrier();
         if (g == 0) {
-          s_m[wave][r] = st.m[q];
+          s_m[wave][r] =
+              st.limit[q] == -INFINITY ? -INFINITY : -st.neg_ref[q];
           s_l[wave][r] = l;
         }
 #pragma unroll
@@ -679,7 +698,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
           float L = 0.f, acc[8] = {};
 #pragma unroll
           for (int w = 0; w < kWaves; ++w) {
-            // A wave without a maximum has sums of 0, or of NaN.
+            // A wave without a finite score has sums of 0, or of NaN.
             const float sm = s_m[w][row16] == -INFINITY
                                  ? 1.f
                                  : __builtin_amdgcn_exp2f(s_m[w][row16] - ref);
@@ -716,8 +735,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
                         : 0;
       most_seen = max(most_seen, st.vis[q]);
       if (valid) all_see = min(all_see, st.vis[q]);
-      st.m[q] = -INFINITY;
-      st.l[q] = 0.f;
+      st.limit[q] = -INFINITY;
+      st.neg_ref[q] = st.l[q] = 0.f;
 #pragma unroll
       for (int m = 0; m < D / 16; ++m) st.o[q][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -752,7 +771,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
         const bool ok = lane_ok<P16>(h, pg, g);
         if (kb + kStep > all_see || !__all(ok))
           vs = mask_step<D, NQ>(st, x, s, ok, kb, h.local, g);
-        finish_step<D, NQ, OUT_F32>(st, x, s, p.scale_log2, vs);
+        finish_step<D, NQ, OUT_F32>(st, x, s, p.scale_log2,
+                                    p.inv_scale_log2, vs);
         if (!more_keys) break;
         load_v<D, P16>(h, pn, next, g, &s);
         pg = pn;
