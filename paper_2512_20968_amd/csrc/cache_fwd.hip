@@ -484,7 +484,7 @@ __device__ __forceinline__ int plan_units(const CacheFwdParams& p, int* s_units,
                   : 1;
       const int64_t n = int64_t{tiles} * (nu + p.seq_units) * p.c.hkv;
       mine = static_cast<int>(n < p.max_units ? n : p.max_units);
-      if (kRows > 32 && tiles > 1) atomicMax(s_longest, nu + p.seq_units);
+      if (kRows > 16 && tiles > 1) atomicMax(s_longest, nu + p.seq_units);
     }
     int y = mine;
 #pragma unroll
@@ -604,7 +604,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
   int run = blockIdx.x, per = 1, at = run, stop = total;
   if (p.split) {
     per = max((total + int(gridDim.x) - 1) / int(gridDim.x), 1);
-    if (kRows > 32 && longest > 0) {
+    if (kRows > 16 && longest > 0) {
       // Whole sequences per run, where that costs at most a twentieth: the tiles
       // of a head then walk over the keys side by side, and find them in their
       // L2.  1000 rows of 4 heads a request over 33K tokens: 30 million misses
@@ -925,12 +925,14 @@ int64_t keys_of(const CacheDims& c) {
 constexpr int64_t kBriefKeys = 512;
 
 Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
-               int64_t rows) {
+               int64_t rows, bool out_f32) {
   const int group = hq / c.hkv;
   Shape s;
   // Rows of a request, were they all alike.
   const int64_t each = (rows + num_requests - 1) / num_requests * group;
-  s.nq = each <= 16 ? 1 : each <= 32 ? 2 : 4;
+  // Three bf16 parts of 64 rows' probabilities do not fit the registers: 1000
+  // rows of 4 heads over 33K tokens take 1894 us in tiles of 32 rows, 2175 of 64.
+  s.nq = each <= 16 ? 1 : each <= 32 || out_f32 ? 2 : 4;
   // Most sequences that rows which do not overlap make.
   const int64_t seqs = (rows * group / (16 * s.nq) + num_requests) * c.hkv;
   const int slots = resident_groups(c.d, s.nq);
@@ -982,19 +984,15 @@ hipError_t launch(const CacheFwdParams& p, const Shape& s, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int D, int NQ>
-hipError_t launch_out(const CacheFwdParams& p, const Shape& s, bool out_f32,
-                      hipStream_t stream) {
-  return out_f32 ? launch<D, NQ, true>(p, s, stream)
-                 : launch<D, NQ, false>(p, s, stream);
-}
-
 template <int D>
 hipError_t launch_d(const CacheFwdParams& p, const Shape& s, bool out_f32,
                     hipStream_t stream) {
-  if (s.nq == 1) return launch_out<D, 1>(p, s, out_f32, stream);
-  if (s.nq == 2) return launch_out<D, 2>(p, s, out_f32, stream);
-  return launch_out<D, 4>(p, s, out_f32, stream);
+  if (s.nq == 4) return launch<D, 4, false>(p, s, stream);
+  if (s.nq == 2)
+    return out_f32 ? launch<D, 2, true>(p, s, stream)
+                   : launch<D, 2, false>(p, s, stream);
+  return out_f32 ? launch<D, 1, true>(p, s, stream)
+                 : launch<D, 1, false>(p, s, stream);
 }
 
 }  // namespace
@@ -1016,7 +1014,7 @@ size_t cache_fwd_workspace(const CacheDims& c, int32_t num_requests,
 hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws,
                             hipStream_t stream) {
   const Shape s = shape_of(params.c, params.hq, params.num_requests,
-                           params.rows);
+                           params.rows, out_f32);
   CacheFwdParams p = params;
   p.split = s.split;
   p.unit_log2 = s.unit_log2;
