@@ -111,7 +111,9 @@ __global__ __launch_bounds__(NT) void rope_kernel(RopeParams p) {
   const uint32_t rot_units = half / N,
                  units = rot_units + (p.d - p.rot) / N;
   const uint32_t heads = p.heads[0] + p.heads[1], of_row = heads * units;
-  const int64_t row0 = int64_t{blockIdx.x} * p.group_rows;
+  const int64_t row0 =
+      (int64_t{blockIdx.y} * gridDim.x + blockIdx.x) * p.group_rows;
+  if (row0 >= p.rows) return;
   const uint32_t rows = static_cast<uint32_t>(
       min(int64_t{p.group_rows}, p.rows - row0));
   const uint32_t items = rows * of_row;
@@ -201,8 +203,11 @@ hipError_t launch_rope(const RopeParams& params, bool f32,
   while (2 * p.group_rows * (p.rot / 2) <= NT &&
          p.rows >= int64_t{2 * p.group_rows} * kGroups)
     p.group_rows *= 2;
-  const dim3 g(static_cast<unsigned>((p.rows + p.group_rows - 1) /
-                                     p.group_rows));
+  // A launch counts its threads in 32 bits per dimension.
+  const int64_t groups = (p.rows + p.group_rows - 1) / p.group_rows;
+  const int64_t side = groups < (1 << 22) ? groups : 1 << 22;
+  const dim3 g(static_cast<unsigned>(side),
+               static_cast<unsigned>((groups + side - 1) / side));
   if (f32) {
     if (p.interleaved)
       hipLaunchKernelGGL((rope_kernel<true, true>), g, dim3(NT), 0, stream, p);

@@ -143,3 +143,21 @@ def test_captured_and_on_another_stream():
     ma.mesh_attn_rope(r, pos, x, z, stream=side)
     side.synchronize()
     assert torch.equal(z, want)
+
+
+def test_more_rows_than_a_launch_counts_threads():
+    """33.6 million rows, two to a workgroup of 256 threads: past 2^32 threads."""
+    rows = 2**25 + 2**10 + 3
+    r = _rope(256, 256, 1, 0)
+    x = torch.zeros(rows, 1, 256, dtype=torch.bfloat16, device="cuda")
+    assert x.numel() > 2**32
+    pos = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    tail = torch.randn(700, 1, 256, generator=torch.Generator().manual_seed(5))
+    x[-700:] = tail.to(torch.bfloat16).cuda()
+    pos[-700:] = torch.arange(700, device="cuda").int() * 1009
+    y, p = x[-700:].clone(), pos[-700:].clone()
+    ma.mesh_attn_rope(r, pos, x, x)
+    want = torch.empty_like(y)
+    ma.mesh_attn_rope(r, p, y, want)
+    assert torch.equal(x[-700:], want)
+    assert not x[:1000].any() and not x[-2000:-700].any()
