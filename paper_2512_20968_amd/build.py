@@ -33,8 +33,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # bf16-output kernel's schedule runs 0.5-1.6 % faster.
 # The attention over the cache keeps every join's own restore of the execution
 # mask: without it a register that was saved inside a nested branch of the fold
-# was restored for the inner branch's lanes alone (seen in the assembly of the
-# 64-row float32 kernel, whose next item then used it in an address).
+# was restored for the inner branch's lanes alone (seen in the assembly of a
+# float32 kernel of 64 rows, whose next item then used it in an address).
 EXTRA = {"cache_fwd.hip": ["-mllvm", "-amdgpu-remove-redundant-endcf=0"],
          "tile_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "tile_fwd.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers"]}

@@ -91,7 +91,7 @@ __device__ __forceinline__ bool valid_page(const Keys& h, int32_t id) {
 }
 
 // The block of the page of half `second` of a step; page 0's for an invalid
-// page, whose keys compute_step() does not use.
+// page, whose keys mask_step() hides.
 template <bool P16>
 __device__ __forceinline__ const uint8_t* page_block(const Keys& h,
                                                      const StepPages& pages,
@@ -432,11 +432,11 @@ __device__ __forceinline__ int32_t stored_keys(const CacheFwdParams& p,
 // units in a row are dealt to the workgroups in equal runs of `per`, so every
 // workgroup has the same work whatever the lengths, which only the device
 // knows.  What a sequence costs beside its keys (finding it, the first loads, the
-// fold) counts as seq_units units in front of them.  A sequence that lies in several runs leaves partial results, two slots
-// a workgroup at most: slot 2 w for the piece that goes on from an earlier run,
-// slot 2 w + 1 for the one that starts in run w and goes on after it;
-// cache_fold_kernel joins them.  p.split 0: every sequence is one unit, and no
-// piece is split.
+// fold) counts as seq_units units in front of them.  A sequence that lies in
+// several runs leaves partial results, two slots a workgroup at most: slot 2 w
+// for the piece that goes on from an earlier run, slot 2 w + 1 for the one that
+// starts in run w and goes on after it; cache_fold_kernel joins them.  p.split 0:
+// every sequence is one unit, and no piece is split.
 constexpr int kWaveKeys = kWaves * kStep;  // keys of a step of each wave
 
 // What the prefix sums leave in LDS per request: its first unit, and, for up to
@@ -608,7 +608,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
       // Whole sequences per run, where that costs at most a twentieth: the tiles
       // of a head then walk over the keys side by side, and find them in their
       // L2.  1000 rows of 4 heads a request over 33K tokens: 30 million misses
-      // and 1103 us without, 1.2 million and 1022 us with.
+      // and 1103 us without, 2 million and 1037 us with.
       longest = __builtin_amdgcn_readfirstlane(longest);
       const int whole = (per + longest - 1) / longest * longest;
       if (whole - per <= per / 20) per = whole;
@@ -619,7 +619,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
     // The others take the runs behind the active ones, without work.
     run = y < each ? x * each + y
                    : 8 * each + x * (int(gridDim.x / 8) - each) + y - each;
-    // Below 2^31: per * gridDim is at most total + gridDim.
+    // Below 2^31: total is below 2^30, and per * gridDim at most a twentieth
+    // and two gridDim larger.
     at = per * run;
     stop = min(at + per, total);
     if (tid == 0) p.fold[run].parts = 0;
@@ -943,7 +944,13 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   //   1 of 1024               10.0/11.6  64 of 1024   22.0/17.3
   //   1 of 2048               10.4/16.4  32 of 1..1024 13.5/11.4
   const bool brief = keys <= kBriefKeys || (keys <= 1024 && seqs >= 256);
-  s.split = !brief && seqs < 4 * slots;
+  // Where there are several sequences per workgroup anyway, those of more tiles
+  // than one stay whole, for their L2's sake; those of one tile are cut, since
+  // their lengths may differ.  Microseconds cut / whole, 8 KV heads of 4:
+  //   8 x 2000 rows of 2000 tokens 597/428   512 x 1 of 1 to 32K  343/446
+  //   1 x 8000 rows of 9000        992/678   1024 x 1 of 1 to 64K 1108/1499
+  const bool one_tile = each <= 16 * s.nq && seqs < (1 << 24);
+  s.split = !brief && (seqs < 4 * slots || one_tile);
   s.unit_log2 = 7;
   static_assert(kWaveKeys == 1 << 7, "least unit");
   // Units are counted in 32 bits.
