@@ -460,7 +460,7 @@ ma_status_t mesh_attn_cache_tables(
     int32_t* cu_new, int64_t rows, int64_t* slots, int32_t* positions,
     int32_t* free_range_out, int32_t* refused, hipStream_t stream);
 
-/* Stores rows of K and V in 4 bits.
+/* Stores rows of K and V in 4 bits; rows < 2^30.
  *   k, v   row r, head h at k + r * k_stride + h * head_dim, bf16 device; the
  *          strides are in elements, multiples of 8, >= Hkv * d (slices of a
  *          fused projection's output).
@@ -480,7 +480,7 @@ ma_status_t mesh_attn_cache_append(const ma_cache_t* cache, int64_t rows,
                                    const int64_t* slots, void* data,
                                    hipStream_t stream);
 
-/* Reads stored rows back, exactly, as bf16 [rows][Hkv][d]: the KV buffer of
+/* Reads rows (fewer than 2^30) back, exactly, as bf16 [rows][Hkv][d]: the KV buffer of
  * the tile calls (a cached prefix under a new tile).  Rows whose slot is out of
  * range are 0. */
 ma_status_t mesh_attn_cache_read(const ma_cache_t* cache, int64_t rows,
@@ -511,10 +511,10 @@ size_t mesh_attn_cache_fwd_workspace_size(const ma_cache_t* cache,
  *              exactly later).
  *   lse        [Hq][rows] float32 device, natural log; -inf for a row that
  *              sees no key, whose O row is 0.
- * Rows of no request are left as they were.  O and LSE are those of
+ * Requests may share pages.  Rows of no request are left as they were.  O and LSE are those of
  * mesh_attn_tile_fwd over the stored values: exact products, float32
  * accumulation and softmax; the probabilities enter the second product in bf16
- * for a bf16 O, and as a sum of two bf16 for a float32 O.  A NaN key or value
+ * for a bf16 O, and as a sum of three bf16 for a float32 O.  A NaN key or value
  * reaches the rows that see it and no other.  A split of the keys over
  * workgroups depends on the sizes and lengths alone: equal calls give equal
  * bits. */

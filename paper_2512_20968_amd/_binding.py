@@ -743,9 +743,9 @@ def mesh_attn_cache_fwd(cache, softmax_scale, q, positions, cu_new, lens,
     f32 = o.dtype is torch.float32
     if ws is None:
         n = mesh_attn_cache_fwd_workspace_size(c, hq, b, rows)
-        ws = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
-        if stream is not None:
-            ws.record_stream(stream)
+        # Of the call's own stream, on which alone it is used.
+        with torch.cuda.stream(stream):
+            ws = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
     elif ws.get_device() != dev or not ws.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor of the call's "
                          "GPU")
@@ -772,8 +772,9 @@ def mesh_attn_cache_fwd(cache, softmax_scale, q, positions, cu_new, lens,
 def mesh_attn_rope(rope, positions, q, q_out, k=None, k_out=None, inverse=0,
                    stream=None):
     """Turns the heads of ``q [rows, heads, d]`` (and of ``k``) by their rows'
-    ``positions [num_axes, rows]`` (int32; ``[rows]`` does for one axis) into ``q_out``, ``k_out`` (the same
-    tensors for in place); bf16 or float32, row strides as they are.
+    ``positions [num_axes, rows]`` (int32; ``[rows]`` does for one axis) into
+    ``q_out``, ``k_out`` (the same tensors for in place); bf16 or float32, row
+    strides as they are.
     ``inverse=1`` turns back: the gradient."""
     r = Rope.make(rope)
     if (k is None) != (k_out is None):

@@ -80,14 +80,16 @@ ma_status_t check_cache(const ma_cache_t* c, CacheDims* out) {
   return MA_OK;
 }
 
-constexpr int64_t kMaxRows = int64_t{1} << 31;
-
-ma_status_t check_rows(int64_t rows) {
-  if (rows < 0 || rows >= kMaxRows)
-    return fail(MA_ERR_INVALID_ARG, "rows %lld outside [0, 2^31)",
-                static_cast<long long>(rows));
+ma_status_t check_rows(int64_t rows, int log2 = 31) {
+  if (rows < 0 || rows >= int64_t{1} << log2)
+    return fail(MA_ERR_INVALID_ARG, "rows %lld outside [0, 2^%d)",
+                static_cast<long long>(rows), log2);
   return MA_OK;
 }
+
+// Rows that append and read take: a launch counts its threads in 32 bits, and
+// a workgroup of 256 has 64 rows at least where there are many.
+constexpr int kStoreRowsLog2 = 30;
 
 ma_status_t check_requests(int32_t n) {
   if (n < 0 || n > MA_CACHE_MAX_REQUESTS)
@@ -194,7 +196,7 @@ ma_status_t mesh_attn_cache_append(const ma_cache_t* cache, int64_t rows,
                                    hipStream_t stream) {
   StoreParams p;
   MA_TRY(check_cache(cache, &p.c));
-  MA_TRY(check_rows(rows));
+  MA_TRY(check_rows(rows, kStoreRowsLog2));
   const int64_t width = int64_t{p.c.hkv} * p.c.d;
   MA_TRY(check_stride("k_stride", k_stride, width, 8));
   MA_TRY(check_stride("v_stride", v_stride, width, 8));
@@ -217,7 +219,7 @@ ma_status_t mesh_attn_cache_read(const ma_cache_t* cache, int64_t rows,
                                  void* k, void* v, hipStream_t stream) {
   LoadParams p;
   MA_TRY(check_cache(cache, &p.c));
-  MA_TRY(check_rows(rows));
+  MA_TRY(check_rows(rows, kStoreRowsLog2));
   if (rows == 0) return ok();
   const Arg args[] = {
       {"slots", slots, 8}, {"data", data, 16}, {"k", k, 16}, {"v", v, 16}};
@@ -253,7 +255,9 @@ ma_status_t mesh_attn_cache_fwd(
   MA_TRY(check_q_heads(num_q_heads, p.c.hkv));
   MA_TRY(check_requests(num_requests));
   MA_TRY(check_rows(rows));
-  if (!(softmax_scale > 0.f) || !std::isfinite(softmax_scale))
+  p.scale_log2 = softmax_scale * 1.4426950408889634f;
+  p.inv_scale_log2 = 1.f / p.scale_log2;
+  if (!(softmax_scale > 0.f) || !std::isfinite(p.scale_log2))
     return fail(MA_ERR_INVALID_ARG, "softmax_scale must be positive and "
                 "finite");
   if (o_dtype != MA_BF16 && o_dtype != MA_FP32)
@@ -293,8 +297,6 @@ ma_status_t mesh_attn_cache_fwd(
   p.hq = num_q_heads;
   p.group = num_q_heads / p.c.hkv;
   p.num_requests = num_requests;
-  p.scale_log2 = softmax_scale * 1.4426950408889634f;
-  p.inv_scale_log2 = 1.f / p.scale_log2;
   return launched(launch_cache_fwd(p, o_dtype == MA_FP32, ws, stream),
                   "cache_fwd launch");
 }
@@ -333,7 +335,8 @@ ma_status_t mesh_attn_rope(const ma_rope_t* rope, int64_t rows,
     p.t.axis[i] = 0;
   }
   // Turns per position modulo 1, in 2^-64: the extended type's 64-bit fraction
-  // holds the product to about a unit of that for frequencies up to 2 pi, and the kernel's product with the position wraps as turns do.
+  // holds the product to about a unit of that for frequencies up to 2 pi, and
+  // the kernel's product with the position wraps as turns do.
   const long double kPerRadian = 0.159154943091895335768883763372514362L;
   for (int i = 0; i < rot / 2; ++i) {
     const double f = rope->inv_freq[i];

@@ -13,11 +13,11 @@ struct CacheShare {
   int32_t striped, n, p;
   int64_t first, len;  // contiguous: [first, first + len)
 
-  // Number of stored positions < x.
+  // Number of stored positions < x, for x up to 2^31; at most 2^31 - 1.
   __host__ __device__ int32_t below(int64_t x) const {
     if (striped) {
       if (x <= p) return 0;
-      if (n == 1) return static_cast<int32_t>(x);
+      if (n == 1) return static_cast<int32_t>(x < INT32_MAX ? x : INT32_MAX);
       // x - p + n - 1 < 2^31 + 2^31.
       return static_cast<int32_t>(static_cast<uint32_t>(x - p + n - 1) /
                                   static_cast<uint32_t>(n));

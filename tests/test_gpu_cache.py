@@ -329,9 +329,9 @@ def check(got, want, d, keys=4096):
     * max_j sum_i |q_i k_ji|: a score is a float32 sum of d exact products
     (truncation allowed for: 2u each) times a rounded scale, so it is off by at
     most (d + 16) 2u reach; a probability by twice that and its exponential's
-    and the sums' roundings, together below 2^-14 for up to 4096 keys; float32 O
-    adds the 2^-16 of a probability's two bf16 parts, bf16 O 2^-8 for the
-    probabilities and 2^-8 for itself."""
+    and the sums' roundings, together (the 2^-23 of a probability's three bf16
+    parts for a float32 O too) below 2^-14 for up to 4096 keys; bf16 O adds 2^-8
+    for the probabilities and 2^-8 for itself."""
     o, lse = (x.double().cpu().numpy() for x in got)
     wo, wl, mass, reach = want
     live = ~np.isnan(reach)
@@ -393,13 +393,13 @@ def test_rows_and_groups(d, hkv, group, new):
     check(b.run(torch.float32 if new % 2 else torch.bfloat16), b.want(), d)
 
 
-@pytest.mark.parametrize("share", SHARES[1:])
+@pytest.mark.parametrize("share", SHARES)
 @pytest.mark.parametrize("d", [64, 128])
 def test_shares_and_rows_without_keys(share, d):
     """Rows before the first stored position, positions of -1 and far past the
     end, a length past the table."""
     c = cache_of(head_dim=d, num_pages=60, **share)
-    lens = [1, 2, 100, 190, 5000]
+    lens = [1, 2, 100, 190, 5000]  # the last one past the table
     new = [1, 2, 7, 20, 3]
     b = Batch(c, lens, new, group=4, seed=4)
     b.positions[5] = -1
@@ -457,6 +457,18 @@ def test_no_key_survives_a_nan_length_of_garbage():
         b.cu = np.array(cu)
         o, lse = b.run()
         assert o.shape[0] == 9 and not torch.isnan(lse).any()
+
+
+def test_requests_that_share_pages_and_positions_in_any_order():
+    c = cache_of(head_dim=128, num_pages=60)
+    b = Batch(c, [190, 170, 190, 40], [9, 5, 17, 1], group=4, seed=16)
+    b.table[1, :8] = b.table[0, :8]
+    b.table[2] = b.table[0]
+    rng = np.random.default_rng(16)
+    for _ in range(2):
+        check(b.run(), b.want(), 128)
+        check(b.run(torch.bfloat16), b.want(), 128)
+        b.positions = rng.integers(-2, 200, len(b.positions))
 
 
 def test_scores_of_every_size():
@@ -557,10 +569,10 @@ def test_far_pages():
 
 
 @pytest.mark.parametrize("b,new", [(257, 1), (1000, 1), (4096, 1), (300, 3)])
-def test_many_requests(b, new):
+def test_many_requests(b, new, hkv=1):
     """More requests than a workgroup keeps the lengths of, up to the limit."""
     rng = np.random.default_rng(b)
-    c = cache_of(num_pages=8000, page_size=16, num_kv_heads=1, max_pages=70)
+    c = cache_of(num_pages=8000, page_size=16, num_kv_heads=hkv, max_pages=70)
     lens = np.minimum(np.exp(rng.uniform(0, 4.5, b)).astype(int), 60)
     lens[rng.integers(b)] = 1100
     lens = np.maximum(lens, new)
@@ -568,6 +580,11 @@ def test_many_requests(b, new):
     news = np.where(lens > 0, new, 0)
     x = Batch(c, lens.tolist(), news.tolist(), group=2, seed=b)
     check(x.run(), x.want(), 64)
+
+
+def test_many_heads_of_many_requests():
+    """More sequences than workgroups, several of one to a workgroup."""
+    test_many_requests(1300, 1, hkv=6)
 
 
 @pytest.mark.parametrize("lens", [[2**31 - 1, 5], [192, 2**31 - 1]])
