@@ -77,10 +77,10 @@ struct LoadParams {
 };
 hipError_t launch_cache_read(const LoadParams& p, hipStream_t stream);
 
-// A sequence of the attention whose partial results are to be joined: the runs
-// of `parts` workgroups from this one on (0: none starts here).
+// A sequence of the attention whose partial results are to be joined: those of
+// `parts` runs from `start` on (0: none).
 struct CacheFold {
-  int32_t first, rr0, rr_end, kvh, parts, pad[3];
+  int32_t first, rr0, rr_end, kvh, parts, start, pad[2];
 };
 
 struct CacheFwdParams {
@@ -101,7 +101,7 @@ struct CacheFwdParams {
   int32_t unit_log2;  // keys of a unit
   int32_t seq_units;  // units that a sequence costs beside its keys
   int32_t max_units;  // most of a launch
-  CacheFold* fold;           // [workgroup]
+  CacheFold* fold;           // [workgroup][2]: goes on in its run, starts in it
   float* part_o;             // [2 * workgroups][rows of a tile][d]
   float* part_ml;            // .. [2]: reference (log2 units) and sum
 };

@@ -534,11 +534,12 @@ struct Item {
 };
 
 // The item at unit `at` of a run that ends at `stop`.
-template <int kRows>
+template <int kRows, bool OWN>
 __device__ __forceinline__ Item locate(const CacheFwdParams& p,
                                        const int* s_units,
                                        const RequestRows* s_kept, int at,
                                        int stop) {
+  const bool split = !OWN && p.split;
   const int B = p.num_requests, hkv = p.c.hkv;
   int lo = 0, hi = B;
   while (hi - lo > 1) {
@@ -556,17 +557,26 @@ __device__ __forceinline__ Item locate(const CacheFwdParams& p,
   it.rr_end = __builtin_amdgcn_readfirstlane(req.end - req.first) * p.group;
   it.local = __builtin_amdgcn_readfirstlane(req.local);
   it.nu =
-      p.split ? max((it.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1) : 1;
+      split ? max((it.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1) : 1;
   const int off = at - __builtin_amdgcn_readfirstlane(s_units[it.b]);
   const int len = it.nu + p.seq_units, seq = off / len;
   const int v0 = off - seq * len;  // of the sequence's units with its cost
   it.u0 = max(v0 - p.seq_units, 0);
-  it.u1 = p.split ? min(v0 + (stop - at) - p.seq_units, it.nu) : 1;
-  it.end = p.split ? min(at - v0 + len, stop) : at + int(gridDim.x);
+  it.u1 = split ? min(v0 + (stop - at) - p.seq_units, it.nu) : 1;
+  it.end = split ? min(at - v0 + len, stop)
+                 : at + int(gridDim.x) * (OWN ? kWaves : 1);
+  const int tiles = (it.rr_end + kRows - 1) / kRows;
   int tile;
-  if (p.split) {
+  if (OWN) {
+    // The waves of a workgroup take neighbouring tiles of a head, and the next
+    // workgroups, which run on other XCDs, the same tiles of the next heads.
+    // Causal rows: the last tiles, which see the most keys, come first.
+    const int quad = seq / (kWaves * hkv), rest = seq - quad * (kWaves * hkv);
+    const int n = min(kWaves, tiles - quad * kWaves);
+    it.kvh = rest / n;
+    tile = tiles - 1 - (quad * kWaves + rest - it.kvh * n);
+  } else if (split) {
     // Runs of neighbouring tiles of a head read the same keys.
-    const int tiles = (it.rr_end + kRows - 1) / kRows;
     it.kvh = seq / tiles;
     tile = seq - it.kvh * tiles;
   } else {
@@ -579,14 +589,17 @@ __device__ __forceinline__ Item locate(const CacheFwdParams& p,
   return it;
 }
 
-template <int D, int NQ, bool OUT_F32, bool P16>
+// OWN: every wave has items of its own, whole sequences, and nothing to fold.
+template <int D, int NQ, bool OUT_F32, bool P16, bool OWN>
 __global__ __launch_bounds__(NT, (kWavesPerSimd<D, NQ>))
 void cache_fwd_kernel(CacheFwdParams p) {
   constexpr int kRows = 16 * NQ;
   constexpr int kPad = D + 4;  // row stride of the fold, in floats
-  __shared__ float s_o[kWaves][16][kPad];
-  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  __shared__ bf16x8 s_q[kQInLds<NQ> ? NQ * (D / 32) * 64 : 1];
+  constexpr int kFolded = OWN ? 1 : kWaves;
+  constexpr int kQ = NQ * (D / 32) * 64;
+  __shared__ float s_o[kFolded][16][kPad];
+  __shared__ float s_m[kFolded][16], s_l[kFolded][16];
+  __shared__ bf16x8 s_q_all[kQInLds<NQ> ? (OWN ? kWaves : 1) * kQ : 1];
   __shared__ int s_wave[kWaves], s_longest;
   extern __shared__ int s_units[];  // [B + 1], then the kept requests
   const int tid = threadIdx.x, lane = tid & 63;
@@ -594,6 +607,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
   const int r = lane & 15, g = lane >> 4;
   RequestRows* s_kept =
       reinterpret_cast<RequestRows*>(s_units + p.num_requests + 1);
+  bf16x8* s_q = s_q_all + (OWN && kQInLds<NQ> ? wave * kQ : 0);
+  const bool split = !OWN && p.split;
 
   int longest;
   const int total = __builtin_amdgcn_readfirstlane(
@@ -601,8 +616,9 @@ void cache_fwd_kernel(CacheFwdParams p) {
   // Split: this workgroup's run.  Workgroup i runs on XCD i % 8; neighbouring
   // runs go to one XCD (the grid is a multiple of 8), whose L2 then serves the
   // tiles of a head, and the runs with work spread over all of them.
-  int run = blockIdx.x, per = 1, at = run, stop = total;
-  if (p.split) {
+  int run = blockIdx.x, per = 1, stop = total;
+  int at = OWN ? run * kWaves + wave : run;
+  if (split) {
     per = max((total + int(gridDim.x) - 1) / int(gridDim.x), 1);
     if (kRows > 16 && longest > 0) {
       // Whole sequences per run, where that costs at most a twentieth: the tiles
@@ -623,7 +639,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
     // and two gridDim larger.
     at = per * run;
     stop = min(at + per, total);
-    if (tid == 0) p.fold[run].parts = 0;
+    if (tid == 0) p.fold[2 * run].parts = p.fold[2 * run + 1].parts = 0;
   }
 
   State<D, NQ> st;
@@ -632,7 +648,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
   for (;;) {
     bool more = false;
     while (at < stop && !more) {
-      it = locate<kRows>(p, s_units, s_kept, at, stop);
+      it = locate<kRows, OWN>(p, s_units, s_kept, at, stop);
       at = it.end;
       more = it.u0 < it.u1;
     }
@@ -651,12 +667,12 @@ void cache_fwd_kernel(CacheFwdParams p) {
       h.page_bytes = int64_t{p.c.hkv} * p.c.block_bytes();
       h.base = p.data + int64_t{it.kvh} * p.c.block_bytes();
       lane_offsets<D>(&h, r, g);
-      kb = (p.split ? it.u0 << p.unit_log2 : 0) + wave * kStep;
-      piece_end = p.split ? min(int64_t{it.u1} << p.unit_log2,
-                                int64_t{it.local})
-                          : it.local;
+      kb = (split ? it.u0 << p.unit_log2 : 0) + (OWN ? 0 : wave * kStep);
+      piece_end = split ? min(int64_t{it.u1} << p.unit_log2,
+                              int64_t{it.local})
+                        : it.local;
       pg = load_pages<P16>(h, kb);
-      if (kQInLds<NQ>) lds_barrier();  // the last item's Q has been read
+      if (kQInLds<NQ> && !OWN) lds_barrier();  // the last item's Q has been read
       const int t = fresh_tid(), r = t & 15, g = (t & 63) >> 4, lane = t & 63;
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
@@ -672,7 +688,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
         for (int c = 0; c < D / 32; ++c) {
           if constexpr (!kQInLds<NQ>)
             st.q[q][c] = *reinterpret_cast<const bf16x8*>(src + 8 * c);
-          else if (q % kWaves == wave)
+          else if (OWN || q % kWaves == wave)
             s_q[(q * (D / 32) + c) * 64 + lane] =
                 *reinterpret_cast<const bf16x8*>(src + 8 * c);
         }
@@ -683,7 +699,30 @@ void cache_fwd_kernel(CacheFwdParams p) {
       }
     }
 
-    if (have_prev) {
+    if constexpr (OWN) if (have_prev) {
+      const int tid = fresh_tid(), r = tid & 15, g = (tid & 63) >> 4;
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        if (prev.rr0 + 16 * q >= prev.rr_end) break;
+        const float l = across_quarters(
+            st.l[q], [](float a, float b) { return a + b; });
+        const int rr = prev.rr0 + 16 * q + r;
+        if (rr < prev.rr_end) {
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            float acc[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              acc[i] = st.o[q][(8 * j + i) % (D / 16)][(8 * j + i) / (D / 16)];
+            store_row<D, OUT_F32>(
+                p, prev.first + rr / p.group, prev.kvh * p.group + rr % p.group,
+                g * (D / 4) + 8 * j, acc,
+                st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
+          }
+        }
+      }
+    }
+    if constexpr (!OWN) if (have_prev) {
       // Fold the waves, 16 rows at a time.
       const bool whole = prev.u0 == 0 && prev.u1 == prev.nu;
       const int slot = 2 * run + (prev.u0 == 0 ? 1 : 0);
@@ -764,7 +803,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
     }
     most_seen = __builtin_amdgcn_readfirstlane(most_seen);
     all_see = __builtin_amdgcn_readfirstlane(all_see);
-    if (kQInLds<NQ>) lds_barrier();
+    if (kQInLds<NQ> && !OWN) lds_barrier();
 
     // The next step's K is loaded into the registers of this one's as soon as
     // the first product has read them, its V after the second: each is in
@@ -772,7 +811,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
     const int kend = min(piece_end, most_seen);
     if (kb < kend) {
       for (;;) {
-        const int next = kb + kWaveKeys;
+        const int next = kb + (OWN ? kStep : kWaveKeys);
         const bool more_keys = next < kend;
         const StepPages pn = load_pages<P16>(h, next);
         // Q's LDS reads stay in the loop (its registers are needed).
@@ -797,53 +836,57 @@ void cache_fwd_kernel(CacheFwdParams p) {
       }
     }
 
-    if (p.split && it.u0 == 0 && it.u1 < it.nu && tid == 0) {
+    const bool goes_on = it.u0 > 0;  // then it is the run's first item
+    if (split && (goes_on || it.u1 < it.nu) && tid == 0) {
+      // The runs that the sequence's keys lie in; the rest of them fill runs
+      // from this one's start or, if they start here, after its end.
       CacheFold f;
       f.first = it.first;
       f.rr0 = it.rr0;
       f.rr_end = it.rr_end;
       f.kvh = it.kvh;
-      // Runs that the sequence's keys lie in: this one, which ends at `stop`
-      // after u1 of them, and those of the rest.
-      f.parts = min((it.nu - it.u1 + per - 1) / per,
-                    int(gridDim.x) - 1 - run) + 1;
-      p.fold[run] = f;
+      f.start = goes_on ? (per * run - it.u0) / per : run;
+      const int more_runs = goes_on ? (it.nu - it.u0 - 1) / per
+                                    : (it.nu - it.u1 + per - 1) / per;
+      f.parts = min(run + more_runs, int(gridDim.x) - 1) - f.start + 1;
+      p.fold[2 * run + (goes_on ? 0 : 1)] = f;
     }
     prev = it;
     have_prev = true;
   }
 }
 
-// Joins the partial results of the sequence that starts in run blockIdx.x and
-// goes on after it: slots 2 w + 1, 2 (w + 1), 2 (w + 2), .. in that order,
-// whatever order they were made in.  Eight dims per thread; a few pieces are
-// walked by one thread, many by kFoldParts threads, whose results are joined
-// through LDS.
-constexpr int kFoldThreads = 512, kFoldParts = 8;
+// Joins the partial results of the sequences that several runs hold: slots 2 w +
+// 1, 2 (w + 1), 2 (w + 2), .. of the one that starts in run w, in an order of
+// their own, whatever order they were made in.  The workgroups of its runs take
+// a slice of its rows each, down to one row; eight dims per thread, and as many
+// threads per row as there are take turns at the pieces and join through LDS.
+// Both launches, so / with one workgroup per sequence: 34 requests of 1 to 56K
+// tokens of one head 17/46 us, 2 of 51K 19/56 us.
+constexpr int kFoldThreads = 512;
 
 template <int D, int NQ, bool OUT_F32>
 __global__ __launch_bounds__(kFoldThreads)
 void cache_fold_kernel(CacheFwdParams p) {
   constexpr int kRows = 16 * NQ, kDimThreads = D / 8;
-  constexpr int kRowThreads = kFoldThreads / kDimThreads;
-  constexpr int kManyRows = kRowThreads / kFoldParts;
-  __shared__ float s_acc[kFoldParts][kManyRows][D];
-  __shared__ float s_m[kFoldParts][kManyRows], s_l[kFoldParts][kManyRows];
-  const int w = blockIdx.x;
-  const CacheFold f = load_const(p.fold, w);
-  if (f.parts < 2) return;
-  const int dim0 = threadIdx.x % kDimThreads * 8;
-  const int t = threadIdx.x / kDimThreads;
-  const bool many = f.parts > 4;
-  const int at_once = many ? kManyRows : kRowThreads;
-  const int pg = many ? t / kManyRows : 0;
-  const int step = many ? kFoldParts : 1;
-  const int my_row = many ? t % kManyRows : t;
-  for (int q0 = 0; q0 < kRows; q0 += at_once) {
-    if (f.rr0 + q0 >= f.rr_end) return;
-    const int row = q0 + my_row;
-    const int rr = f.rr0 + row;
-    const bool valid = row < kRows && rr < f.rr_end;
+  __shared__ float s_acc[kFoldThreads][9];  // [9]: apart in the LDS banks
+  __shared__ float s_m[kFoldThreads / kDimThreads];
+  __shared__ float s_l[kFoldThreads / kDimThreads];
+  const int run = blockIdx.x, tid = threadIdx.x;
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {
+    const CacheFold f = load_const(p.fold, 2 * run + which);
+    if (f.parts < 2) continue;
+    // Rows of a slice; more than one run, so they are half of all at most.
+    int n = kRows / 2;
+    while (n > 1 && kRows / n * 2 <= f.parts) n /= 2;
+    const int q0 = (run - f.start) * n;
+    if (q0 >= kRows || f.rr0 + q0 >= f.rr_end) continue;
+    const int dim0 = tid % kDimThreads * 8;
+    const int at = tid / kDimThreads, my = at % n, pg = at / n;
+    const int groups = kFoldThreads / (n * kDimThreads);  // a power of two
+    const int row = q0 + my, rr = f.rr0 + row;
+    const bool valid = rr < f.rr_end;
     float M = -INFINITY, L = 0.f, acc[8] = {};
     auto fold = [&](float m, float l, const float* x) {
       const float mn = fmaxf(M, m);
@@ -857,9 +900,9 @@ void cache_fold_kernel(CacheFwdParams p) {
     };
     if (valid)
 #pragma unroll 4
-      for (int i = pg; i < f.parts; i += step) {
-        const int64_t slot = i == 0 ? 2 * int64_t{w} + 1 : 2 * (int64_t{w} + i);
-        const int64_t pr = slot * kRows + row;
+      for (int i = pg; i < f.parts; i += groups) {
+        const int64_t w = f.start + i;
+        const int64_t pr = (i == 0 ? 2 * w + 1 : 2 * w) * kRows + row;
         float x[8];
         const f32x4* src =
             reinterpret_cast<const f32x4*>(p.part_o + pr * D + dim0);
@@ -871,26 +914,25 @@ void cache_fold_kernel(CacheFwdParams p) {
         }
         fold(p.part_ml[2 * pr], p.part_ml[2 * pr + 1], x);
       }
-    if (many) {
+    for (int half = groups / 2; half > 0; half /= 2) {
+      if (half >= f.parts) continue;
       __syncthreads();
+      if (pg >= half && pg < 2 * half) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s_acc[pg][my_row][dim0 + i] = acc[i];
-      if (dim0 == 0) {
-        s_m[pg][my_row] = M;
-        s_l[pg][my_row] = L;
+        for (int i = 0; i < 8; ++i) s_acc[tid][i] = acc[i];
+        s_m[at] = M;  // the same of all dims' threads
+        s_l[at] = L;
       }
       __syncthreads();
-      M = -INFINITY;
-      L = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-      for (int j = 0; j < kFoldParts; ++j)
-        fold(s_m[j][my_row], s_l[j][my_row], &s_acc[j][my_row][dim0]);
+      if (pg < half)
+        fold(s_m[at + half * n], s_l[at + half * n],
+             s_acc[tid + half * n * kDimThreads]);
     }
     if (pg == 0 && valid)
       store_row<D, OUT_F32>(p, f.first + rr / p.group,
                             f.kvh * p.group + rr % p.group, dim0, acc,
                             M == -INFINITY ? 0.f : M, L);
+    __syncthreads();
   }
 }
 
@@ -910,6 +952,7 @@ int resident_groups(int head_dim, int nq) {
 struct Shape {
   int nq;          // 16-row columns per tile
   bool split;
+  bool own;        // a wave's items are its own
   int grid, unit_log2, max_units, seq_units;
 };
 
@@ -924,6 +967,11 @@ int64_t keys_of(const CacheDims& c) {
   return int64_t{c.max_pages} << c.page_log2;
 }
 constexpr int64_t kBriefKeys = 512;
+
+// Workgroups of a launch of whole sequences per wave, of what fits at once: more
+// are dealt out as others end, each makes the plan.  4 x 4000 rows of 4 heads and
+// as many keys: 640 us with 2, 544 with 4 and with 8.
+constexpr int64_t kOwnGrid = 4;
 
 Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
                int64_t rows, bool out_f32) {
@@ -962,14 +1010,29 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   while (s.split && units_of() >= most && s.unit_log2 < 30) ++s.unit_log2;
   const int64_t units = units_of();
   s.max_units = static_cast<int>(units < most ? units : most - 1);
-  const int64_t grid = s.split ? slots : seqs;
+  // A wave each for whole sequences, where there are enough for all waves and
+  // the last round of them is nearly full: nothing is folded, and a wave's own
+  // overhead lies beside the others' work.  Microseconds so / a workgroup each,
+  // 8 KV heads:
+  //   106 x 444 rows of 16 heads    1543/3347   8 x 600 rows of 4 heads over 4096
+  //   16 x 600 of 4, float32 O       138/238    (2464 for 2048 waves)  411/333
+  //   1000 x 1 of 4, 1 to 500 keys    48/108    1 x 8000 of 9000       659/678
+  const int64_t waves = int64_t{kWaves} * slots;
+  const int64_t rounds = (seqs + waves - 1) / waves;
+  s.own = !s.split && seqs >= waves &&
+          (rounds > 2 || rounds * waves - seqs <= seqs / 4);
+  const int64_t own_groups = (seqs + kWaves - 1) / kWaves;
+  const int64_t grid = s.split ? slots
+                       : !s.own ? seqs
+                       : own_groups < kOwnGrid * slots ? own_groups
+                                                       : kOwnGrid * slots;
   s.grid = static_cast<int>(grid < 65536 ? grid : 65536);
   return s;
 }
 
-// Workspace of a split launch of `groups` workgroups: CacheFold of each, then the
+// Workspace of a split launch of `groups` workgroups: two CacheFold of each, then the
 // partial results: O, reference and sum of two tiles each.
-size_t fold_bytes(int groups) { return sizeof(CacheFold) * groups; }
+size_t fold_bytes(int groups) { return 2 * sizeof(CacheFold) * groups; }
 size_t part_rows(int groups, int nq) { return size_t{32} * nq * groups; }
 
 template <int D, int NQ, bool OUT_F32>
@@ -978,12 +1041,13 @@ hipError_t launch(const CacheFwdParams& p, const Shape& s, hipStream_t stream) {
   const size_t lds =
       (n + 1) * 4 + (n <= kKeptRequests ? n * sizeof(RequestRows) : 0);
   const dim3 grid(static_cast<unsigned>(s.grid));
-  if (p.c.page_log2 == 4)
-    hipLaunchKernelGGL((cache_fwd_kernel<D, NQ, OUT_F32, true>), grid, dim3(NT),
-                       lds, stream, p);
-  else
-    hipLaunchKernelGGL((cache_fwd_kernel<D, NQ, OUT_F32, false>), grid,
-                       dim3(NT), lds, stream, p);
+  const auto kernel =
+      p.c.page_log2 == 4
+          ? (s.own ? cache_fwd_kernel<D, NQ, OUT_F32, true, true>
+                   : cache_fwd_kernel<D, NQ, OUT_F32, true, false>)
+          : (s.own ? cache_fwd_kernel<D, NQ, OUT_F32, false, true>
+                   : cache_fwd_kernel<D, NQ, OUT_F32, false, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(NT), lds, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !s.split) return e;
   hipLaunchKernelGGL((cache_fold_kernel<D, NQ, OUT_F32>), grid,
