@@ -699,29 +699,6 @@ void cache_fwd_kernel(CacheFwdParams p) {
       }
     }
 
-    if constexpr (OWN) if (have_prev) {
-      const int tid = fresh_tid(), r = tid & 15, g = (tid & 63) >> 4;
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        if (prev.rr0 + 16 * q >= prev.rr_end) break;
-        const float l = across_quarters(
-            st.l[q], [](float a, float b) { return a + b; });
-        const int rr = prev.rr0 + 16 * q + r;
-        if (rr < prev.rr_end) {
-#pragma unroll
-          for (int j = 0; j < D / 32; ++j) {
-            float acc[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              acc[i] = st.o[q][(8 * j + i) % (D / 16)][(8 * j + i) / (D / 16)];
-            store_row<D, OUT_F32>(
-                p, prev.first + rr / p.group, prev.kvh * p.group + rr % p.group,
-                g * (D / 4) + 8 * j, acc,
-                st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
-          }
-        }
-      }
-    }
     if constexpr (!OWN) if (have_prev) {
       // Fold the waves, 16 rows at a time.
       const bool whole = prev.u0 == 0 && prev.u1 == prev.nu;
@@ -836,6 +813,30 @@ void cache_fwd_kernel(CacheFwdParams p) {
       }
     }
 
+    if constexpr (OWN) {
+      // Stored before the next item's loads, which then have its registers.
+      const int tid = fresh_tid(), r = tid & 15, g = (tid & 63) >> 4;
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        if (it.rr0 + 16 * q >= it.rr_end) break;
+        const float l = across_quarters(
+            st.l[q], [](float a, float b) { return a + b; });
+        const int rr = it.rr0 + 16 * q + r;
+        if (rr < it.rr_end) {
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) {
+            float acc[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              acc[i] = st.o[q][(8 * j + i) % (D / 16)][(8 * j + i) / (D / 16)];
+            store_row<D, OUT_F32>(
+                p, it.first + rr / p.group, it.kvh * p.group + rr % p.group,
+                g * (D / 4) + 8 * j, acc,
+                st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
+          }
+        }
+      }
+    }
     const bool goes_on = it.u0 > 0;  // then it is the run's first item
     if (split && (goes_on || it.u1 < it.nu) && tid == 0) {
       // The runs that the sequence's keys lie in; the rest of them fill runs
