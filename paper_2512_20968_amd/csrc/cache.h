@@ -96,6 +96,8 @@ struct CacheFwdParams {
   float* lse;
   int64_t rows;
   int32_t hq, group, num_requests;
+  uint32_t group_mul;   // token_head()
+  int32_t group_shift;
   float scale_log2, inv_scale_log2;
   int32_t split;      // whether sequences are cut
   int32_t unit_log2;  // keys of a unit

@@ -419,6 +419,18 @@ __device__ __forceinline__ void store_row(const CacheFwdParams& p, int64_t row,
   }
 }
 
+// The token and the head (of all query heads) of row rr of a KV head's rows;
+// group_mul / 2^group_shift is 1 / group, exact enough for rr < 2^30.
+struct TokenHead {
+  int tok, head;
+};
+__device__ __forceinline__ TokenHead token_head(const CacheFwdParams& p,
+                                                uint32_t rr, int kvh) {
+  const uint32_t tok = static_cast<uint32_t>(
+      (uint64_t{rr} * p.group_mul) >> p.group_shift);
+  return {int(tok), kvh * p.group + int(rr - tok * p.group)};
+}
+
 __device__ __forceinline__ int32_t stored_keys(const CacheFwdParams& p,
                                                int32_t len) {
   const int64_t most = int64_t{p.c.max_pages} << p.c.page_log2;
@@ -674,21 +686,23 @@ void cache_fwd_kernel(CacheFwdParams p) {
       pg = load_pages<P16>(h, kb);
       if (kQInLds<NQ> && !OWN) lds_barrier();  // the last item's Q has been read
       const int t = fresh_tid(), r = t & 15, g = (t & 63) >> 4, lane = t & 63;
+      bf16x8 staged[kQInLds<NQ> && OWN ? NQ : 1][D / 32];  // to LDS later
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         const int mine = it.rr0 + 16 * q + r;
         const uint32_t rr = mine < it.rr_end ? mine : it.rr0;
-        const uint32_t tok = rr / uint32_t(p.group);
-        const int64_t row = it.first + int64_t{tok};
-        const int head = it.kvh * p.group + int(rr - tok * p.group);
+        const TokenHead th = token_head(p, rr, it.kvh);
+        const int64_t row = int64_t{it.first} + th.tok;
         const uint16_t* src =
-            p.q + row * p.q_stride + int64_t{head} * D + g * (D / 4);
+            p.q + row * p.q_stride + int64_t{th.head} * D + g * (D / 4);
         pos[q] = p.positions[row];
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           if constexpr (!kQInLds<NQ>)
             st.q[q][c] = *reinterpret_cast<const bf16x8*>(src + 8 * c);
-          else if (OWN || q % kWaves == wave)
+          else if constexpr (OWN)
+            staged[q][c] = *reinterpret_cast<const bf16x8*>(src + 8 * c);
+          else if (q % kWaves == wave)
             s_q[(q * (D / 32) + c) * 64 + lane] =
                 *reinterpret_cast<const bf16x8*>(src + 8 * c);
         }
@@ -696,6 +710,13 @@ void cache_fwd_kernel(CacheFwdParams p) {
       if (kb < piece_end) {
         load_k<D, P16>(h, pg, kb, r, &s);
         load_v<D, P16>(h, pg, kb, g, &s);
+      }
+      if constexpr (kQInLds<NQ> && OWN) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c)
+            s_q[(q * (D / 32) + c) * 64 + lane] = staged[q][c];
       }
     }
 
@@ -740,8 +761,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
             for (int i = 0; i < 8; ++i) acc[i] += s_o[w][row16][dim0 + i] * sm;
           }
           if (whole) {
-            store_row<D, OUT_F32>(p, prev.first + rr / p.group,
-                                  prev.kvh * p.group + rr % p.group, dim0, acc,
+            const TokenHead th = token_head(p, rr, prev.kvh);
+            store_row<D, OUT_F32>(p, prev.first + th.tok, th.head, dim0, acc,
                                   ref, L);
           } else {
             const int64_t pr = int64_t{slot} * kRows + 16 * q + row16;
@@ -815,13 +836,14 @@ void cache_fwd_kernel(CacheFwdParams p) {
 
     if constexpr (OWN) {
       // Stored before the next item's loads, which then have its registers.
-      const int tid = fresh_tid(), r = tid & 15, g = (tid & 63) >> 4;
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
-        if (it.rr0 + 16 * q >= it.rr_end) break;
+        const int tid = fresh_tid(), r = tid & 15, g = (tid & 63) >> 4;
+        if (it.rr0 + 16 * q >= it.rr_end) continue;
         const float l = across_quarters(
             st.l[q], [](float a, float b) { return a + b; });
         const int rr = it.rr0 + 16 * q + r;
+        const TokenHead th = token_head(p, rr, it.kvh);
         if (rr < it.rr_end) {
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
@@ -830,8 +852,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
             for (int i = 0; i < 8; ++i)
               acc[i] = st.o[q][(8 * j + i) % (D / 16)][(8 * j + i) / (D / 16)];
             store_row<D, OUT_F32>(
-                p, it.first + rr / p.group, it.kvh * p.group + rr % p.group,
-                g * (D / 4) + 8 * j, acc,
+                p, it.first + th.tok, th.head, g * (D / 4) + 8 * j, acc,
                 st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
           }
         }
@@ -929,10 +950,11 @@ void cache_fold_kernel(CacheFwdParams p) {
         fold(s_m[at + half * n], s_l[at + half * n],
              s_acc[tid + half * n * kDimThreads]);
     }
-    if (pg == 0 && valid)
-      store_row<D, OUT_F32>(p, f.first + rr / p.group,
-                            f.kvh * p.group + rr % p.group, dim0, acc,
+    if (pg == 0 && valid) {
+      const TokenHead th = token_head(p, rr, f.kvh);
+      store_row<D, OUT_F32>(p, f.first + th.tok, th.head, dim0, acc,
                             M == -INFINITY ? 0.f : M, L);
+    }
     __syncthreads();
   }
 }
@@ -1092,6 +1114,11 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
   p.unit_log2 = s.unit_log2;
   p.seq_units = s.seq_units;
   p.max_units = s.max_units;
+  int log2 = 0;
+  while ((1 << log2) < p.group) ++log2;
+  p.group_shift = 30 + log2;
+  p.group_mul = static_cast<uint32_t>(
+      ((uint64_t{1} << p.group_shift) + p.group - 1) / p.group);
   p.fold = nullptr;
   p.part_o = p.part_ml = nullptr;
   if (s.split) {
