@@ -587,6 +587,43 @@ def test_many_heads_of_many_requests():
     test_many_requests(1300, 1, hkv=6)
 
 
+@pytest.mark.parametrize("d,group,new,dtype", [
+    (64, 3, 1, torch.float32), (128, 2, 1, torch.bfloat16),
+    (128, 5, 4, torch.float32), (128, 7, 6, torch.bfloat16),
+    (64, 4, 20, torch.bfloat16)])
+def test_a_sequence_of_hundreds_of_runs(d, group, new, dtype):
+    """Every run keeps a few hundred keys: no sum is longer than before."""
+    c = cache_of(head_dim=d, page_size=64, num_kv_heads=1, num_pages=700,
+                 max_pages=600)
+    b = Batch(c, [38000, 5, 3000], [new, 1, new], group=group, seed=18)
+    check(b.run(dtype), b.want(), d)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d,ps,b,group,new", [
+    (64, 16, 500, 1, 1), (128, 32, 500, 2, 1), (128, 16, 80, 4, 30),
+    (64, 64, 80, 4, 30), (128, 64, 70, 7, 33)])
+@pytest.mark.parametrize("share", SHARES[:2])
+def test_more_short_sequences_than_waves(d, ps, b, group, new, dtype, share):
+    """16 KV heads: a wave each for whole sequences, some of them empty."""
+    rng = np.random.default_rng(b + new)
+    c = cache_of(head_dim=d, page_size=ps, num_kv_heads=16, num_pages=3000,
+                 max_pages=512 // ps, **share)
+    lens = rng.integers(0, 90, b)
+    lens[rng.integers(b, size=3)] = 300
+    news = np.minimum(lens, rng.integers(1, new + 1, b) if new > 1 else 1)
+    news[::3] = np.minimum(lens[::3], new)
+    # What the rows are counted by on the host: padding makes them more.
+    x = Batch(c, lens.tolist(), news.tolist(), group=group, seed=17,
+              pad=b * new - int(news.sum()))
+    rows = len(x.positions)
+    x.positions[rng.integers(rows, size=9)] = -1
+    x.positions[rng.integers(rows, size=9)] = 7
+    x.table[5, 0] = -3
+    x.table[6, 0] = 3000
+    check(x.run(dtype), x.want(), d)
+
+
 @pytest.mark.parametrize("lens", [[2**31 - 1, 5], [192, 2**31 - 1]])
 def test_lengths_past_the_table(lens):
     for share in SHARES:
