@@ -460,7 +460,7 @@ ma_status_t mesh_attn_cache_tables(
     int32_t* cu_new, int64_t rows, int64_t* slots, int32_t* positions,
     int32_t* free_range_out, int32_t* refused, hipStream_t stream);
 
-/* Stores rows of K and V in 4 bits; rows < 2^30.
+/* Stores rows of K and V in 4 bits.
  *   k, v   row r, head h at k + r * k_stride + h * head_dim, bf16 device; the
  *          strides are in elements, multiples of 8, >= Hkv * d (slices of a
  *          fused projection's output).
@@ -480,7 +480,7 @@ ma_status_t mesh_attn_cache_append(const ma_cache_t* cache, int64_t rows,
                                    const int64_t* slots, void* data,
                                    hipStream_t stream);
 
-/* Reads rows (fewer than 2^30) back, exactly, as bf16 [rows][Hkv][d]: the KV buffer of
+/* Reads stored rows back, exactly, as bf16 [rows][Hkv][d]: the KV buffer of
  * the tile calls (a cached prefix under a new tile).  Rows whose slot is out of
  * range are 0. */
 ma_status_t mesh_attn_cache_read(const ma_cache_t* cache, int64_t rows,

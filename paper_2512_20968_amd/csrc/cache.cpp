@@ -80,16 +80,14 @@ ma_status_t check_cache(const ma_cache_t* c, CacheDims* out) {
   return MA_OK;
 }
 
-ma_status_t check_rows(int64_t rows, int log2 = 31) {
-  if (rows < 0 || rows >= int64_t{1} << log2)
-    return fail(MA_ERR_INVALID_ARG, "rows %lld outside [0, 2^%d)",
-                static_cast<long long>(rows), log2);
+constexpr int64_t kMaxRows = int64_t{1} << 31;
+
+ma_status_t check_rows(int64_t rows) {
+  if (rows < 0 || rows >= kMaxRows)
+    return fail(MA_ERR_INVALID_ARG, "rows %lld outside [0, 2^31)",
+                static_cast<long long>(rows));
   return MA_OK;
 }
-
-// Rows that append and read take: a launch counts its threads in 32 bits, and
-// a workgroup of 256 has 64 rows at least where there are many.
-constexpr int kStoreRowsLog2 = 30;
 
 ma_status_t check_requests(int32_t n) {
   if (n < 0 || n > MA_CACHE_MAX_REQUESTS)
@@ -196,7 +194,7 @@ ma_status_t mesh_attn_cache_append(const ma_cache_t* cache, int64_t rows,
                                    hipStream_t stream) {
   StoreParams p;
   MA_TRY(check_cache(cache, &p.c));
-  MA_TRY(check_rows(rows, kStoreRowsLog2));
+  MA_TRY(check_rows(rows));
   const int64_t width = int64_t{p.c.hkv} * p.c.d;
   MA_TRY(check_stride("k_stride", k_stride, width, 8));
   MA_TRY(check_stride("v_stride", v_stride, width, 8));
@@ -219,7 +217,7 @@ ma_status_t mesh_attn_cache_read(const ma_cache_t* cache, int64_t rows,
                                  void* k, void* v, hipStream_t stream) {
   LoadParams p;
   MA_TRY(check_cache(cache, &p.c));
-  MA_TRY(check_rows(rows, kStoreRowsLog2));
+  MA_TRY(check_rows(rows));
   if (rows == 0) return ok();
   const Arg args[] = {
       {"slots", slots, 8}, {"data", data, 16}, {"k", k, 16}, {"v", v, 16}};

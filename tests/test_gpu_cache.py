@@ -650,6 +650,26 @@ def test_tables_for_a_billion_tokens():
     check((o, lse), want, 64)
 
 
+def test_more_rows_than_a_launch_has_workgroups_in_a_row():
+    """2^26 rows and a few, sixteen to a workgroup: the last ones' grid."""
+    c = cache_of(head_dim=128, num_kv_heads=1)
+    rows, few = 2**26 + 21, 40
+    k = torch.empty(rows, 1, 128, dtype=torch.bfloat16, device="cuda")
+    slots = torch.full((rows,), -1, dtype=torch.int64, device="cuda")
+    k[-few:] = torch.randn(few, 1, 128, dtype=torch.bfloat16, device="cuda")
+    slots[-few:] = torch.arange(few, device="cuda") * 3
+    data, want = random_bytes(c), random_bytes(c)
+    ma.mesh_attn_cache_append(c, k, k, slots, data)
+    ma.mesh_attn_cache_append(c, k[-few:], k[-few:], slots[-few:], want)
+    assert torch.equal(data, want)
+    v = torch.empty_like(k)
+    ma.mesh_attn_cache_read(c, slots, data, k, v)
+    wk, wv = torch.empty_like(k[-few:]), torch.empty_like(k[-few:])
+    ma.mesh_attn_cache_read(c, slots[-few:], data, wk, wv)
+    assert torch.equal(k[-few:], wk) and torch.equal(v[-few:], wv)
+    assert not k[:-few].any() and not v[:-few].any()
+
+
 def test_far_rows():
     """Q and O past 2^31 elements: the last rows, over a few keys."""
     c = cache_of(head_dim=128, num_kv_heads=1, page_size=64, num_pages=4)

@@ -70,7 +70,7 @@ def _append(c=None, rows=4, k=A, ks=128, v=A, vs=128, slots=A, data=A):
 
 
 @pytest.mark.parametrize("kw,text", [
-    (dict(rows=-1), "rows"), (dict(rows=2**30), "rows"),
+    (dict(rows=-1), "rows"), (dict(rows=2**31), "rows"),
     (dict(k=None), "k is NULL"), (dict(v=None), "v is NULL"),
     (dict(slots=None), "slots is NULL"), (dict(data=None), "data is NULL"),
     (dict(k=A + 8), "k is not 16"), (dict(v=A + 2), "v is not 16"),
@@ -90,7 +90,7 @@ def test_read_refusals():
         assert _read(_cache(), args=args) == INVALID
         assert f"{name} is NULL" in ma.mesh_attn_last_error()
     assert _read(_cache(), rows=-1) == INVALID
-    assert _read(_cache(), rows=2**30) == INVALID
+    assert _read(_cache(), rows=2**31) == INVALID
 
 
 def test_nothing_to_do_is_accepted_without_buffers():
