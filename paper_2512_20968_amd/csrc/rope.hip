@@ -10,8 +10,8 @@
 // Streaming: every element is read and written once.  A workgroup takes a few
 // rows, makes each of their angles once, in LDS, and then walks over the 16-byte
 // units of their heads in the order in which they lie in memory, two units
-// per thread in flight.  16384 rows of 40 bf16 heads of 128 (336 MB): 64.9 us,
-// 5.2 TB/s, as a large copy; with the angles made by every thread that walks
+// per thread in flight.  16384 rows of 40 bf16 heads of 128 (336 MB): 63.7 us,
+// 5.3 TB/s, as a large copy; with the angles made by every thread that walks
 // over heads it took 72 to 79 us.
 
 #include <hip/hip_runtime.h>
