@@ -624,6 +624,23 @@ def test_more_short_sequences_than_waves(d, ps, b, group, new, dtype, share):
     check(x.run(dtype), x.want(), d)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_nan_in_a_short_sequence_of_many(dtype):
+    """Only the heads of its KV head, and for V its 32 dims, become NaN."""
+    c = cache_of(num_kv_heads=16, num_pages=1500, max_pages=32)
+    b = Batch(c, [30] * 500, [1] * 500, group=2, seed=19)
+    for request, head, what in ((3, 2, "k"), (9, 15, "v"), (499, 0, "k")):
+        at = request * 30 + 5
+        k, v = b.k[at:at + 1].cuda(), b.v[at:at + 1].cuda()
+        (k if what == "k" else v)[0, head, 40] = float("nan")
+        ma.mesh_attn_cache_append(c, k, v, i64(b.slots[at:at + 1]), b.data)
+    o, lse = (x.isnan().cpu() for x in b.run(dtype))
+    want = torch.zeros_like(o)
+    want[3, 4:6] = want[9, 30:32, 32:] = want[499, :2] = True
+    assert torch.equal(o, want)
+    assert torch.equal(lse.T, want.all(-1))
+
+
 @pytest.mark.parametrize("lens", [[2**31 - 1, 5], [192, 2**31 - 1]])
 def test_lengths_past_the_table(lens):
     for share in SHARES:
