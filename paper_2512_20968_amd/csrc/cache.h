@@ -99,7 +99,8 @@ struct CacheFwdParams {
   uint32_t group_mul;   // token_head()
   int32_t group_shift;
   float scale_log2, inv_scale_log2;
-  int32_t split;      // whether sequences are cut
+  int32_t split;      // whether sequences are cut, ..
+  int32_t may_stay_whole;  // .. unless their lengths speak against it
   int32_t unit_log2;  // keys of a unit
   int32_t seq_units;  // units that a sequence costs beside its keys
   int32_t max_units;  // most of a launch

@@ -456,7 +456,7 @@ __device__ __forceinline__ int32_t stored_keys(const CacheFwdParams& p,
 // fold) counts as seq_units units in front of them.  A sequence that lies in
 // several runs leaves partial results, two slots a workgroup at most: slot 2 w
 // for the piece that goes on from an earlier run, slot 2 w + 1 for the one that
-// starts in run w and goes on after it; cache_fold_kernel joins them.  p.split 0:
+// starts in run w and goes on after it; cache_fold_kernel joins them.  Not split:
 // every sequence is one unit, and no piece is split.
 constexpr int kWaveKeys = kWaves * kStep;  // keys of a step of each wave
 
@@ -480,15 +480,77 @@ __device__ __forceinline__ RequestRows load_request(const CacheFwdParams& p,
   return r;
 }
 
+// A request's sequences: tiles of each KV head, and units of each.
+struct Sequences {
+  int tiles, units;
+};
+
+template <int kRows>
+__device__ __forceinline__ Sequences sequences_of(const CacheFwdParams& p,
+                                                  const RequestRows& r,
+                                                  bool split) {
+  const uint32_t rr = uint32_t(r.end - r.first) * p.group;  // below 2^30
+  return {int((rr + kRows - 1) / kRows),
+          split ? max((r.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1)
+                : 1};
+}
+
+// Whether the sequences of a launch that may cut them are better left whole,
+// dealt out in turns: the cut gives every workgroup the same number of units, of
+// which those that come after a tile's last row are none, and costs kCutUnits
+// for the pieces of cut sequences and their fold; whole, the longest one and
+// `turns` mean ones bound it, a mean one without half of the new keys.  An
+// estimate: rows may see less or more than this.  Microseconds cut / whole, 8 KV
+// heads of 4:
+//   1 x 4000 of 4000 keys  244/157    2 x 1000 of 33000  1018/968
+//   1 x  900 of 2000        57/38     1 x 1100 of 20000   352/484
+//   1 x  130 of 2000        28/33     1 x  900 of 20000   294/300
+constexpr int kCutUnits = 10;
+
+struct Totals {
+  unsigned long long seqs, units, mean;
+  int longest;
+};
+
+template <int kRows>
+__device__ __forceinline__ bool whole_is_better(const CacheFwdParams& p,
+                                                Totals* s_totals) {
+  if (threadIdx.x == 0) *s_totals = Totals{0, 0, 0, 0};
+  __syncthreads();
+  for (int b = threadIdx.x; b < p.num_requests; b += NT) {
+    const RequestRows r = load_request(p, b);
+    const Sequences q = sequences_of<kRows>(p, r, true);
+    if (q.tiles == 0) continue;
+    const int64_t n = int64_t{q.tiles} * p.c.hkv;
+    const int all = q.units + p.seq_units;
+    // The keys of the new rows, if they are the request's last positions.
+    const int fresh =
+        r.local - stored_keys(p, max(p.lens[b], 0) - (r.end - r.first));
+    const int mean = all - min(fresh >> (p.unit_log2 + 1), all - 1);
+    atomicAdd(&s_totals->seqs, static_cast<unsigned long long>(n));
+    atomicAdd(&s_totals->units, static_cast<unsigned long long>(n * all));
+    atomicAdd(&s_totals->mean, static_cast<unsigned long long>(n * mean));
+    atomicMax(&s_totals->longest, all);
+  }
+  __syncthreads();
+  const uint64_t n = s_totals->seqs, grid = gridDim.x;
+  const uint64_t cut = s_totals->units / grid + kCutUnits;
+  const uint64_t turns = (n + grid - 1) / grid;
+  return uint64_t(s_totals->longest) <= cut &&
+         turns * s_totals->mean <= cut * n;
+}
+
 // First units of the requests in LDS, by prefix sums over the workgroup; the
 // sums are capped at max_units, which rows that do not overlap cannot pass.
 // Returns the number of units; *longest is the longest sequence of a request
 // with several tiles (0: there is none).
 template <int kRows>
-__device__ __forceinline__ int plan_units(const CacheFwdParams& p, int* s_units,
-                                          RequestRows* s_kept, int* s_wave,
-                                          int* s_longest, int* longest) {
+__device__ __forceinline__ int plan_units(const CacheFwdParams& p, bool split,
+                                          int* s_units, RequestRows* s_kept,
+                                          int* s_wave, int* s_longest,
+                                          int* longest) {
   const int B = p.num_requests, tid = threadIdx.x, lane = tid & 63;
+  const int cost = split ? p.seq_units : 0;
   int base = 0;
   if (tid == 0) *s_longest = 0;
   __syncthreads();
@@ -498,14 +560,10 @@ __device__ __forceinline__ int plan_units(const CacheFwdParams& p, int* s_units,
     if (b < B) {
       const RequestRows r = load_request(p, b);
       if (B <= kKeptRequests) s_kept[b] = r;
-      const uint32_t rr = uint32_t(r.end - r.first) * p.group;  // below 2^30
-      const uint32_t tiles = (rr + kRows - 1) / kRows;
-      const int nu =
-          p.split ? max((r.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1)
-                  : 1;
-      const int64_t n = int64_t{tiles} * (nu + p.seq_units) * p.c.hkv;
+      const Sequences q = sequences_of<kRows>(p, r, split);
+      const int64_t n = int64_t{q.tiles} * (q.units + cost) * p.c.hkv;
       mine = static_cast<int>(n < p.max_units ? n : p.max_units);
-      if (kRows > 16 && tiles > 1) atomicMax(s_longest, nu + p.seq_units);
+      if (kRows > 16 && q.tiles > 1) atomicMax(s_longest, q.units + cost);
     }
     int y = mine;
 #pragma unroll
@@ -556,11 +614,10 @@ struct Item {
 
 // The item at unit `at` of a run that ends at `stop`.
 template <int kRows, bool OWN>
-__device__ __forceinline__ Item locate(const CacheFwdParams& p,
+__device__ __forceinline__ Item locate(const CacheFwdParams& p, bool split,
                                        const int* s_units,
                                        const RequestRows* s_kept, int at,
                                        int stop) {
-  const bool split = !OWN && p.split;
   const int B = p.num_requests, hkv = p.c.hkv;
   int lo = 0, hi = B;
   while (hi - lo > 1) {
@@ -580,12 +637,11 @@ __device__ __forceinline__ Item locate(const CacheFwdParams& p,
   it.nu =
       split ? max((it.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1) : 1;
   const int off = at - __builtin_amdgcn_readfirstlane(s_units[it.b]);
-  const int len = it.nu + p.seq_units, seq = off / len;
+  const int len = split ? it.nu + p.seq_units : 1, seq = off / len;
   const int v0 = off - seq * len;  // of the sequence's units with its cost
-  it.u0 = max(v0 - p.seq_units, 0);
+  it.u0 = split ? max(v0 - p.seq_units, 0) : 0;
   it.u1 = split ? min(v0 + (stop - at) - p.seq_units, it.nu) : 1;
-  it.end = split ? min(at - v0 + len, stop)
-                 : at + int(gridDim.x) * (OWN ? kWaves : 1);
+  it.end = min(at - v0 + len, stop);
   const int tiles = (it.rr_end + kRows - 1) / kRows;
   int tile;
   if (OWN) {
@@ -603,8 +659,9 @@ __device__ __forceinline__ Item locate(const CacheFwdParams& p,
   } else {
     // Workgroup i runs on XCD i % 8: with a multiple of 8 heads, a head's keys
     // are read through one L2.
-    tile = seq / hkv;
-    it.kvh = seq - tile * hkv;
+    const int from_last = seq / hkv;
+    it.kvh = seq - from_last * hkv;
+    tile = tiles - 1 - from_last;
   }
   it.rr0 = tile * kRows;
   return it;
@@ -629,23 +686,36 @@ void cache_fwd_kernel(CacheFwdParams p) {
   RequestRows* s_kept =
       reinterpret_cast<RequestRows*>(s_units + p.num_requests + 1);
   bf16x8* s_q = s_q_all + (OWN && kQInLds<NQ> ? wave * kQ : 0);
-  const bool split = !OWN && p.split;
+  bool split = !OWN && p.split;
+  if constexpr (kRows > 16 && !OWN) {
+    __shared__ Totals s_totals;
+    if (split && p.may_stay_whole)
+      split = !__builtin_amdgcn_readfirstlane(
+          whole_is_better<kRows>(p, &s_totals));
+  }
 
   int longest;
   const int total = __builtin_amdgcn_readfirstlane(
-      plan_units<kRows>(p, s_units, s_kept, s_wave, &s_longest, &longest));
+      plan_units<kRows>(p, split, s_units, s_kept, s_wave, &s_longest,
+                        &longest));
   // Split: this workgroup's run.  Workgroup i runs on XCD i % 8; neighbouring
   // runs go to one XCD (the grid is a multiple of 8), whose L2 then serves the
   // tiles of a head, and the runs with work spread over all of them.
   int run = blockIdx.x, per = 1, stop = total;
   int at = OWN ? run * kWaves + wave : run;
+  // Whole sequences: to the workgroup's next one; where tiles differ, there and
+  // back again, so that those with the longer ones of one turn have the shorter
+  // ones of the next.
+  constexpr bool kBack = kRows > 16 && !OWN;
+  int hop = kBack ? 2 * int(gridDim.x - 1 - run) + 1
+                  : int(gridDim.x) * (OWN ? kWaves : 1);
   if (split) {
     per = max((total + int(gridDim.x) - 1) / int(gridDim.x), 1);
     if (kRows > 16 && longest > 0) {
       // Whole sequences per run, where that costs at most a twentieth: the tiles
       // of a head then walk over the keys side by side, and find them in their
-      // L2.  1000 rows of 4 heads a request over 33K tokens: 30 million misses
-      // and 1103 us without, 2 million and 1037 us with.
+      // L2.  1000 rows of 4 heads a request over 33K tokens, when cut: 30 million
+      // misses and 1103 us without, 2 million and 1037 us with.
       longest = __builtin_amdgcn_readfirstlane(longest);
       const int whole = (per + longest - 1) / longest * longest;
       if (whole - per <= per / 20) per = whole;
@@ -660,8 +730,9 @@ void cache_fwd_kernel(CacheFwdParams p) {
     // and two gridDim larger.
     at = per * run;
     stop = min(at + per, total);
-    if (tid == 0) p.fold[2 * run].parts = p.fold[2 * run + 1].parts = 0;
   }
+  if (!OWN && p.split && tid == 0)
+    p.fold[2 * run].parts = p.fold[2 * run + 1].parts = 0;
 
   State<D, NQ> st;
   Item it, prev;
@@ -669,8 +740,13 @@ void cache_fwd_kernel(CacheFwdParams p) {
   for (;;) {
     bool more = false;
     while (at < stop && !more) {
-      it = locate<kRows, OWN>(p, s_units, s_kept, at, stop);
-      at = it.end;
+      it = locate<kRows, OWN>(p, split, s_units, s_kept, at, stop);
+      if (split) {
+        at = it.end;
+      } else {
+        at += hop;
+        if (kBack) hop = 2 * int(gridDim.x) - hop;
+      }
       more = it.u0 < it.u1;
     }
     Keys h;
@@ -984,6 +1060,7 @@ int resident_groups(int head_dim, int nq) {
 struct Shape {
   int nq;          // 16-row columns per tile
   bool split;
+  bool may_stay_whole;  // the device looks at the lengths
   bool own;        // a wave's items are its own
   int grid, unit_log2, max_units, seq_units;
 };
@@ -1002,7 +1079,8 @@ constexpr int64_t kBriefKeys = 512;
 
 // Workgroups of a launch of whole sequences per wave, of what fits at once: more
 // are dealt out as others end, each makes the plan.  4 x 4000 rows of 4 heads and
-// as many keys: 640 us with 2, 544 with 4 and with 8.
+// as many keys: 633 us with 2, 527 with 4 and with 8; 106 x 444 of 16: 1257, 1276
+// and 1296.
 constexpr int64_t kOwnGrid = 4;
 
 Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
@@ -1025,17 +1103,20 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   //   1 of 2048               10.4/16.4  32 of 1..1024 13.5/11.4
   const bool brief = keys <= kBriefKeys || (keys <= 1024 && seqs >= 256);
   // Where there are several sequences per workgroup anyway, those of more tiles
-  // than one stay whole, for their L2's sake; those of one tile are cut, since
-  // their lengths may differ.  Microseconds cut / whole, 8 KV heads of 4:
-  //   8 x 2000 rows of 2000 tokens 597/428   512 x 1 of 1 to 32K  343/446
-  //   1 x 8000 rows of 9000        992/678   1024 x 1 of 1 to 64K 1108/1499
+  // than one stay whole, for their L2's sake and since tiles differ in what they
+  // see; with fewer, the device looks at the lengths (whole_is_better).  Those of
+  // one tile are cut, since their lengths may differ.  Microseconds cut / whole, 8
+  // KV heads of 4:
+  //   8 x 2000 rows of 2000 tokens 587/324   512 x 1 of 1 to 32K  343/446
+  //   1 x 8000 rows of 9000        998/644   1024 x 1 of 1 to 64K 1108/1499
   const bool one_tile = each <= 16 * s.nq && seqs < (1 << 24);
   s.split = !brief && (seqs < 4 * slots || one_tile);
   s.unit_log2 = 7;
   static_assert(kWaveKeys == 1 << 7, "least unit");
   // Units are counted in 32 bits.
   const int64_t most = int64_t{1} << 30;
-  s.seq_units = s.split ? kSeqUnits : 0;
+  s.seq_units = kSeqUnits;
+  s.may_stay_whole = s.split && !one_tile;
   auto units_of = [&] {
     return s.split ? seqs * ((keys >> s.unit_log2) + 1 + s.seq_units) : seqs;
   };
@@ -1046,9 +1127,9 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   // the last round of them is nearly full: nothing is folded, and a wave's own
   // overhead lies beside the others' work.  Microseconds so / a workgroup each,
   // 8 KV heads:
-  //   106 x 444 rows of 16 heads    1543/3347   8 x 600 rows of 4 heads over 4096
-  //   16 x 600 of 4, float32 O       138/238    (2464 for 2048 waves)  411/333
-  //   1000 x 1 of 4, 1 to 500 keys    48/108    1 x 8000 of 9000       659/678
+  //   106 x 444 rows of 16 heads    1276/3145   8 x 600 rows of 4 heads over 4096
+  //   16 x 600 of 4, float32 O       135/237    (2464 for 2048 waves)  411/329
+  //   1000 x 1 of 4, 1 to 500 keys    47/107    8 x 2000 of 2000       331/419
   const int64_t waves = int64_t{kWaves} * slots;
   const int64_t rounds = (seqs + waves - 1) / waves;
   s.own = !s.split && seqs >= waves &&
@@ -1122,6 +1203,7 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
   p.split = s.split;
   p.unit_log2 = s.unit_log2;
   p.seq_units = s.seq_units;
+  p.may_stay_whole = s.may_stay_whole;
   p.max_units = s.max_units;
   int log2 = 0;
   while ((1 << log2) < p.group) ++log2;

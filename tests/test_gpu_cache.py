@@ -276,8 +276,9 @@ class Batch:
             self.data, o, lse, ws=ws, stream=stream)
         return o, lse
 
-    def want(self):
-        """As oracle.cache.attention, of all keys of a request at once."""
+    def want(self, heads=None):
+        """As oracle.cache.attention, of all keys of a request at once; of some
+        heads."""
         c = self.c
         rows, hq, d = self.q.shape
         hkv, ps = c["num_kv_heads"], c["page_size"]
@@ -302,7 +303,7 @@ class Batch:
             k, v = k.double().cpu().numpy(), v.double().cpu().numpy()
             sees = ok[None] & (oc.key_positions(c, n)[None]
                                <= self.positions[lo:hi, None])
-            for h in range(hq):
+            for h in range(hq) if heads is None else heads:
                 kh, vh = k[:, h // group], v[:, h // group]
                 x = self.scale * (q[lo:hi, h] @ kh.T)
                 x[~sees] = -np.inf
@@ -321,6 +322,9 @@ class Batch:
                 reach[h, lo:hi] = [
                     self.scale * (np.abs(kh[m]) @ np.abs(qq)).max(initial=0.0)
                     for qq, m in zip(q[lo:hi, h], sees)]
+        if heads is not None:
+            o, lse, mass, reach = o[:, heads], lse[heads], mass[:, heads], \
+                reach[heads]
         return o, lse, mass, reach
 
 
@@ -622,6 +626,28 @@ def test_more_short_sequences_than_waves(d, ps, b, group, new, dtype, share):
     x.table[5, 0] = -3
     x.table[6, 0] = 3000
     check(x.run(dtype), x.want(), d)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,new,share", [
+    ([1400], [1350], SHARES[0]), ([1200, 700, 90], [1100, 600, 1], SHARES[0]),
+    ([3900], [1300], SHARES[1]), ([30000, 300], [300, 280], SHARES[2])])
+def test_prompts_of_more_tiles_than_workgroups(d, dtype, lens, new, share):
+    """Whether sequences are cut is the kernel's choice, by lengths and rows; rows
+    that see more or less than that supposes are as right."""
+    c = cache_of(head_dim=d, page_size=64, num_kv_heads=16, num_pages=200,
+                 max_pages=100, **share)
+    b = Batch(c, lens, new, group=2, seed=20)
+    heads = [1, 12, 31]
+    o, lse = b.run(dtype)
+    check((o[:, heads], lse[heads]), b.want(heads), d)
+    rng = np.random.default_rng(20)
+    b.positions = np.where(np.arange(len(b.positions)) % 3 == 0,
+                           rng.integers(-1, max(lens), len(b.positions)),
+                           max(lens) - 1)
+    o, lse = b.run(dtype)
+    check((o[:, heads], lse[heads]), b.want(heads), d)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
