@@ -99,6 +99,7 @@ struct CacheFwdParams {
   uint32_t group_mul;   // token_head()
   int32_t group_shift;
   float scale_log2, inv_scale_log2;
+  int32_t least_keys, most_keys;  // stored keys of the launch's requests
   int32_t split;      // whether sequences are cut, ..
   int32_t may_stay_whole;  // .. unless their lengths speak against it
   int32_t unit_log2;  // keys of a unit

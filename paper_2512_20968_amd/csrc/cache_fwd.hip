@@ -480,7 +480,8 @@ __device__ __forceinline__ RequestRows load_request(const CacheFwdParams& p,
   return r;
 }
 
-// A request's sequences: tiles of each KV head, and units of each.
+// A request's sequences: tiles of each KV head (none of a request that is another
+// launch's), and units of each.
 struct Sequences {
   int tiles, units;
 };
@@ -490,7 +491,8 @@ __device__ __forceinline__ Sequences sequences_of(const CacheFwdParams& p,
                                                   const RequestRows& r,
                                                   bool split) {
   const uint32_t rr = uint32_t(r.end - r.first) * p.group;  // below 2^30
-  return {int((rr + kRows - 1) / kRows),
+  const bool mine = r.local >= p.least_keys && r.local <= p.most_keys;
+  return {mine ? int((rr + kRows - 1) / kRows) : 0,
           split ? max((r.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1)
                 : 1};
 }
@@ -1056,13 +1058,14 @@ int resident_groups(int head_dim, int nq) {
                           : kWavesPerSimd<128, 4>);
 }
 
-// How a call is launched, from its sizes alone.
+// How a call is launched, from its sizes alone: requests of up to own_keys stored
+// keys with a wave for every sequence (-1: none), the others cut, or, without
+// `cut`, with a workgroup for every sequence.
 struct Shape {
-  int nq;          // 16-row columns per tile
-  bool split;
-  bool may_stay_whole;  // the device looks at the lengths
-  bool own;        // a wave's items are its own
-  int grid, unit_log2, max_units, seq_units;
+  int nq;  // 16-row columns per tile
+  bool cut, may_stay_whole;  // .. where the device finds it better
+  int own_keys, own_grid, whole_grid, cut_grid;
+  int unit_log2, max_units;
 };
 
 // Units that a sequence counts beside its keys.  128 requests of 1 to 16384
@@ -1102,27 +1105,7 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   //   1 of 1024               10.0/11.6  64 of 1024   22.0/17.3
   //   1 of 2048               10.4/16.4  32 of 1..1024 13.5/11.4
   const bool brief = keys <= kBriefKeys || (keys <= 1024 && seqs >= 256);
-  // Where there are several sequences per workgroup anyway, those of more tiles
-  // than one stay whole, for their L2's sake and since tiles differ in what they
-  // see; with fewer, the device looks at the lengths (whole_is_better).  Those of
-  // one tile are cut, since their lengths may differ.  Microseconds cut / whole, 8
-  // KV heads of 4:
-  //   8 x 2000 rows of 2000 tokens 587/324   512 x 1 of 1 to 32K  343/446
-  //   1 x 8000 rows of 9000        998/644   1024 x 1 of 1 to 64K 1108/1499
-  const bool one_tile = each <= 16 * s.nq && seqs < (1 << 24);
-  s.split = !brief && (seqs < 4 * slots || one_tile);
-  s.unit_log2 = 7;
-  static_assert(kWaveKeys == 1 << 7, "least unit");
-  // Units are counted in 32 bits.
-  const int64_t most = int64_t{1} << 30;
-  s.seq_units = kSeqUnits;
-  s.may_stay_whole = s.split && !one_tile;
-  auto units_of = [&] {
-    return s.split ? seqs * ((keys >> s.unit_log2) + 1 + s.seq_units) : seqs;
-  };
-  while (s.split && units_of() >= most && s.unit_log2 < 30) ++s.unit_log2;
-  const int64_t units = units_of();
-  s.max_units = static_cast<int>(units < most ? units : most - 1);
+  const bool one_tile = each <= 16 * s.nq;
   // A wave each for whole sequences, where there are enough for all waves and
   // the last round of them is nearly full: nothing is folded, and a wave's own
   // overhead lies beside the others' work.  Microseconds so / a workgroup each,
@@ -1130,40 +1113,78 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   //   106 x 444 rows of 16 heads    1276/3145   8 x 600 rows of 4 heads over 4096
   //   16 x 600 of 4, float32 O       135/237    (2464 for 2048 waves)  411/329
   //   1000 x 1 of 4, 1 to 500 keys    47/107    8 x 2000 of 2000       331/419
+  // Requests with far more keys than rows are not among them (nor are those of one
+  // tile): a few of them would be a few waves' work, long after the others.
   const int64_t waves = int64_t{kWaves} * slots;
   const int64_t rounds = (seqs + waves - 1) / waves;
-  s.own = !s.split && seqs >= waves &&
-          (rounds > 2 || rounds * waves - seqs <= seqs / 4);
+  const bool own = (brief || !one_tile) && seqs >= waves &&
+                   (rounds > 2 || rounds * waves - seqs <= seqs / 4);
+  const int64_t tokens = (rows + num_requests - 1) / num_requests;
+  const int64_t limit = tokens < 1024 ? 2048 : 2 * tokens;
+  s.own_keys = !own ? -1
+                    : static_cast<int>(brief || limit > keys ? keys : limit);
+  // The others, unless tables are short, are cut, or left whole by workgroups
+  // where the lengths speak for it (whole_is_better; never those of one tile,
+  // since only their lengths differ: 512 requests of 1 to 32K tokens, one row of 4
+  // heads, 343 us cut, 446 whole).
+  s.cut = !brief && s.own_keys < keys;
+  s.may_stay_whole = !one_tile;
+  s.unit_log2 = 7;
+  static_assert(kWaveKeys == 1 << 7, "least unit");
+  // Units are counted in 32 bits.  (There are fewer than 2^27 sequences.)
+  const int64_t most = int64_t{1} << 30;
+  auto units_of = [&] {
+    return seqs * ((keys >> s.unit_log2) + 1 + kSeqUnits);
+  };
+  while (units_of() >= most && s.unit_log2 < 30) ++s.unit_log2;
+  s.max_units = static_cast<int>(units_of());
   const int64_t own_groups = (seqs + kWaves - 1) / kWaves;
-  const int64_t grid = s.split ? slots
-                       : !s.own ? seqs
-                       : own_groups < kOwnGrid * slots ? own_groups
-                                                       : kOwnGrid * slots;
-  s.grid = static_cast<int>(grid < 65536 ? grid : 65536);
+  s.own_grid = static_cast<int>(own_groups < kOwnGrid * slots
+                                    ? own_groups
+                                    : kOwnGrid * slots);
+  s.whole_grid = static_cast<int>(seqs < 65536 ? seqs : 65536);
+  s.cut_grid = slots;
   return s;
 }
 
-// Workspace of a split launch of `groups` workgroups: two CacheFold of each, then the
+// Workspace of a cut launch of `groups` workgroups: two CacheFold of each, then the
 // partial results: O, reference and sum of two tiles each.
 size_t fold_bytes(int groups) { return 2 * sizeof(CacheFold) * groups; }
 size_t part_rows(int groups, int nq) { return size_t{32} * nq * groups; }
 
-template <int D, int NQ, bool OUT_F32>
-hipError_t launch(const CacheFwdParams& p, const Shape& s, hipStream_t stream) {
+template <int D, int NQ, bool OUT_F32, bool OWN>
+hipError_t launch_fwd(const CacheFwdParams& p, int groups, hipStream_t stream) {
   const size_t n = static_cast<size_t>(p.num_requests);
   const size_t lds =
       (n + 1) * 4 + (n <= kKeptRequests ? n * sizeof(RequestRows) : 0);
-  const dim3 grid(static_cast<unsigned>(s.grid));
-  const auto kernel =
-      p.c.page_log2 == 4
-          ? (s.own ? cache_fwd_kernel<D, NQ, OUT_F32, true, true>
-                   : cache_fwd_kernel<D, NQ, OUT_F32, true, false>)
-          : (s.own ? cache_fwd_kernel<D, NQ, OUT_F32, false, true>
-                   : cache_fwd_kernel<D, NQ, OUT_F32, false, false>);
-  hipLaunchKernelGGL(kernel, grid, dim3(NT), lds, stream, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !s.split) return e;
-  hipLaunchKernelGGL((cache_fold_kernel<D, NQ, OUT_F32>), grid,
+  const auto kernel = p.c.page_log2 == 4
+                          ? cache_fwd_kernel<D, NQ, OUT_F32, true, OWN>
+                          : cache_fwd_kernel<D, NQ, OUT_F32, false, OWN>;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(groups)), dim3(NT), lds,
+                     stream, p);
+  return hipGetLastError();
+}
+
+template <int D, int NQ, bool OUT_F32>
+hipError_t launch(CacheFwdParams p, const Shape& s, hipStream_t stream) {
+  hipError_t e = hipSuccess;
+  p.split = 0;
+  p.least_keys = 0;
+  p.most_keys = INT32_MAX;
+  if (s.own_keys >= 0) {
+    if (s.cut) p.most_keys = s.own_keys;
+    e = launch_fwd<D, NQ, OUT_F32, true>(p, s.own_grid, stream);
+    if (e != hipSuccess || !s.cut) return e;
+    p.least_keys = s.own_keys + 1;
+    p.most_keys = INT32_MAX;
+  }
+  if (!s.cut)
+    return launch_fwd<D, NQ, OUT_F32, false>(p, s.whole_grid, stream);
+  p.split = 1;
+  e = launch_fwd<D, NQ, OUT_F32, false>(p, s.cut_grid, stream);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((cache_fold_kernel<D, NQ, OUT_F32>),
+                     dim3(static_cast<unsigned>(s.cut_grid)),
                      dim3(kFoldThreads), 0, stream, p);
   return hipGetLastError();
 }
@@ -1200,9 +1221,8 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
   const Shape s = shape_of(params.c, params.hq, params.num_requests,
                            params.rows, out_f32);
   CacheFwdParams p = params;
-  p.split = s.split;
   p.unit_log2 = s.unit_log2;
-  p.seq_units = s.seq_units;
+  p.seq_units = kSeqUnits;
   p.may_stay_whole = s.may_stay_whole;
   p.max_units = s.max_units;
   int log2 = 0;
@@ -1212,11 +1232,11 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
       ((uint64_t{1} << p.group_shift) + p.group - 1) / p.group);
   p.fold = nullptr;
   p.part_o = p.part_ml = nullptr;
-  if (s.split) {
+  if (s.cut) {
     p.fold = static_cast<CacheFold*>(ws);
-    p.part_o =
-        reinterpret_cast<float*>(static_cast<char*>(ws) + fold_bytes(s.grid));
-    p.part_ml = p.part_o + part_rows(s.grid, s.nq) * p.c.d;
+    p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) +
+                                        fold_bytes(s.cut_grid));
+    p.part_ml = p.part_o + part_rows(s.cut_grid, s.nq) * p.c.d;
   }
   return p.c.d == 128 ? launch_d<128>(p, s, out_f32, stream)
                       : launch_d<64>(p, s, out_f32, stream);

@@ -651,6 +651,25 @@ def test_prompts_of_more_tiles_than_workgroups(d, dtype, lens, new, share):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d,ps,group,long", [
+    (64, 64, 4, [2048, 2049, 3900]), (128, 16, 4, [3000] * 5),
+    (128, 64, 7, []), (64, 16, 5, [4096, 0, 4095])])
+def test_short_and_long_sequences_of_many_tiles(d, ps, group, long, dtype):
+    """Enough for all waves; those with more than 2048 keys are another launch's."""
+    rng = np.random.default_rng(len(long))
+    c = cache_of(head_dim=d, page_size=ps, num_kv_heads=16,
+                 num_pages=30000 // ps, max_pages=4096 // ps)
+    lens = rng.integers(0, 120, 80)
+    lens[rng.permutation(80)[:len(long)]] = long
+    new = np.minimum(lens, rng.integers(20, 31, 80))
+    x = Batch(c, lens.tolist(), new.tolist(), group=group, seed=21,
+              pad=80 * 30 - int(new.sum()))
+    heads = [0, 16 * group // 2, 16 * group - 1]
+    o, lse = x.run(dtype)
+    check((o[:, heads], lse[heads]), x.want(heads), d)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_nan_in_a_short_sequence_of_many(dtype):
     """Only the heads of its KV head, and for V its 32 dims, become NaN."""
     c = cache_of(num_kv_heads=16, num_pages=1500, max_pages=32)
