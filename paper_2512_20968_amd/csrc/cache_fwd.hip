@@ -7,12 +7,13 @@
 // group) rows.  The four waves of a workgroup take every fourth step of 32 keys
 // with accumulators of their own and fold them at the end, so that every stored
 // byte is loaded and converted once per item, whatever the number of rows.  Where
-// there are more sequences than waves, a wave takes items of its own.
+// there are more sequences than waves, and no long ones, a wave takes items of its
+// own.
 //
 // Measured, 8 KV heads of 4 query heads, head dim 128: four requests' shares of 1M
 // tokens, one row each and float32 O, 211 us for 1.14 GB, 5.4 TB/s, bound by HBM;
 // 128 requests of 1 to 16K tokens 55 us for 0.23 GB, 4.2 TB/s, by the round trips
-// at the ends of 1024 sequences; 2 x 1000 rows over 33K tokens 1030 us, 1.03
+// at the ends of 1024 sequences; 2 x 1000 rows over 33K tokens 1016 us, 1.04
 // PFLOP/s, by the instructions of a step of 64 rows and 32 keys: 64 matrix
 // instructions of 16 cycles, 270 vector ones (32 exponentials, 64 conversions) of
 // 4.5, or 9 while another wave's matrix instruction runs, 2400 cycles in all.
