@@ -511,12 +511,12 @@ size_t mesh_attn_cache_fwd_workspace_size(const ma_cache_t* cache,
  *              exactly later).
  *   lse        [Hq][rows] float32 device, natural log; -inf for a row that
  *              sees no key, whose O row is 0.
- * Requests may share pages.  Rows of no request are left as they were.  O and LSE are those of
- * mesh_attn_tile_fwd over the stored values: exact products, float32
- * accumulation and softmax; the probabilities enter the second product in bf16
- * for a bf16 O, and as a sum of three bf16 for a float32 O.  A NaN key or value
- * reaches the rows that see it and no other.  A split of the keys over
- * workgroups depends on the sizes and lengths alone: equal calls give equal
+ * Requests may share pages.  Rows of no request are left as they were.  O and
+ * LSE are those of mesh_attn_tile_fwd over the stored values: exact products,
+ * float32 accumulation and softmax; the probabilities enter the second product
+ * in bf16 for a bf16 O, and as a sum of three bf16 for a float32 O.  A NaN key
+ * or value reaches the rows that see it and no other.  How the keys are split
+ * over workgroups depends on the sizes and lengths alone: equal calls give equal
  * bits. */
 ma_status_t mesh_attn_cache_fwd(
     const ma_cache_t* cache, int32_t num_q_heads, float softmax_scale,

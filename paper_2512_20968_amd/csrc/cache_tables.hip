@@ -7,9 +7,10 @@
 // makes the prefix sums for itself in LDS (they are at most 4096 requests, 16 a
 // thread) and takes a share of the rows and new pages, and there is one launch
 // and no workspace: 3.2 us for 40 requests of one new token, of which 2.5 are the
-// launch, 7.1 us for 700 requests with 17 thousand new tokens.  No workgroup reads what another writes: block table
-// entries below a request's old pages are only read, those from there on only
-// written (a row on a new page takes its number from the free list).
+// launch, 7.0 us for 700 requests with 17 thousand new tokens.  No workgroup
+// reads what another writes: block table entries below a request's old pages are
+// only read, those from there on only written (a row on a new page takes its
+// number from the free list).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
