@@ -669,6 +669,69 @@ def test_short_and_long_sequences_of_many_tiles(d, ps, group, long, dtype):
     check((o[:, heads], lse[heads]), x.want(heads), d)
 
 
+def test_two_streams_at_once():
+    """Calls that overlap, each with the binding's own workspace."""
+    c = cache_of(head_dim=128, num_kv_heads=8, num_pages=700, max_pages=600)
+    a = Batch(c, [8000, 2000], [40, 1], group=4, seed=22)
+    b = Batch(c, [5, 9000], [5, 3], group=4, seed=23)
+    want = a.run(), b.run()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        for x, s in zip((a, b), streams):
+            q = x.q.cuda()
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got.append(x.run(q=q, stream=s))
+    torch.cuda.synchronize()
+    for i, (o, lse) in enumerate(got):
+        assert torch.equal(o, want[i % 2][0])
+        assert torch.equal(lse, want[i % 2][1])
+
+
+def test_a_captured_prompt_replays_with_other_lengths():
+    """The same launches cut the sequences of one batch and leave another's whole."""
+    c = cache_of(head_dim=128, num_kv_heads=16, page_size=64, num_pages=400,
+                 max_pages=300)
+    batches = [Batch(c, lens, new, group=2, seed=24) for lens, new in (
+        ([1400, 600], [1350, 10]), ([16000, 1360], [600, 760]),
+        ([1360, 0], [1360, 0]))]
+    rows, d = 1360, 128
+    q = torch.zeros(rows, 32, d, dtype=torch.bfloat16, device="cuda")
+    positions, cu = torch.zeros(rows, **I32), torch.zeros(3, **I32)
+    lens, table = torch.zeros(2, **I32), torch.zeros(2, 300, **I32)
+    data = torch.zeros_like(batches[0].data)
+    o = torch.zeros(rows, 32, d, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(32, rows, device="cuda")
+    ws = torch.empty(ma.mesh_attn_cache_fwd_workspace_size(c, 32, 2, rows),
+                     dtype=torch.uint8, device="cuda")
+
+    def step():
+        ma.mesh_attn_cache_fwd(c, d ** -0.5, q, positions, cu, lens, table,
+                               data, o, lse, ws=ws)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    heads = [0, 17, 31]
+    for b in batches + batches[:2]:
+        q.copy_(b.q)
+        for t, x in ((positions, b.positions), (cu, b.cu), (lens, b.lens),
+                     (table, b.table)):
+            t.copy_(i32(x))
+        data.copy_(b.data)
+        o.fill_(123.0)
+        lse.fill_(123.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check((o[:, heads], lse[heads]), b.want(heads), d)
+        got = o.clone()
+        step()
+        assert torch.equal(o, got)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_nan_in_a_short_sequence_of_many(dtype):
     """Only the heads of its KV head, and for V its 32 dims, become NaN."""
