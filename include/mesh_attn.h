@@ -533,8 +533,9 @@ ma_status_t mesh_attn_cache_fwd(
  * positions[axis[i]][row] * inv_freq[i]:
  *   (a, b) -> (a cos - b sin, b cos + a sin);
  * inverse = 1 turns it back, which is also the gradient.  The other dims are
- * copied.  Angles are reduced exactly (64-bit fractions of a turn), so far
- * positions are as accurate as near ones.
+ * copied.  A frequency's turn per position is rounded to 2^-64 of a turn and
+ * its product with the position reduced exactly, so an angle is off by at most
+ * 2^-34 of a turn before its sine and cosine, whatever frequency and position.
  * ------------------------------------------------------------------------- */
 typedef struct {
   int32_t head_dim;       /* a multiple of 16, at most 256                   */

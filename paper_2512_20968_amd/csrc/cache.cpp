@@ -115,6 +115,26 @@ ma_status_t check_q_heads(int32_t hq, int32_t hkv) {
   return MA_OK;
 }
 
+// f / (2 pi) modulo 1 in units of 2^-64, rounded to nearest, for |f| < 2^31: the
+// kernel's product with the position wraps as turns do, so what is rounded off
+// here is all that a far position's angle lacks.  f's 53-bit integer m times
+// 1 / (2 pi) cut to 128 bits, of which at most 2^31 2^-128 is missing.
+uint64_t turn_per_position(double f) {
+  constexpr uint64_t kHigh = 0x28be60db9391054aull;
+  constexpr uint64_t kLow = 0x7f09d5f47d4d3770ull;
+  int exponent;
+  const double fraction = std::frexp(std::fabs(f), &exponent);
+  if (fraction == 0.0) return 0;
+  const uint64_t m = static_cast<uint64_t>(fraction * 0x1p53);
+  typedef unsigned __int128 u128;
+  const u128 product = u128{kHigh} * m + ((u128{kLow} * m) >> 64);
+  // The result is product 2^(exponent - 53); exponent is at most 31.
+  const int shift = 52 - exponent;
+  const u128 twice = shift < 128 ? product >> shift : u128{0};
+  const uint64_t turn = static_cast<uint64_t>((twice + 1) >> 1);
+  return f < 0 ? uint64_t{0} - turn : turn;
+}
+
 #define MA_TRY(expr)                       \
   do {                                     \
     const ma_status_t st_ = (expr);        \
@@ -332,20 +352,11 @@ ma_status_t mesh_attn_rope(const ma_rope_t* rope, int64_t rows,
     p.t.turn[i] = 0;
     p.t.axis[i] = 0;
   }
-  // Turns per position modulo 1, in 2^-64: the extended type's 64-bit fraction
-  // holds the product to about a unit of that for frequencies up to 2 pi, and
-  // the kernel's product with the position wraps as turns do.
-  const long double kPerRadian = 0.159154943091895335768883763372514362L;
   for (int i = 0; i < rot / 2; ++i) {
     const double f = rope->inv_freq[i];
     if (!(std::fabs(f) < 2147483648.0))
       return fail(MA_ERR_INVALID_ARG, "inv_freq[%d] = %g", i, f);
-    const long double t = static_cast<long double>(std::fabs(f)) * kPerRadian;
-    const long double frac = t - static_cast<uint32_t>(t);
-    const long double scaled = frac * 0x1p64L + 0.5L;
-    const uint64_t u =
-        scaled >= 0x1p64L ? 0 : static_cast<uint64_t>(scaled);
-    p.t.turn[i] = f < 0 ? uint64_t{0} - u : u;
+    p.t.turn[i] = turn_per_position(f);
     const int32_t a = rope->axis ? rope->axis[i] : 0;
     if (a < 0 || a >= rope->num_axes)
       return fail(MA_ERR_INVALID_ARG, "axis[%d] = %d outside [0, %d)", i, a,

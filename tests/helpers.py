@@ -5,6 +5,8 @@ float32 accumulation; backward max |dX err| <= 5e-2 * max |dX|."""
 
 import sys
 import time
+from fractions import Fraction
+from functools import lru_cache
 
 import numpy as np
 import torch
@@ -313,3 +315,28 @@ def oracle_backward_rows(prob, q_idx, kv_idx, q, k, v, do, kv_heads, q_rows,
             dk[:, ki] += gk
             dv[:, ki] += gv
     return dq, dk, dv, q_heads
+
+
+@lru_cache(maxsize=1)
+def turns_per_radian():
+    """1 / (2 pi) to 2^-390, by pi / 4 = 4 atan(1/5) - atan(1/239) (Machin) in
+    integers."""
+    one = 1 << 400
+
+    def atan_of_inverse(n):
+        term, k = one // n, 1
+        total = 0
+        while term:
+            total += term // k if k % 4 == 1 else -(term // k)
+            term //= n * n
+            k += 2
+        return total
+
+    pi = 4 * (4 * atan_of_inverse(5) - atan_of_inverse(239))
+    return Fraction(one, 2 * pi)
+
+
+def exact_angle(freq, position):
+    """position * freq (a double, an integer) modulo a turn, in (-pi, pi]."""
+    turn = Fraction(freq) * int(position) * turns_per_radian() % 1
+    return float((turn - 1 if turn > Fraction(1, 2) else turn)) * 2 * np.pi

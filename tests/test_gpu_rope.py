@@ -7,6 +7,8 @@ import torch
 import paper_2512_20968_amd as ma
 from oracle import cache as oc
 
+from helpers import exact_angle
+
 pytestmark = pytest.mark.gpu
 
 
@@ -161,3 +163,26 @@ def test_more_rows_than_a_launch_counts_threads():
     ma.mesh_attn_rope(r, p, y, want)
     assert torch.equal(x[-700:], want)
     assert not x[:1000].any() and not x[-2000:-700].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_frequencies_at_far_positions(dtype):
+    """Frequencies far past a turn, up to the limit, against angles of exact
+    integers; tolerances as _check's."""
+    freq = [7.5, 100.0, 1e3, 1e4, 1e6, 1.2e8, -2.0**30, 2.0**31 - 1]
+    r = dict(head_dim=16, rotary_dim=16, inv_freq=freq)
+    pos = [0, 1, 77, 1000003, 2**30 + 1, 2**31 - 1, -1, -12345, -2**31]
+    x = torch.randn(len(pos), 3, 16,
+                    generator=torch.Generator().manual_seed(3))
+    x = x.to(dtype).cuda()
+    y = torch.empty_like(x)
+    ma.mesh_attn_rope(r, torch.tensor(pos).int().cuda(), x, y)
+    phi = np.array([[exact_angle(f, t) for f in freq] for t in pos])[:, None]
+    z = x.double().cpu().numpy()
+    a, b = z[..., :8], z[..., 8:]
+    want = np.concatenate([a * np.cos(phi) - b * np.sin(phi),
+                           b * np.cos(phi) + a * np.sin(phi)], -1)
+    tol = np.tile(np.hypot(a, b), 2) * 2.0**-21
+    if dtype == torch.bfloat16:
+        tol += np.abs(want) * 2.0**-8
+    assert np.all(np.abs(y.double().cpu().numpy() - want) <= tol)
