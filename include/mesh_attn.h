@@ -450,9 +450,9 @@ size_t mesh_attn_cache_bytes(const ma_cache_t* cache);
  *                   the last request.
  *   refused         [1] int32: number of refused requests.
  * rows may be larger or smaller than the number of new tokens (rows past it
- * get -1; tokens past rows get no slot).  Outputs must not alias inputs: a
- * loop of steps alternates between two buffers each for the lengths and the
- * free range. */
+ * get -1; tokens past rows get no slot).  No output may overlap an input
+ * or another output (MA_ERR_INVALID_ARG): a loop of steps alternates between
+ * two buffers each for the lengths and the free range. */
 ma_status_t mesh_attn_cache_tables(
     const ma_cache_t* cache, int32_t num_requests, const int32_t* lens,
     const int32_t* new_lens, const int32_t* free_pages, int32_t num_free,

@@ -33,6 +33,17 @@ ma_status_t check_args(const Arg* a, int n) {
   return MA_OK;
 }
 
+struct Range {
+  const void* p;
+  size_t bytes;
+};
+
+bool overlap(const Range& a, const Range& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p);
+  const uintptr_t y = reinterpret_cast<uintptr_t>(b.p);
+  return a.bytes > 0 && b.bytes > 0 && x < y + b.bytes && y < x + a.bytes;
+}
+
 ma_status_t launched(hipError_t e, const char* what) {
   if (e != hipSuccess)
     return fail(MA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
@@ -185,11 +196,27 @@ ma_status_t mesh_attn_cache_tables(
     const Arg args[] = {{"slots", slots, 8}, {"positions", positions, 4}};
     MA_TRY(check_args(args, 2));
   }
-  // Written while other workgroups of the launch still read them.
-  if (free_range_out == free_range || (num_requests > 0 && lens_out == lens))
-    return fail(MA_ERR_INVALID_ARG,
-                "lens_out and free_range_out must not alias lens and "
-                "free_range");
+  // Outputs, then inputs: the former are written while other workgroups of the
+  // launch still read the latter.
+  const size_t n = static_cast<size_t>(num_requests);
+  const Range ranges[] = {
+      {block_table, 4 * n * static_cast<size_t>(p.c.max_pages)},
+      {lens_out, 4 * n},
+      {cu_new, 4 * (n + 1)},
+      {slots, 8 * static_cast<size_t>(rows)},
+      {positions, 4 * static_cast<size_t>(rows)},
+      {free_range_out, 8},
+      {refused, 4},
+      {lens, 4 * n},
+      {new_lens, 4 * n},
+      {free_pages, 4 * static_cast<size_t>(num_free)},
+      {free_range, 8}};
+  constexpr int kOutputs = 7, kRanges = 11;
+  for (int i = 0; i < kOutputs; ++i)
+    for (int j = i + 1; j < kRanges; ++j)
+      if (overlap(ranges[i], ranges[j]))
+        return fail(MA_ERR_INVALID_ARG,
+                    "an output must not alias an input or another output");
   p.lens = lens;
   p.new_lens = new_lens;
   p.free_pages = free_pages;

@@ -3,6 +3,10 @@ sampled rows, tolerance checks).  The tolerances are the parity bar: forward
 max |O err| <= 2e-2 and max |LSE err| <= 1e-3 (absolute) for bf16 inputs with
 float32 accumulation; backward max |dX err| <= 5e-2 * max |dX|."""
 
+import ctypes
+import os
+import shutil
+import subprocess
 import sys
 import time
 from fractions import Fraction
@@ -13,6 +17,7 @@ import torch
 
 import oracle
 import paper_2512_20968_amd as ma
+from paper_2512_20968_amd import _binding
 
 O_TOL = 2e-2
 LSE_TOL = 1e-3
@@ -315,6 +320,29 @@ def oracle_backward_rows(prob, q_idx, kv_idx, q, k, v, do, kv_heads, q_rows,
             dk[:, ki] += gk
             dv[:, ki] += gv
     return dq, dk, dv, q_heads
+
+
+def cache_host_library(directory):
+    """csrc/cache.cpp linked with stand-ins for its kernels
+    (stub_launches.cpp), as a ctypes library; None without g++."""
+    gxx = shutil.which("g++")
+    if gxx is None:
+        return None
+    here = os.path.dirname(os.path.abspath(__file__))
+    root = os.path.dirname(here)
+    csrc = os.path.join(root, "paper_2512_20968_amd", "csrc")
+    out = os.path.join(str(directory), "libcachehost.so")
+    subprocess.run(
+        [gxx, "-std=c++17", "-O1", "-Wall", "-shared", "-fPIC",
+         "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(root, "include"), "-I",
+         csrc, "-I", "/opt/rocm/include", os.path.join(csrc, "cache.cpp"),
+         os.path.join(here, "stub_launches.cpp"), "-o", out,
+         "-Wl,-Bsymbolic"], check=True)
+    lib = ctypes.CDLL(out)
+    for name in ("mesh_attn_cache_tables", "mesh_attn_rope"):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = _binding._SIGNATURES[name]
+    return lib
 
 
 @lru_cache(maxsize=1)

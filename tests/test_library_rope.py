@@ -3,41 +3,20 @@ with stand-ins for the kernels (stub_launches.cpp), against exact integers."""
 
 import ctypes
 import math
-import os
 import random
-import shutil
-import subprocess
 from fractions import Fraction
 
 import pytest
 
 import paper_2512_20968_amd as ma
-from paper_2512_20968_amd import _binding
 
-from helpers import turns_per_radian
-
-ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-HERE = os.path.join(ROOT, "tests")
+from helpers import cache_host_library, turns_per_radian
 
 
 @pytest.fixture(scope="module")
 def lib(tmp_path_factory):
-    gxx = shutil.which("g++")
-    if gxx is None:
-        pytest.skip("g++ not available")
-    out = tmp_path_factory.mktemp("rope") / "librope.so"
-    csrc = os.path.join(ROOT, "paper_2512_20968_amd", "csrc")
-    subprocess.run(
-        [gxx, "-std=c++17", "-O1", "-Wall", "-shared", "-fPIC",
-         "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROOT, "include"), "-I",
-         csrc, "-I", "/opt/rocm/include", os.path.join(csrc, "cache.cpp"),
-         os.path.join(HERE, "stub_launches.cpp"), "-o", str(out),
-         "-Wl,-Bsymbolic"], check=True)
-    lib = ctypes.CDLL(str(out))
-    name = "mesh_attn_rope"
-    lib.mesh_attn_rope.restype, lib.mesh_attn_rope.argtypes = \
-        _binding._SIGNATURES[name]
-    return lib
+    lib = cache_host_library(tmp_path_factory.mktemp("rope"))
+    return lib or pytest.skip("g++ not available")
 
 
 def turns(lib, freq):
