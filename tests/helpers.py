@@ -368,3 +368,76 @@ def exact_angle(freq, position):
     """position * freq (a double, an integer) modulo a turn, in (-pi, pi]."""
     turn = Fraction(freq) * int(position) * turns_per_radian() % 1
     return float((turn - 1 if turn > Fraction(1, 2) else turn)) * 2 * np.pi
+
+
+class ExactScores:
+    """Requests of two keys whose scores, keys and values a float32 kernel over
+    the 4-bit cache makes without rounding: what it rounds afterwards is little.
+
+    q is a multiple of 1/8 up to 2, k and v E2M1 values with a 6 in each group
+    of 32 (scale 1), v positive: scores are multiples of 1/16 below 2^11.  The
+    softmax scale is 2^-8, so |score| stays below 0.69 (asserted).
+
+    With u = 2^-23: the argument x - max of a probability (log2 units, below 2)
+    is rounded by u / 2 and carries log2(e)'s own rounding, u / 2.8 of it; with
+    the exponential's unit in the last place a probability is off by 2 u of
+    itself, and O by at most twice that, 4 u (its weights sum to 1).  Three bf16
+    hold its 24 bits.  Six products are added, each addition cut to u of the sum
+    (all are positive): 6 u.  The sum of the probabilities 1 u, the reciprocal
+    1 u, the last product u / 2: 12.5 u of O in all.  LSE: 3 u of the sum are
+    4.4 u of its log2; the logarithm, the addition and the last product 1 u
+    each (values below 2): 8 u."""
+
+    O_BOUND = 12.5 * 2.0**-23
+    LSE_BOUND = 8 * 2.0**-23
+    scale = 2.0**-8
+
+    def __init__(self, requests, new, hkv, group, d, seed=0):
+        rng = np.random.default_rng(seed)
+        steps = np.array([0.5, 1.0, 1.5, 2.0, 3.0, 4.0])
+        self.shape = requests, new, hkv, group, d
+        self.k, self.v = (rng.choice(steps, (requests * 2, hkv, d))
+                          for _ in range(2))
+        self.k[..., ::32] = self.v[..., ::32] = 6.0
+        self.k *= rng.choice([-1.0, 1.0], self.k.shape)
+        self.q = rng.integers(-16, 17, (requests * new, hkv * group, d)) / 8.0
+
+    def _by_request(self):
+        r, new, hkv, group, d = self.shape
+        q = self.q.reshape(r, new, hkv, group, d)
+        k = self.k.reshape(r, 2, hkv, d)
+        x = self.scale * np.einsum("rnhgd,rkhd->rnhgk", q, k)
+        assert np.abs(x).max() < 0.69  # two of them: 2 log2 units
+        return x, self.v.reshape(r, 2, hkv, d)
+
+    def output(self, p, v):
+        """sum_k p_k v_k of every row, as O."""
+        r, new, hkv, group, d = self.shape
+        return np.einsum("rnhgk,rkhd->rnhgd", p, v).reshape(
+            r * new, hkv * group, d)
+
+    def want(self):
+        """O [rows, Hq, d] and LSE [Hq, rows]."""
+        x, v = self._by_request()
+        total = np.exp(x).sum(-1)
+        o = self.output(np.exp(x) / total[..., None], v)
+        r, new, hkv, group, _ = self.shape
+        return o, np.log(total).reshape(r * new, hkv * group).T
+
+    def with_parts(self, parts, cut):
+        """O with every probability (float32, relative to the largest one) held
+        as `parts` bf16, cut off or rounded one after the other, and nothing
+        else rounded."""
+        x, v = self._by_request()
+        p = np.exp(x - x.max(-1, keepdims=True)).astype(np.float32)
+        rest, held = p.copy(), np.zeros(p.shape)
+        for _ in range(parts):
+            if cut:
+                part = (rest.view(np.uint32) & np.uint32(0xffff0000)).view(
+                    np.float32)
+            else:
+                part = torch.tensor(rest).to(torch.bfloat16).float().numpy()
+            held += part
+            rest = rest - part
+        total = p.astype(np.float64).sum(-1)[..., None]
+        return self.output(held / total, v)

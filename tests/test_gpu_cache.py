@@ -8,6 +8,8 @@ import torch
 import paper_2512_20968_amd as ma
 from oracle import cache as oc
 
+from helpers import ExactScores
+
 pytestmark = pytest.mark.gpu
 
 I32 = dict(dtype=torch.int32, device="cuda")
@@ -359,6 +361,37 @@ def check(got, want, d, keys=4096):
     assert np.all(np.abs(lse[fine] - wl[fine]) <= ltol[fine])
     # Rows of no request are left alone.
     assert np.all(o[~live.T] == 123.0) and np.all(lse[~live] == 123.0)
+
+
+@pytest.mark.parametrize("d,hkv,group,new,requests,pages", [
+    (128, 2, 4, 1, 40, 1), (64, 2, 2, 1, 40, 200), (128, 2, 4, 8, 11, 200),
+    (64, 1, 3, 40, 5, 1), (128, 1, 4, 30, 5, 200), (64, 16, 2, 1, 520, 1),
+    (128, 16, 4, 12, 90, 1)])
+def test_float32_probabilities_keep_24_bits(d, hkv, group, new, requests,
+                                            pages):
+    """Exact scores and values of one sign, two keys a request: what is left of
+    a float32 O's error (the bound is derived beside the inputs), too little for
+    probabilities of two bf16."""
+    c = cache_of(head_dim=d, num_kv_heads=hkv, num_pages=requests,
+                 max_pages=pages)
+    x = ExactScores(requests, new, hkv, group, d)
+    slots = (np.arange(requests)[:, None] * 16 + np.arange(2)).ravel()
+    data = random_bytes(c)
+    bf = [torch.tensor(a).to(torch.bfloat16).cuda() for a in (x.q, x.k, x.v)]
+    ma.mesh_attn_cache_append(c, bf[1], bf[2], i64(slots), data)
+    rows = requests * new
+    table = np.full((requests, pages), -1)
+    table[:, 0] = np.arange(requests)
+    o = torch.full((rows, hkv * group, d), 123.0, device="cuda")
+    lse = torch.full((hkv * group, rows), 123.0, device="cuda")
+    ma.mesh_attn_cache_fwd(c, x.scale, bf[0], i32([1] * rows),
+                           i32(np.arange(requests + 1) * new),
+                           i32([2] * requests), i32(table), data, o, lse)
+    want_o, want_lse = x.want()
+    got = o.double().cpu().numpy()
+    assert np.all(np.abs(got - want_o) <= x.O_BOUND * want_o)
+    assert np.all(np.abs(lse.double().cpu().numpy() - want_lse)
+                  <= x.LSE_BOUND)
 
 
 LENGTHS = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 160, 190]

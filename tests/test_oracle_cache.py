@@ -7,6 +7,8 @@ import pytest
 import oracle
 from oracle import cache as oc
 
+from helpers import ExactScores
+
 
 def _cache(**kw):
     c = dict(num_pages=6, page_size=16, num_kv_heads=2, head_dim=64,
@@ -195,3 +197,31 @@ def test_rope_is_a_rotation_of_complex_pairs(interleaved):
     np.testing.assert_allclose(
         (w * y).sum(), (oc.rope(w, pos, freq, axis, 32, interleaved, True)
                         * x).sum())
+
+
+@pytest.mark.parametrize("shape", [(40, 1, 2, 4, 128), (40, 1, 2, 2, 64),
+                                   (11, 8, 2, 4, 128), (5, 40, 1, 3, 64)])
+def test_two_bf16_probabilities_miss_the_float32_bound(shape):
+    """The bound that the kernel's float32 O is held to: three parts of a
+    probability meet it with nothing lost, two parts, cut off or rounded, and one
+    do not."""
+    x = ExactScores(*shape)
+    want, lse = x.want()
+    # The inputs are what the cache holds, and the oracle agrees about them.
+    for a in (x.k, x.v):
+        np.testing.assert_array_equal(oc.values(*oc.quantize(a)), a)
+    c = _cache(num_kv_heads=shape[2], head_dim=shape[4], num_pages=1)
+    data = np.zeros((1, shape[2], oc.page_bytes(c)), dtype=np.uint8)
+    oc.write_rows(c, data, x.k[:2], x.v[:2], [0, 1])
+    o, l, _, _ = oc.attention(c, x.scale, x.q[:1], [1], [0, 1], [2],
+                              np.array([[0]]), data)
+    np.testing.assert_allclose(o, want[:1], rtol=1e-13)
+    np.testing.assert_allclose(l, lse[:, :1], rtol=1e-13)
+
+    def off(parts, cut):
+        return (np.abs(x.with_parts(parts, cut) - want) / want).max()
+
+    assert off(3, True) < 0.25 * x.O_BOUND
+    for parts in (1, 2):
+        for cut in (True, False):
+            assert off(parts, cut) > 1.5 * x.O_BOUND, (parts, cut)
