@@ -723,6 +723,45 @@ def test_two_streams_at_once():
         assert torch.equal(lse, want[i % 2][1])
 
 
+def test_calls_back_to_back_on_two_streams():
+    """Every buffer is there before the first call, so that the calls of one
+    stream are in flight while the other's run, each with a workspace of the
+    binding: the results are those of the calls alone."""
+    c = cache_of(head_dim=128, num_kv_heads=8, page_size=64, num_pages=400,
+                 max_pages=300)
+    calls, want = [], []
+    for seed, (lens, new) in enumerate((([15000, 2000], [300, 1]),
+                                        ([5, 17000, 3000], [5, 150, 3]))):
+        b = Batch(c, lens, new, group=4, seed=25 + seed)
+        want.append(b.run())
+        calls.append((b, [b.q.cuda()] + [i32(x) for x in (
+            b.positions, b.cu, b.lens, b.table)] + [b.data]))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    rounds = 12
+    out = [[(torch.full_like(o, 123.0), torch.full_like(lse, 123.0))
+            for _ in range(rounds)] for o, lse in want]
+    marks = [[[torch.cuda.Event(enable_timing=True) for _ in range(2)]
+              for _ in range(rounds)] for _ in want]
+    begin = torch.cuda.Event(enable_timing=True)
+    begin.record()
+    torch.cuda.synchronize()
+    for i in range(rounds):
+        for j, ((b, args), s) in enumerate(zip(calls, streams)):
+            marks[j][i][0].record(s)
+            ma.mesh_attn_cache_fwd(c, b.scale, *args, *out[j][i], stream=s)
+            marks[j][i][1].record(s)
+    torch.cuda.synchronize()
+    for results, (o, lse) in zip(out, want):
+        for x, y in results:
+            assert torch.equal(x, o) and torch.equal(y, lse)
+    # They did overlap: most calls begin before the other stream's call of the
+    # same round ends, and end after it begins.
+    at = [[[begin.elapsed_time(e) for e in pair] for pair in side]
+          for side in marks]
+    both = sum(a[0] < b[1] and b[0] < a[1] for a, b in zip(*at))
+    assert both > rounds // 2, at
+
+
 def test_a_captured_prompt_replays_with_other_lengths():
     """The same launches cut the sequences of one batch and leave another's whole."""
     c = cache_of(head_dim=128, num_kv_heads=16, page_size=64, num_pages=400,
