@@ -496,6 +496,39 @@ def test_no_key_survives_a_nan_length_of_garbage():
         assert o.shape[0] == 9 and not torch.isnan(lse).any()
 
 
+@pytest.mark.parametrize("d,group,rows,dtype", [
+    (64, 2, 9, torch.float32), (128, 4, 70, torch.bfloat16),
+    (128, 8, 300, torch.float32)])
+def test_absurd_row_ranges_stay_inside_the_buffers(d, group, rows, dtype):
+    """cu_new that decreases, or lies outside the rows: the rows it still gives
+    to a request are right, all others and what lies around O and LSE as they
+    were."""
+    c = cache_of(head_dim=d, page_size=64, num_pages=100, max_pages=40)
+    b = Batch(c, [700, 60], [rows - 4, 2], group=group, seed=7, pad=2)
+    b.positions = np.random.default_rng(rows).integers(-2, 800, rows)
+    top, guard, heads = 2**31 - 1, 4096, [0, b.hq - 1]
+    for cu in ([0, 3, 1], [-5, 3, top], [rows, rows, rows], [4, 0, 2],
+               [-top - 1, -7, -3], [top, top, top], [0, top, 0],
+               [rows - 1, rows + 1, top], [2, 2, rows], [rows + 9, 1, rows]):
+        b.cu = np.array(cu)
+        flat = [torch.full((guard + n + guard,), 123.0, dtype=t, device="cuda")
+                for n, t in ((rows * b.hq * d, dtype),
+                             (b.hq * rows, torch.float32))]
+        o = flat[0][guard:-guard].view(rows, b.hq, d)
+        lse = flat[1][guard:-guard].view(b.hq, rows)
+        ma.mesh_attn_cache_fwd(c, b.scale, b.q.cuda(), i32(b.positions),
+                               i32(b.cu), i32(b.lens), i32(b.table), b.data, o,
+                               lse)
+        for x in flat:
+            assert torch.all(x[:guard] == 123.0), cu
+            assert torch.all(x[-guard:] == 123.0), cu
+        want = b.want(heads)
+        check((o[:, heads], lse[heads]), want, d)
+        of_none = torch.tensor(np.isnan(want[3][0])).cuda()
+        assert torch.all(o[of_none] == 123.0), cu
+        assert torch.all(lse[:, of_none] == 123.0), cu
+
+
 def test_requests_that_share_pages_and_positions_in_any_order():
     c = cache_of(head_dim=128, num_pages=60)
     b = Batch(c, [190, 170, 190, 40], [9, 5, 17, 1], group=4, seed=16)
