@@ -529,6 +529,23 @@ def test_absurd_row_ranges_stay_inside_the_buffers(d, group, rows, dtype):
         assert torch.all(lse[:, of_none] == 123.0), cu
 
 
+@pytest.mark.parametrize("d,ps,share", [(128, 64, SHARES[0]),
+                                        (128, 16, SHARES[1]),
+                                        (64, 256, SHARES[3])])
+def test_ragged_batch_against_the_oracles_own_reader(d, ps, share):
+    """Keys and values by the oracle from the cache's bytes, none of them by the
+    read kernel; several pages a request, and one of them not a page."""
+    c = cache_of(head_dim=d, page_size=ps, num_pages=60,
+                 max_pages=max(2, 320 // ps), **share)
+    b = Batch(c, [300, 0, 65, 17, 129], [3, 0, 1, 2, 1], group=3, seed=27,
+              pad=1)
+    b.table[4, 0] = 60
+    want = oc.attention(c, b.scale, b.q.double().numpy(), b.positions, b.cu,
+                        b.lens, b.table, b.data.cpu().numpy())
+    check(b.run(), want, d)
+    check(b.run(torch.bfloat16), want, d)
+
+
 def test_requests_that_share_pages_and_positions_in_any_order():
     c = cache_of(head_dim=128, num_pages=60)
     b = Batch(c, [190, 170, 190, 40], [9, 5, 17, 1], group=4, seed=16)
