@@ -449,10 +449,15 @@ size_t mesh_attn_cache_bytes(const ma_cache_t* cache);
  *   positions       [rows] int32: row r's position in its sequence; -1 behind
  *                   the last request.
  *   refused         [1] int32: number of refused requests.
- * rows may be larger or smaller than the number of new tokens (rows past it
- * get -1; tokens past rows get no slot).  No output may overlap an input
- * or another output (MA_ERR_INVALID_ARG): a loop of steps alternates between
- * two buffers each for the lengths and the free range. */
+ * rows may be larger or smaller than the number of new tokens: rows past it get
+ * -1; tokens past rows get no slot, but count in lens_out and are in no way
+ * refused, so a later attention would read slots that were never written:
+ * cu_new[num_requests] > rows tells that there are some.  A request that is
+ * refused for want of pages takes those it wanted out of the reach of all later
+ * requests of the call.
+ * No output may overlap an input or another output (MA_ERR_INVALID_ARG): a loop
+ * of steps alternates between two buffers each for the lengths and the free
+ * range. */
 ma_status_t mesh_attn_cache_tables(
     const ma_cache_t* cache, int32_t num_requests, const int32_t* lens,
     const int32_t* new_lens, const int32_t* free_pages, int32_t num_free,
@@ -515,7 +520,8 @@ size_t mesh_attn_cache_fwd_workspace_size(const ma_cache_t* cache,
  * LSE are those of mesh_attn_tile_fwd over the stored values: exact products,
  * float32 accumulation and softmax; the probabilities enter the second product
  * in bf16 for a bf16 O, and as a sum of three bf16 for a float32 O.  A NaN key
- * or value reaches the rows that see it and no other.  How the keys are split
+ * or value reaches the rows that see it and no other: the key makes O and LSE NaN
+ * (the tile's LSE would be -inf), the value O.  How the keys are split
  * over workgroups depends on the sizes and lengths alone: equal calls give equal
  * bits. */
 ma_status_t mesh_attn_cache_fwd(

@@ -32,9 +32,12 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # its float32-output kernel then fits 256 registers without a spill, and the
 # bf16-output kernel's schedule runs 0.5-1.6 % faster.
 # The attention over the cache keeps every join's own restore of the execution
-# mask: without it a register that was saved inside a nested branch of the fold
-# was restored for the inner branch's lanes alone (seen in the assembly of a
-# float32 kernel of 64 rows, whose next item then used it in an address).
+# mask: in a kernel that is no longer built (float32 O, tiles of 64 rows) the
+# compiler left one out, and a register saved inside a nested branch of the fold
+# was restored for the inner branch's lanes alone and then used in an address.
+# The present kernels' assembly has no join that runs vector instructions before
+# its restore, with this flag or without; what the register allocator puts there
+# changes with any edit, so the flag stays.
 EXTRA = {"cache_fwd.hip": ["-mllvm", "-amdgpu-remove-redundant-endcf=0"],
          "tile_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "tile_fwd.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers"]}

@@ -15,8 +15,10 @@
 // 128 requests of 1 to 16K tokens 55 us for 0.23 GB, 4.2 TB/s, by the round trips
 // at the ends of 1024 sequences; 2 x 1000 rows over 33K tokens 1016 us, 1.04
 // PFLOP/s, by the instructions of a step of 64 rows and 32 keys: 64 matrix
-// instructions of 16 cycles, 270 vector ones (32 exponentials, 64 conversions) of
-// 4.5, or 9 while another wave's matrix instruction runs, 2400 cycles in all.
+// instructions of 16 cycles, 273 vector ones (32 exponentials, 64 conversions, 32
+// permutes) of 4.5, or 9 while another wave's matrix instruction runs, 2400 cycles
+// in all.  The same with float32 O, in tiles of 32 rows: 1892 us; 64 matrix and 282
+// vector instructions a step, for half the rows.
 //
 // MFMA conventions (16x16x32): lane l holds, for A, row l % 16 and the k-values
 // of quarter l / 16; for B, column l % 16 and the same quarter; accumulator
@@ -604,7 +606,10 @@ __device__ __forceinline__ int fresh_tid() {
 
 // Waves per SIMD: as many as the registers allow with few spills.  Head dim 128,
 // 16 rows: 3 (768 workgroups) read 1.1 GB in 209 us, 4 with spills 239; 32 rows:
-// 2 take 80 us for 16 requests of 8 rows each over 16K tokens, 3 with spills 127.
+// 2 took 80 us for 16 requests of 8 tokens of 4 heads over 16K tokens (68 now, where
+// the bytes take 53), 3 with spills 127.  64 rows at head dim 128 spill with 2: where
+// sequences are cut 6 registers, around the loop over the keys, or with pages of 16
+// 20, of which a step reads 5; where waves own theirs 2 and 3.
 template <int D, int NQ>
 constexpr int kWavesPerSimd = D == 64 ? (NQ == 1 ? 4 : NQ == 2 ? 3 : 2)
                                       : (NQ == 1 ? 3 : 2);
@@ -1091,7 +1096,9 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
                int64_t rows, bool out_f32) {
   const int group = hq / c.hkv;
   Shape s;
-  // Rows of a request, were they all alike.
+  // Rows of a request, were they all alike: the host knows no more.  A batch of
+  // decode tokens and a chunk has one height for both: 127 requests of a token and
+  // one of 300 over 16K keys (16 rows) take 199 us, apart 47 and 107.
   const int64_t each = (rows + num_requests - 1) / num_requests * group;
   // Three bf16 parts of 64 rows' probabilities do not fit the registers: 1000
   // rows of 4 heads over 33K tokens take 1894 us in tiles of 32 rows, 2175 of 64.
@@ -1100,8 +1107,9 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   const int64_t seqs = (rows * group / (16 * s.nq) + num_requests) * c.hkv;
   const int slots = resident_groups(c.d, s.nq);
   const int64_t keys = keys_of(c);
-  // Short tables (the lengths may be shorter still) are not worth a second
-  // launch.  Microseconds cut / whole, one row of 4 heads per KV head, 8 KV heads:
+  // Short tables are not worth a second launch.  (The lengths may be shorter still,
+  // which the host cannot know: wide tables of short requests are cut.)
+  // Microseconds cut / whole, one row of 4 heads per KV head, 8 KV heads:
   //   1 request of 256 tokens  9.1/6.7   64 of  512   18.3/12.1
   //   1 of 1024               10.0/11.6  64 of 1024   22.0/17.3
   //   1 of 2048               10.4/16.4  32 of 1..1024 13.5/11.4
@@ -1125,9 +1133,9 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   s.own_keys = !own ? -1
                     : static_cast<int>(brief || limit > keys ? keys : limit);
   // The others, unless tables are short, are cut, or left whole by workgroups
-  // where the lengths speak for it (whole_is_better; never those of one tile,
-  // since only their lengths differ: 512 requests of 1 to 32K tokens, one row of 4
-  // heads, 343 us cut, 446 whole).
+  // where the lengths speak for it (whole_is_better; never where the mean is one
+  // tile: 512 requests of 1 to 32K tokens, one row of 4 heads, 343 us cut, 446
+  // whole).
   s.cut = !brief && s.own_keys < keys;
   s.may_stay_whole = !one_tile;
   s.unit_log2 = 7;

@@ -1,11 +1,11 @@
 // Rotary positions with several axes (mesh_attn_rope).
 //
 // A pair turns by position * frequency.  The host gives every pair's turn per
-// position as a 64-bit fraction of a full turn; multiplied by the position
-// modulo 2^64 this is the angle's exact fraction of a turn to 2^31 * 2^-64,
+// position as a 64-bit fraction of a full turn, off by at most 2^-65; multiplied
+// by the position modulo 2^64 this is the angle's fraction of a turn to 2^-34,
 // where a float32 angle of a position near a million has lost five digits.  The
-// fraction's top two bits after rounding are the quadrant, the rest (at most an
-// eighth of a turn) goes to sincospi in float32.
+// fraction's top two bits after rounding are the quadrant; sine and cosine of the
+// rest (at most an eighth of a turn) are Taylor polynomials in float32.
 //
 // Streaming: every element is read and written once.  A workgroup takes a few
 // rows, makes each of their angles once, in LDS, and then walks over the 16-byte
@@ -190,9 +190,9 @@ __global__ __launch_bounds__(NT) void rope_kernel(RopeParams p) {
 
 }  // namespace
 
-// Workgroups before one takes more rows.  16384 float32 rows of 20 heads, 32
-// pairs: 63.7 us with 4 rows each (4096 workgroups), 69.3 with 8; 3001 rows of 16
-// heads 6.8 us with one each, 10.9 with 16.
+// Workgroups before one takes more rows.  16384 float32 rows of 20 heads of
+// 128, 32 pairs (336 MB): 63.7 us with 4 rows each (4096 workgroups), 69.3 with
+// 8; 3001 rows of 16 heads of 64 6.8 us with one each, 10.9 with 16.
 constexpr int kGroups = 4096;
 
 hipError_t launch_rope(const RopeParams& params, bool f32,
