@@ -570,6 +570,89 @@ ma_status_t mesh_attn_rope(const ma_rope_t* rope, int64_t rows,
                            int64_t k_out_stride, ma_dtype_t dtype,
                            int32_t inverse, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Attention under a score rule: capped scores, a distance bias, and ranges of
+ * keys (packed documents, prefixes, windows, padding).
+ *
+ * Query row i of head h, at position p_i, scores key j at position p_j as
+ *   x_ij = cap tanh(s <q_i, k_j> / cap) - slopes[h] |p_i - p_j|
+ * and sees it where key_begin[i] <= p_j < key_end[i]:
+ * O_i = sum_j exp(x_ij - LSE_i) v_j, LSE_i = ln sum_j exp(x_ij) over those keys.
+ * A row that sees none has O = 0 and LSE = -inf, whatever is in Q, K and V.
+ * Documents packed one after the other: begin and end of the row's document (end
+ * p_i + 1 if causal); a prefix that all of its document's rows see: end at least
+ * the prefix's; a window of w: begin at least p_i - w + 1; padding: begin = end.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  float cap;                /* 0: none; else finite and > 0                  */
+  const float* slopes;      /* [num_q_heads] device, or NULL: no bias        */
+  const int32_t* key_begin; /* [rows] device, or NULL: 0                     */
+  const int32_t* key_end;   /* [rows] device, or NULL: p_i + 1 (the tile calls
+                               with causal 0: everything)                    */
+} ma_score_t;
+
+/* Most partitions of a list in the calls below. */
+#define MA_SCORE_MAX_LIST 256
+
+/* Device workspace bytes of mesh_attn_score_fwd (0 if it needs none, or for
+ * invalid arguments). */
+size_t mesh_attn_score_fwd_workspace_size(const ma_problem_t* prob, int32_t nq,
+                                          int32_t nkv);
+
+/* O and LSE of a tile's rows under a rule.  The problem, lists and buffers are
+ * those of mesh_attn_tile_fwd, with these differences:
+ *   partition_len  any length from 1 on: partitions are not cut into whole
+ *                  blocks;
+ *   causal         decides only where the rule has no key_end;
+ *   score          the rule, its arrays indexed by the tile's query rows; NULL
+ *                  for none;
+ *   q, k, v        row r, head h at q + r * q_stride + h * head_dim, bf16
+ *                  device; strides in elements, multiples of 8, at least heads
+ *                  * head_dim, at most 2^24 (slices of a fused projection);
+ *   lists          at most MA_SCORE_MAX_LIST partitions each; rows times heads
+ *                  at most 2^28.
+ *   o              [nq*P][Hq][d] dense, bf16 or float32.  The probabilities
+ *                  enter the second product in bf16 for a bf16 O, and as a sum
+ *                  of three bf16 for a float32 O (a partial to be merged).
+ * A NaN or an infinity reaches the rows that see it and no other.  The call
+ * keeps no state and may be captured into a graph; equal calls give equal bits.
+ * A workspace serves one call, or one replay, at a time. */
+ma_status_t mesh_attn_score_fwd(const ma_problem_t* prob, const int32_t* q_idx,
+                                int32_t nq, const int32_t* kv_idx, int32_t nkv,
+                                const ma_score_t* score, const void* q,
+                                int64_t q_stride, const void* k,
+                                int64_t k_stride, const void* v,
+                                int64_t v_stride, void* o, ma_dtype_t o_dtype,
+                                float* lse, void* ws, size_t ws_bytes,
+                                hipStream_t stream);
+
+/* Device workspace bytes of mesh_attn_score_bwd; 0 for invalid arguments. */
+size_t mesh_attn_score_bwd_workspace_size(const ma_problem_t* prob, int32_t nq,
+                                          int32_t nkv);
+
+/* Gradients of <dO, O> for the tile under the same rule, given the final O and
+ * LSE of its rows:
+ *   P_ij = exp(x_ij - LSE_i), D_i = <dO_i, O_i>, T_ij = tanh(s <q_i, k_j> / cap),
+ *   dV_j = sum_i P_ij dO_i,  dS_ij = P_ij (<dO_i, v_j> - D_i) (1 - T_ij^2),
+ *   dQ_i = s sum_j dS_ij k_j,  dK_j = s sum_i dS_ij q_i.
+ *   o, d_o      [nq*P][Hq][d] bf16, dense;  lse [Hq][nq*P] float32.
+ *   dq          [nq*P][Hq][d];  dk, dv [nkv*P][Hkv][d], dense, grad_dtype: bf16
+ *               (sums in float32, rounded once; P and dS enter the products in
+ *               bf16).  MA_FP32 is not served (MA_ERR_UNSUPPORTED).
+ * Rows that see no key have dQ = 0 and give nothing to dK, dV; a NaN or an
+ * infinity of a pair that is seen gives NaN to its row's dQ and its key's dK or dV
+ * and to no other.  Deterministic (no atomics); may be captured. */
+ma_status_t mesh_attn_score_bwd(const ma_problem_t* prob, const int32_t* q_idx,
+                                int32_t nq, const int32_t* kv_idx, int32_t nkv,
+                                const ma_score_t* score, const void* q,
+                                int64_t q_stride, const void* k,
+                                int64_t k_stride, const void* v,
+                                int64_t v_stride, const void* o,
+                                const void* d_o, const float* lse, void* dq,
+                                void* dk, void* dv, ma_dtype_t grad_dtype,
+                                void* ws, size_t ws_bytes,
+                                hipStream_t stream);
+
 /* Text of the last non-OK status returned on the calling thread ("" if none).
  * The pointer stays valid until the next library call on that thread. */
 const char* mesh_attn_last_error(void);

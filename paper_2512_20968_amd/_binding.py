@@ -148,6 +148,34 @@ class Rope(ctypes.Structure):
                    axis=(ctypes.c_int32 * len(axis))(*map(int, axis)))
 
 
+class Score(ctypes.Structure):
+    """ma_score_t.  ``Score.make`` takes a mapping with any of the field names:
+    a float and GPU tensors (``slopes`` float32 [heads]; ``key_begin``,
+    ``key_end`` int32 [rows]), which the structure keeps alive."""
+    _fields_ = [("cap", ctypes.c_float),
+                ("slopes", ctypes.c_void_p),
+                ("key_begin", ctypes.c_void_p),
+                ("key_end", ctypes.c_void_p)]
+    tensors = (None, None, None)
+
+    @classmethod
+    def make(cls, score):
+        if isinstance(score, Score):
+            return score
+        score = dict(score or {})
+        cap = float(score.pop("cap", 0.0))
+        ts = tuple(score.pop(n, None)
+                   for n in ("slopes", "key_begin", "key_end"))
+        if score:
+            raise ValueError(f"unknown fields of a score rule: {sorted(score)}")
+        for t in ts:
+            if t is not None and not isinstance(t, _torch().Tensor):
+                raise TypeError("a score rule's arrays must be torch.Tensors")
+        self = cls(cap, *(None if t is None else t.data_ptr() for t in ts))
+        self.tensors = ts
+        return self
+
+
 _i32 = ctypes.c_int32
 _i64 = ctypes.c_int64
 _p = ctypes.c_void_p
@@ -155,6 +183,7 @@ _sz = ctypes.c_size_t
 _PROB = ctypes.POINTER(Problem)
 _CACHE = ctypes.POINTER(Cache)
 _I32P = ctypes.POINTER(ctypes.c_int32)
+_SCORE = ctypes.POINTER(Score)
 
 _SIGNATURES = {
     "mesh_attn_block_shape": (None, [_i32, _i32, _I32P, _I32P]),
@@ -203,6 +232,14 @@ _SIGNATURES = {
     "mesh_attn_rope": (_i32, [ctypes.POINTER(Rope), _i64, _p, _i32, _p, _i64,
                               _p, _i64, _i32, _p, _i64, _p, _i64, _i32, _i32,
                               _p]),
+    "mesh_attn_score_fwd_workspace_size": (_sz, [_PROB, _i32, _i32]),
+    "mesh_attn_score_fwd": (_i32, [_PROB, _I32P, _i32, _I32P, _i32, _SCORE, _p,
+                                   _i64, _p, _i64, _p, _i64, _p, _i32, _p, _p,
+                                   _sz, _p]),
+    "mesh_attn_score_bwd_workspace_size": (_sz, [_PROB, _i32, _i32]),
+    "mesh_attn_score_bwd": (_i32, [_PROB, _I32P, _i32, _I32P, _i32, _SCORE, _p,
+                                   _i64, _p, _i64, _p, _i64, _p, _p, _p, _p,
+                                   _p, _p, _i32, _p, _sz, _p]),
     "mesh_attn_last_error": (ctypes.c_char_p, []),
 }
 
@@ -803,3 +840,107 @@ def mesh_attn_rope(rope, positions, q, q_out, k=None, k_out=None, inverse=0,
         _stream_ptr(stream))
     _check("mesh_attn_rope", st)
     return q_out, k_out
+
+
+# ---------------------------------------------------------------------------
+# Attention under a score rule
+# ---------------------------------------------------------------------------
+
+def mesh_attn_score_fwd_workspace_size(prob, nq, nkv):
+    return int(load_library().mesh_attn_score_fwd_workspace_size(
+        ctypes.byref(Problem.make(prob)), int(nq), int(nkv)))
+
+
+def mesh_attn_score_bwd_workspace_size(prob, nq, nkv):
+    return int(load_library().mesh_attn_score_bwd_workspace_size(
+        ctypes.byref(Problem.make(prob)), int(nq), int(nkv)))
+
+
+def _score_args(score, rows, hq, dev):
+    """The rule, its tensors checked against the call's rows and heads."""
+    s, t = Score.make(score), _torch_module
+    slopes, begin, end = s.tensors
+    if slopes is not None:
+        _arg(slopes, "slopes", (hq,), t.float32, dev)
+    if begin is not None:
+        _arg(begin, "key_begin", (rows,), t.int32, dev)
+    if end is not None:
+        _arg(end, "key_end", (rows,), t.int32, dev)
+    return s
+
+
+def _call_workspace(ws, nbytes, dev, like, stream):
+    """Pointer and bytes of the caller's workspace, or of one of the call's own
+    stream, on which alone it is used; the tensor with them."""
+    torch = _torch_module
+    if ws is None:
+        with torch.cuda.stream(stream):
+            ws = torch.empty(max(nbytes(), 16), dtype=torch.uint8,
+                             device=like.device)
+    elif ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor of the call's "
+                         "GPU")
+    return ws, ws.data_ptr(), ws.nbytes
+
+
+def mesh_attn_score_fwd(prob, q_idx, kv_idx, score, q, k, v, o, lse, ws=None,
+                        stream=None):
+    """O and LSE of a tile under a score rule (a mapping with ``cap``,
+    ``slopes``, ``key_begin``, ``key_end``, or a ``Score``).  ``q [nq P, Hq,
+    d]``, ``k, v [nkv P, Hkv, d]`` bf16, row strides as they are; ``o`` bf16
+    (final) or float32 (partial)."""
+    dev, torch = _device_index(stream, q, "q"), _torch_module
+    pr = Problem.make(prob)
+    qa, qp, nq = _idx(q_idx)
+    ka, kp, nkv = _idx(kv_idx)
+    P, hq, hkv, d = (pr.partition_len, pr.num_q_heads, pr.num_kv_heads,
+                     pr.head_dim)
+    rows, bf = nq * P, torch.bfloat16
+    s = _score_args(score, rows, hq, dev)
+    qq, qs = _heads(q, "q", rows, hq, d, bf, dev)
+    kk, ks = _heads(k, "k", nkv * P, hkv, d, bf, dev)
+    vv, vs = _heads(v, "v", nkv * P, hkv, d, bf, dev)
+    f32 = o.dtype is torch.float32
+    ws, wp, wn = _call_workspace(
+        ws, lambda: mesh_attn_score_fwd_workspace_size(pr, nq, nkv), dev, q,
+        stream)
+    st = load_library().mesh_attn_score_fwd(
+        pr, qp, nq, kp, nkv, s, qq, qs, kk, ks, vv, vs,
+        _arg(o, "o", (rows, hq, d), torch.float32 if f32 else bf, dev),
+        MA_FP32 if f32 else MA_BF16,
+        _arg(lse, "lse", (hq, rows), torch.float32, dev), wp, wn,
+        _stream_ptr(stream))
+    _check("mesh_attn_score_fwd", st)
+    return o, lse
+
+
+def mesh_attn_score_bwd(prob, q_idx, kv_idx, score, q, k, v, o, d_o, lse, dq,
+                        dk, dv, ws=None, stream=None):
+    """dQ, dK, dV (bf16) of a tile under a score rule, from the final O (bf16)
+    and LSE; buffers as in ``mesh_attn_score_fwd``, ``o``, ``d_o`` and the
+    gradients dense."""
+    dev, torch = _device_index(stream, q, "q"), _torch_module
+    pr = Problem.make(prob)
+    qa, qp, nq = _idx(q_idx)
+    ka, kp, nkv = _idx(kv_idx)
+    P, hq, hkv, d = (pr.partition_len, pr.num_q_heads, pr.num_kv_heads,
+                     pr.head_dim)
+    rows, keys, bf = nq * P, nkv * P, torch.bfloat16
+    s = _score_args(score, rows, hq, dev)
+    qq, qs = _heads(q, "q", rows, hq, d, bf, dev)
+    kk, ks = _heads(k, "k", keys, hkv, d, bf, dev)
+    vv, vs = _heads(v, "v", keys, hkv, d, bf, dev)
+    ws, wp, wn = _call_workspace(
+        ws, lambda: mesh_attn_score_bwd_workspace_size(pr, nq, nkv), dev, q,
+        stream)
+    st = load_library().mesh_attn_score_bwd(
+        pr, qp, nq, kp, nkv, s, qq, qs, kk, ks, vv, vs,
+        _arg(o, "o", (rows, hq, d), bf, dev),
+        _arg(d_o, "d_o", (rows, hq, d), bf, dev),
+        _arg(lse, "lse", (hq, rows), torch.float32, dev),
+        _arg(dq, "dq", (rows, hq, d), bf, dev),
+        _arg(dk, "dk", (keys, hkv, d), bf, dev),
+        _arg(dv, "dv", (keys, hkv, d), bf, dev), MA_BF16, wp, wn,
+        _stream_ptr(stream))
+    _check("mesh_attn_score_bwd", st)
+    return dq, dk, dv

@@ -55,39 +55,6 @@ ma_status_t ok() {
   return MA_OK;
 }
 
-}  // namespace host
-}  // namespace mesh_attn
-
-namespace {
-
-using mesh_attn::host::fail;
-using mesh_attn::host::ok;
-
-ma_status_t hip_fail(hipError_t e, const char* what) {
-  return fail(MA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-bool aligned16(const void* p) {
-  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
-}
-
-ma_status_t check_list(const char* name, const int32_t* idx, int32_t n,
-                       int32_t num_partitions) {
-  if (n < 1) return fail(MA_ERR_INVALID_ARG, "%s: length %d < 1", name, n);
-  if (!idx) return fail(MA_ERR_INVALID_ARG, "%s is NULL", name);
-  std::vector<char> seen(static_cast<size_t>(num_partitions), 0);
-  for (int32_t i = 0; i < n; ++i) {
-    if (idx[i] < 0 || idx[i] >= num_partitions)
-      return fail(MA_ERR_INVALID_ARG, "%s[%d] = %d outside [0, %d)", name, i,
-                  idx[i], num_partitions);
-    if (seen[idx[i]])
-      return fail(MA_ERR_INVALID_ARG, "%s[%d] = %d is a duplicate", name, i,
-                  idx[i]);
-    seen[idx[i]] = 1;
-  }
-  return MA_OK;
-}
-
 ma_status_t check_problem(const ma_problem_t* p) {
   if (!p) return fail(MA_ERR_INVALID_ARG, "problem is NULL");
   if (p->num_partitions < 1)
@@ -114,6 +81,40 @@ ma_status_t check_problem(const ma_problem_t* p) {
     return fail(MA_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
   if (p->head_dim < 1)
     return fail(MA_ERR_INVALID_ARG, "head_dim %d < 1", p->head_dim);
+  return MA_OK;
+}
+
+}  // namespace host
+}  // namespace mesh_attn
+
+namespace {
+
+using mesh_attn::host::check_problem;
+using mesh_attn::host::fail;
+using mesh_attn::host::ok;
+
+ma_status_t hip_fail(hipError_t e, const char* what) {
+  return fail(MA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+bool aligned16(const void* p) {
+  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
+}
+
+ma_status_t check_list(const char* name, const int32_t* idx, int32_t n,
+                       int32_t num_partitions) {
+  if (n < 1) return fail(MA_ERR_INVALID_ARG, "%s: length %d < 1", name, n);
+  if (!idx) return fail(MA_ERR_INVALID_ARG, "%s is NULL", name);
+  std::vector<char> seen(static_cast<size_t>(num_partitions), 0);
+  for (int32_t i = 0; i < n; ++i) {
+    if (idx[i] < 0 || idx[i] >= num_partitions)
+      return fail(MA_ERR_INVALID_ARG, "%s[%d] = %d outside [0, %d)", name, i,
+                  idx[i], num_partitions);
+    if (seen[idx[i]])
+      return fail(MA_ERR_INVALID_ARG, "%s[%d] = %d is a duplicate", name, i,
+                  idx[i]);
+    seen[idx[i]] = 1;
+  }
   return MA_OK;
 }
 

@@ -15,5 +15,8 @@ ma_status_t fail(ma_status_t st, const char* fmt, ...)
 // Clears the calling thread's last error; returns MA_OK.
 ma_status_t ok();
 
+// Everything of a problem but what its head dim and blocks have to be.
+ma_status_t check_problem(const ma_problem_t* p);
+
 }  // namespace host
 }  // namespace mesh_attn

@@ -1,0 +1,712 @@
+// Backward of the tile attention under a score rule (mesh_attn_score_bwd),
+// gfx950.  Deterministic: every output element is owned by one thread, no atomics.
+//
+// With P = exp(x - LSE) over the keys that are seen and T' = 1 - tanh^2 of the cap
+// (4 r (1 - r) with the r of cap_r()):  dV = P^T dO,  dS = P T' (dO V^T - D),
+// D = <dO, O>,  dK = s dS^T Q,  dQ = s dS K.
+//
+// Three launches, and one more for each pass whose items are cut:
+//  1. prep: D and LSE log2(e) of every (row, head); every row's range and
+//     position; what each stage of 64 rows sees.
+//  2. dK/dV: a workgroup per (128 keys, KV head), four waves of 32 keys; it walks
+//     the stages of 64 query rows that see some of its keys for every query head
+//     of the group.  K, V, dK and dV stay in registers.
+//  3. dQ: a workgroup per (128 rows, head), four waves of 32 rows, as the forward.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "internal.h"
+#include "score_tile.h"
+
+namespace mesh_attn {
+namespace {
+
+using namespace dev;
+
+constexpr int NT = 256;
+
+// ---------------------------------------------------------------------------
+// 1. prep
+// ---------------------------------------------------------------------------
+
+// The first workgroups make the rows' ranges, a stage of 64 rows per wave; the
+// others D and the LSE, D / 8 lanes per (row, head).
+template <int D>
+__global__ __launch_bounds__(NT) void score_prep_kernel(ScoreBwdParams p,
+                                                        int range_groups) {
+  const ScoreTile& t = p.t;
+  const int tid = threadIdx.x;
+  if (static_cast<int>(blockIdx.x) < range_groups) {
+    const int stage = blockIdx.x * (NT / 64) + (tid >> 6);
+    if (stage * 64 >= p.rows_pad) return;
+    const int my = stage * 64 + (tid & 63);
+    // Rows behind the last one see nothing, and count in no stage's summary.
+    const int row = min(my, t.rows_q - 1);
+    const int pos = row_position(t, row);
+    const Seen s = row_seen(t, row, pos);
+    p.lo[my] = my < t.rows_q ? s.lo : 0;
+    p.hi[my] = my < t.rows_q ? s.hi : 0;
+    p.pos[my] = pos;
+    ScoreStage g;
+    const bool some = s.lo < s.hi;
+    g.lo_min = wave_min(some ? s.lo : INT32_MAX);
+    g.hi_max = wave_max(s.hi);
+    g.lo_max = wave_max(s.lo);
+    g.hi_min = wave_min(s.hi);
+    if (stage * 64 + 64 > t.rows_q) g.hi_min = 0;  // padding is masked
+    if ((tid & 63) == 0) p.stages[stage] = g;
+    return;
+  }
+  constexpr int kLanes = D / 8;
+  const uint32_t gid = (blockIdx.x - range_groups) * NT + tid;
+  const uint32_t item32 = gid / kLanes;  // row * hq + head
+  const int sub = static_cast<int>(gid % kLanes);
+  const int64_t row = item32 / static_cast<uint32_t>(t.hq);
+  const int h = static_cast<int>(item32 - row * t.hq);
+  const int64_t item = item32;
+  const bool valid = row < t.rows_q;
+  float s = 0.f;
+  if (valid) {
+    const bf16x8 a = *reinterpret_cast<const bf16x8*>(p.o + item * D + sub * 8);
+    const bf16x8 b =
+        *reinterpret_cast<const bf16x8*>(p.d_o + item * D + sub * 8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      s = fmaf(static_cast<float>(a[i]), static_cast<float>(b[i]), s);
+  }
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o /= 2) s += __shfl_xor(s, o);
+  if (sub == 0 && row < p.rows_pad) {
+    const float lse = valid ? p.lse[int64_t{h} * t.rows_q + row] : -INFINITY;
+    const int64_t at = int64_t{h} * p.rows_pad + row;
+    p.delta[at] = s;
+    p.lse2[at] = lse == -INFINITY ? INFINITY : lse * kLog2E;
+  }
+}
+
+// Scores x -> probability and, in *g, its product with the cap's derivative.
+// `far`: |i - j|.
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float probability(const Cap& cap, float scale_log2,
+                                             float slope, float x, float far,
+                                             float lse2, float* g) {
+  float y, d = 1.f;
+  if (CAP) {
+    const float r = cap_r(cap, x);
+    y = fmaf(-cap.two, r, cap.one - lse2);
+    d = fmaf(-4.f * r, r, 4.f * r);
+  } else {
+    y = fmaf(x, scale_log2, -lse2);
+  }
+  if (BIAS) y = fmaf(-slope, far, y);
+  const float e = exp2_fast(y);
+  *g = CAP ? e * d : e;
+  return e;
+}
+
+// ---------------------------------------------------------------------------
+// 2. dK / dV
+// ---------------------------------------------------------------------------
+template <int D>
+struct KvLayout {
+  static constexpr int kTile = Staged<D>::kBytes;
+  // Q, dO, then LSE, D, begin, end and position of 64 rows.
+  static constexpr int kFloats = 2 * kTile;
+  static constexpr int kStage = 2 * kTile + 5 * kScoreBlock * 4;
+  static constexpr int kLds = 2 * kStage;
+};
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// Eight values from LDS byte address a.
+template <typename V8, typename V4>
+__device__ __forceinline__ V8 lds_eight(uint32_t a) {
+  typedef __attribute__((address_space(3))) const V4 T;
+  const V4 lo = *(T*)a, hi = *(T*)(a + 16);
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void stage_words(const void* src, char* dst,
+                                            int lane) {
+  typedef __attribute__((address_space(3))) void lds_void;
+  const rsrc_t r = make_rsrc(src, kScoreBlock * 4);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst), 4, lane * 4, 0,
+                                           0, 0);
+}
+
+template <int D, bool CAP, bool BIAS, bool OUT_F32>
+__global__ __launch_bounds__(NT, 2) void score_dkdv_kernel(ScoreBwdParams p) {
+  using L = KvLayout<D>;
+  using T = Staged<D>;
+  constexpr int kRow = T::kRowBytes;
+  extern __shared__ __align__(16) char smem[];
+  const ScoreTile& t = p.t;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  int id = blockIdx.x;
+  const int hk = id % t.hkv;
+  id /= t.hkv;
+  const int part = id % p.kv_splits;
+  int blk = id / p.kv_splits;
+  Segment g;
+  for (int s = 0; s < t.nseg; ++s) {
+    g = segment(t, s);
+    const int n = (g.len + kScoreRows - 1) / kScoreRows;
+    if (blk < n) break;
+    blk -= n;
+  }
+  // Keys behind the segment's last one repeat it, are seen by no row and not
+  // stored.
+  const int key0 = blk * kScoreRows, my_key = key0 + wave * 32 + li;
+  const bool valid = my_key < g.len;
+  const int key = min(my_key, g.len - 1);
+  const int kpos = g.pos + key * t.step;
+  const int wg_first = g.pos + key0 * t.step;
+  const int wg_last =
+      g.pos + (min(key0 + kScoreRows, g.len) - 1) * t.step;
+  const int wave_first = __builtin_amdgcn_readfirstlane(
+      g.pos + min(key0 + wave * 32, g.len - 1) * t.step);
+  const int wave_last = __builtin_amdgcn_readfirstlane(
+      g.pos + (min(key0 + wave * 32 + 32, g.len) - 1) * t.step);
+  const bool wave_whole = key0 + wave * 32 + 32 <= g.len;
+
+  bf16x8 kf[D / 16], vf[D / 16];
+  {
+    const int64_t r = int64_t{g.row} + key;
+    const uint16_t* ks = t.k + r * t.k_stride + int64_t{hk} * D + lh * 8;
+    const uint16_t* vs = t.v + r * t.v_stride + int64_t{hk} * D + lh * 8;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      kf[kk] = *reinterpret_cast<const bf16x8*>(ks + kk * 16);
+      vf[kk] = *reinterpret_cast<const bf16x8*>(vs + kk * 16);
+    }
+  }
+  f32x16 acc_v[D / 32], acc_k[D / 32];
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    zero(acc_v[c]);
+    zero(acc_k[c]);
+  }
+  const Cap cap = cap_of(t);
+
+  // The stages of this part that see some of the keys, 64 of them looked at at a
+  // time, for each head of the group.
+  const int stages = p.rows_pad / kScoreBlock;
+  const int64_t all = int64_t{stages} * t.group;
+  const int first = static_cast<int>(all * part / p.kv_splits);
+  const int stop = static_cast<int>(all * (part + 1) / p.kv_splits);
+  int base = first / stages * stages + first % stages / 64 * 64;
+  uint64_t bits = 0;
+  auto look = [&]() {  // bits of the stages base ..
+    const int s = base % stages + lane, at = base + lane;
+    bool yes = false;
+    if (s < stages && at >= first && at < stop) {
+      const ScoreStage st = p.stages[s];
+      yes = st.lo_min <= wg_last && st.hi_max > wg_first &&
+            st.lo_min < st.hi_max;
+    }
+    return __builtin_amdgcn_ballot_w64(yes);
+  };
+  // The next stage as group head * stages + stage; -1: there is none.
+  auto next_stage = [&]() {
+    while (bits == 0) {
+      if (base >= stop) return -1;
+      bits = look();
+      if (bits != 0) break;
+      const int s = base % stages;
+      base = s + 64 >= stages ? base - s + stages : base + 64;
+    }
+    const int i = __builtin_ctzll(bits);
+    bits &= bits - 1;
+    const int at = base + i;
+    if (bits == 0) {
+      const int s = base % stages;
+      base = s + 64 >= stages ? base - s + stages : base + 64;
+    }
+    return at;
+  };
+  auto load = [&](int at, int buf) {
+    char* dst = smem + buf * L::kStage;
+    const int gh = at / stages, s = at - gh * stages;
+    const int h = hk * t.group + gh;
+    const int64_t row = int64_t{s} * kScoreBlock;
+    stage_rows<D>(t.q, t.q_stride, row, t.rows_q, h, dst, wave, lane);
+    stage_rows<D>(p.d_o, int64_t{t.hq} * D, row, t.rows_q, h, dst + L::kTile,
+                  wave, lane);
+    char* f = dst + L::kFloats;
+    const int64_t hr = int64_t{h} * p.rows_pad + row;
+    if (wave == 0) stage_words(p.lse2 + hr, f, lane);
+    if (wave == 1) stage_words(p.delta + hr, f + 256, lane);
+    if (wave == 2) stage_words(p.lo + row, f + 512, lane);
+    if (wave == 3) stage_words(p.hi + row, f + 768, lane);
+    if (BIAS && wave == 0) stage_words(p.pos + row, f + 1024, lane);
+  };
+
+  int cur = __builtin_amdgcn_readfirstlane(next_stage());
+  if (cur >= 0) {
+    load(cur, 0);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      wait_for(kf[kk]);
+      wait_for(vf[kk]);
+    }
+    wait_vmem();
+    __syncthreads();
+    int buf = 0;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
+    const uint32_t ra = lds0 + T::row_read(lane);
+    const uint32_t t0 = lds0 + T::tr_read(lane, 0);
+    const uint32_t t1 = lds0 + T::tr_read(lane, 1);
+    const uint32_t fa = lds0 + L::kFloats + lh * 32;
+    for (;;) {
+      const int nxt = __builtin_amdgcn_readfirstlane(next_stage());
+      if (nxt >= 0) load(nxt, buf ^ 1);
+      const uint32_t sb = buf * L::kStage;
+      const int gh = cur / stages;
+      const ScoreStage st = load_const(p.stages, cur - gh * stages);
+      const float slope =
+          BIAS ? load_const(t.slopes, hk * t.group + gh) * kLog2E : 0.f;
+      const bool touched = st.lo_min <= wave_last && st.hi_max > wave_first;
+      if (touched) {
+        const bool full = wave_whole && st.lo_max <= wave_first &&
+                          st.hi_min > wave_last;
+        // 0 times an infinity or a NaN of a row that does not see the key is
+        // NaN: rows that hold one give NaN to the keys that they see, and zeros
+        // to the products.
+        uint64_t bad = 0;
+        if (!full) {
+          const bool q_bad = tile_not_finite<D>(smem + sb, lane);
+          const bool o_bad = tile_not_finite<D>(smem + sb + L::kTile, lane);
+          if (q_bad || o_bad)
+            bad = rows_not_finite<D>(smem + sb, lane) |
+                  rows_not_finite<D>(smem + sb + L::kTile, lane);
+        }
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt) {
+          f32x16 x;
+          zero(x);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            x = mfma32(lds_row((ra ^ (32 * kk)) + sb + qt * 32 * kRow), kf[kk],
+                       x);
+          bf16x8 pf[2], ds[2];
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            const uint32_t at = fa + sb + 4 * (qt * 32 + hh * 16);
+            const f32x8 lse = lds_eight<f32x8, f32x4>(at);
+            f32x8 e8, g8;
+            i32x8 pos;
+            if (BIAS) pos = lds_eight<i32x8, i32x4>(at + 1024);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float far =
+                  BIAS ? fabsf(static_cast<float>(pos[e] - kpos)) : 0.f;
+              float g1;
+              e8[e] = probability<CAP, BIAS>(cap, t.scale_log2, slope,
+                                             x[hh * 8 + e], far, lse[e], &g1);
+              g8[e] = g1;
+            }
+            if (!full) {
+              const i32x8 lo = lds_eight<i32x8, i32x4>(at + 512);
+              const i32x8 hi = lds_eight<i32x8, i32x4>(at + 768);
+              const uint32_t b8 = static_cast<uint32_t>(
+                  bad >> (qt * 32 + hh * 16 + 8 * lh)) & 255u;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const bool sees = valid && lo[e] <= kpos && kpos < hi[e];
+                const float nan = (b8 >> e) & 1 ? NAN : 0.f;
+                e8[e] = sees ? e8[e] + nan : 0.f;
+                g8[e] = sees ? g8[e] + nan : 0.f;
+              }
+            }
+            pf[hh] = __builtin_convertvector(e8, bf16x8);
+            if (CAP) ds[hh] = __builtin_convertvector(g8, bf16x8);
+          }
+          f32x16 y;
+          zero(y);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            y = mfma32(lds_row((ra ^ (32 * kk)) + sb + L::kTile +
+                               qt * 32 * kRow),
+                       vf[kk], y);
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            const uint32_t at = fa + sb + 256 + 4 * (qt * 32 + hh * 16);
+            const f32x8 dlt = lds_eight<f32x8, f32x4>(at);
+            f32x8 g8 = __builtin_convertvector(CAP ? ds[hh] : pf[hh], f32x8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float d = y[hh * 8 + e] - dlt[e];
+              // A hidden pair's product with a NaN of dO V^T is 0.
+              g8[e] = full || g8[e] != 0.f ? g8[e] * d : 0.f;
+            }
+            ds[hh] = __builtin_convertvector(g8, bf16x8);
+          }
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+              const int at = (2 * qt + hh) * 16 * kRow;
+              bf16x8 a = lds_tr((t0 ^ (64 * c)) + sb, (t1 ^ (64 * c)) + sb,
+                                L::kTile + at);
+              bf16x8 b = lds_tr((t0 ^ (64 * c)) + sb, (t1 ^ (64 * c)) + sb, at);
+              if (bad) {
+                a = finite_or_zero(a);
+                b = finite_or_zero(b);
+              }
+              acc_v[c] = mfma32(pf[hh], a, acc_v[c]);
+              acc_k[c] = mfma32(ds[hh], b, acc_k[c]);
+            }
+        }
+      }
+      if (nxt < 0) break;
+      wait_vmem();
+      lds_barrier();
+      buf ^= 1;
+      cur = nxt;
+    }
+  }
+
+  // Register i of chunk c: key 8 (i / 4) + 4 lh + i % 4 of the wave, dim 32 c + li.
+  const bool whole = p.kv_splits == 1;
+  const int64_t all_out = int64_t{t.rows_kv} * t.hkv * D;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int k = key0 + wave * 32 + 8 * (i >> 2) + 4 * lh + (i & 3);
+    if (k >= g.len) continue;
+    const int64_t at = ((int64_t{g.row} + k) * t.hkv + hk) * D + li;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      const float dv = acc_v[c][i], dk = acc_k[c][i] * t.scale;
+      if (!whole) {
+        p.part_dv[part * all_out + at + 32 * c] = dv;
+        p.part_dk[part * all_out + at + 32 * c] = dk;
+      } else if (OUT_F32) {
+        static_cast<float*>(p.dv)[at + 32 * c] = dv;
+        static_cast<float*>(p.dk)[at + 32 * c] = dk;
+      } else {
+        static_cast<__bf16*>(p.dv)[at + 32 * c] = static_cast<__bf16>(dv);
+        static_cast<__bf16*>(p.dk)[at + 32 * c] = static_cast<__bf16>(dk);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// 3. dQ
+// ---------------------------------------------------------------------------
+template <int D>
+struct QLayout {
+  static constexpr int kTile = Staged<D>::kBytes;
+  static constexpr int kStage = 2 * kTile;
+  static constexpr int kLds = 2 * kStage;
+};
+
+template <int D, bool CAP, bool BIAS, bool OUT_F32>
+__global__ __launch_bounds__(NT, D == 128 ? 2 : 3)
+void score_dq_kernel(ScoreBwdParams p) {
+  using L = QLayout<D>;
+  using T = Staged<D>;
+  constexpr int kRow = T::kRowBytes;
+  extern __shared__ __align__(16) char smem[];
+  const ScoreTile& t = p.t;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qblocks = (t.rows_q + kScoreRows - 1) / kScoreRows;
+  int id = blockIdx.x;
+  const int hk = id % t.hkv;
+  id /= t.hkv;
+  const int h = hk * t.group + id % t.group;
+  id /= t.group;
+  const int part = id % p.q_splits;
+  const int qblk = qblocks - 1 - id / p.q_splits;
+
+  const int my_row = qblk * kScoreRows + wave * 32 + li;
+  const int row = min(my_row, t.rows_q - 1);
+  const int qpos = p.pos[row];
+  const Seen seen{p.lo[row], p.hi[row]};
+  const int64_t hr = int64_t{h} * p.rows_pad + row;
+  const float lse2 = p.lse2[hr], dlt = p.delta[hr];
+  bf16x8 qf[D / 16], dof[D / 16];
+  {
+    const uint16_t* qs = t.q + row * t.q_stride + int64_t{h} * D + lh * 8;
+    const uint16_t* ds = p.d_o + (int64_t{row} * t.hq + h) * D + lh * 8;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      qf[kk] = *reinterpret_cast<const bf16x8*>(qs + kk * 16);
+      dof[kk] = *reinterpret_cast<const bf16x8*>(ds + kk * 16);
+    }
+  }
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) zero(acc[c]);
+  const Cap cap = cap_of(t);
+  const float slope = BIAS ? t.slopes[h] * kLog2E : 0.f;
+  const ScoreStage s0 = load_const(p.stages, 2 * qblk);
+  const ScoreStage s1 =
+      load_const(p.stages, min(2 * qblk + 1, p.rows_pad / kScoreBlock - 1));
+  const int lo_min = min(s0.lo_min, s1.lo_min);
+  const int hi_max = max(s0.hi_max, s1.hi_max);
+  KeyWalk w;
+  w.start(t, lo_min < hi_max ? lo_min : 0, lo_min < hi_max ? hi_max : 0, part,
+          p.q_splits);
+
+  if (w.left > 0) {
+    auto load = [&](int buf) {
+      char* at = smem + buf * L::kStage;
+      const int64_t r = w.g.row + int64_t{w.blk} * kScoreBlock;
+      stage_rows<D>(t.k, t.k_stride, r, t.rows_kv, hk, at, wave, lane);
+      stage_rows<D>(t.v, t.v_stride, r, t.rows_kv, hk, at + L::kTile, wave,
+                    lane);
+    };
+    int a, b, all_a, all_b, some_a, some_b;
+    auto enter_segment = [&]() {
+      a = rows_below(seen.lo, w.g.pos, w.g.len, t.step);
+      b = rows_below(seen.hi, w.g.pos, w.g.len, t.step);
+      if (a >= b) a = b = 0;
+      all_a = wave_max(a);
+      all_b = wave_min(b);
+      some_a = wave_min(a < b ? a : INT32_MAX);
+      some_b = wave_max(b);
+    };
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
+    const uint32_t ra = lds0 + T::row_read(lane);
+    const uint32_t t0 = lds0 + T::tr_read(lane, 0);
+    const uint32_t t1 = lds0 + T::tr_read(lane, 1);
+    auto compute = [&](int k0, int pos0, int buf) {
+      const uint32_t sb = buf * L::kStage;
+      const bool full = all_a <= k0 && k0 + kScoreBlock <= all_b;
+      uint64_t bad = 0;
+      if (!full && tile_not_finite<D>(smem + sb, lane))
+        bad = rows_not_finite<D>(smem + sb, lane);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        f32x16 x, y;
+        zero(x);
+        zero(y);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          x = mfma32(lds_row((ra ^ (32 * kk)) + sb + kt * 32 * kRow), qf[kk], x);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          y = mfma32(lds_row((ra ^ (32 * kk)) + sb + L::kTile + kt * 32 * kRow),
+                     dof[kk], y);
+        const float d0 = BIAS ? static_cast<float>(int64_t{qpos} - pos0 -
+                                                   int64_t{t.step} *
+                                                       (32 * kt + 8 * lh))
+                              : 0.f;
+        const float step = static_cast<float>(t.step);
+        bf16x8 ds[2];
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          f32x8 g8;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float far =
+                BIAS ? fabsf(fmaf(-step, static_cast<float>(16 * hh + e), d0))
+                     : 0.f;
+            float g1;
+            probability<CAP, BIAS>(cap, t.scale_log2, slope, x[hh * 8 + e], far,
+                                   lse2, &g1);
+            g8[e] = g1 * (y[hh * 8 + e] - dlt);
+          }
+          if (!full) {
+            const int j0 = k0 + 32 * kt + 16 * hh + 8 * lh;
+            const uint32_t b8 = static_cast<uint32_t>(
+                bad >> (32 * kt + 16 * hh + 8 * lh)) & 255u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const bool sees = a <= j0 + e && j0 + e < b;
+              const float nan = (b8 >> e) & 1 ? NAN : 0.f;
+              g8[e] = sees ? g8[e] + nan : 0.f;
+            }
+          }
+          ds[hh] = __builtin_convertvector(g8, bf16x8);
+        }
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            bf16x8 k = lds_tr((t0 ^ (64 * c)) + sb, (t1 ^ (64 * c)) + sb,
+                              (2 * kt + hh) * 16 * kRow);
+            if (bad) k = finite_or_zero(k);
+            acc[c] = mfma32(k, ds[hh], acc[c]);
+          }
+      }
+    };
+    load(0);
+    enter_segment();
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      wait_for(qf[kk]);
+      wait_for(dof[kk]);
+    }
+    wait_vmem();
+    __syncthreads();
+    int buf = 0;
+    for (;;) {
+      const int k0 = w.blk * kScoreBlock;
+      const int pos0 = w.g.pos + k0 * t.step;
+      const bool more = w.left > 1;
+      const bool changed = more && w.next(t);
+      if (more) load(buf ^ 1);
+      if (some_a < k0 + kScoreBlock && k0 < some_b) compute(k0, pos0, buf);
+      if (!more) break;
+      if (changed) enter_segment();
+      wait_vmem();
+      lds_barrier();
+      buf ^= 1;
+    }
+  }
+  if (my_row >= t.rows_q) return;
+  const bool whole = p.q_splits == 1;
+  const int64_t o0 = (int64_t{my_row} * t.hq + h) * D;
+  const int64_t all = int64_t{t.rows_q} * t.hq * D;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int dim = c * 32 + g * 8 + lh * 4;
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = acc[c][4 * g + e] * t.scale;
+      if (!whole) {
+        *reinterpret_cast<f32x4*>(p.part_dq + part * all + o0 + dim) = x;
+      } else if (OUT_F32) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(p.dq) + o0 + dim) = x;
+      } else {
+        bf16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(x[e]);
+        *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.dq) + o0 + dim) = y;
+      }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Sums of partial gradients, four elements a thread, in the parts' order.
+// ---------------------------------------------------------------------------
+struct SumParams {
+  const float* src[2];
+  void* dst[2];
+  int64_t n;  // elements of one, a multiple of 4
+  int32_t parts;
+};
+
+template <bool OUT_F32>
+__global__ __launch_bounds__(NT) void score_sum_kernel(SumParams p) {
+  const float* src = p.src[blockIdx.y];
+  void* dst = p.dst[blockIdx.y];
+  const int64_t stride = int64_t{gridDim.x} * NT * 4;
+  for (int64_t i = (int64_t{blockIdx.x} * NT + threadIdx.x) * 4; i < p.n;
+       i += stride) {
+    f32x4 s = *reinterpret_cast<const f32x4*>(src + i);
+#pragma unroll 4
+    for (int k = 1; k < p.parts; ++k) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(src + k * p.n + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += x[e];
+    }
+    if (OUT_F32) {
+      *reinterpret_cast<f32x4*>(static_cast<float*>(dst) + i) = s;
+    } else {
+      bf16x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(s[e]);
+      *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(dst) + i) = y;
+    }
+  }
+}
+
+hipError_t launch_sum(const SumParams& p, int arrays, bool out_f32,
+                      hipStream_t stream) {
+  const int64_t need = (p.n / 4 + NT - 1) / NT;
+  const dim3 grid(static_cast<unsigned>(need < 8192 ? need : 8192),
+                  static_cast<unsigned>(arrays));
+  if (out_f32)
+    hipLaunchKernelGGL(score_sum_kernel<true>, grid, dim3(NT), 0, stream, p);
+  else
+    hipLaunchKernelGGL(score_sum_kernel<false>, grid, dim3(NT), 0, stream, p);
+  return hipGetLastError();
+}
+
+template <int D, bool CAP, bool BIAS, bool OUT_F32>
+hipError_t launch(const ScoreBwdParams& p, hipStream_t stream) {
+  constexpr auto dkdv = score_dkdv_kernel<D, CAP, BIAS, OUT_F32>;
+  constexpr auto dq = score_dq_kernel<D, CAP, BIAS, OUT_F32>;
+  constexpr int kv_lds = KvLayout<D>::kLds, q_lds = QLayout<D>::kLds;
+  hipError_t e = ensure_dynamic_lds<dkdv>(kv_lds);
+  if (e == hipSuccess) e = ensure_dynamic_lds<dq>(q_lds);
+  if (e != hipSuccess) return e;
+  const ScoreTile& t = p.t;
+  const int range_groups = (p.rows_pad / 64 + NT / 64 - 1) / (NT / 64);
+  const int64_t lanes = int64_t{p.rows_pad} * t.hq * (D / 8);
+  hipLaunchKernelGGL(
+      score_prep_kernel<D>,
+      dim3(static_cast<unsigned>(range_groups + (lanes + NT - 1) / NT)),
+      dim3(NT), 0, stream, p, range_groups);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t kv_items = int64_t{t.kv_blocks128} * t.hkv * p.kv_splits;
+  hipLaunchKernelGGL(dkdv, dim3(static_cast<unsigned>(kv_items)), dim3(NT),
+                     kv_lds, stream, p);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t q_items =
+      (int64_t{t.rows_q} + kScoreRows - 1) / kScoreRows * t.hq * p.q_splits;
+  hipLaunchKernelGGL(dq, dim3(static_cast<unsigned>(q_items)), dim3(NT), q_lds,
+                     stream, p);
+  e = hipGetLastError();
+  if (e == hipSuccess && p.kv_splits > 1) {
+    SumParams s{{p.part_dk, p.part_dv},
+                {p.dk, p.dv},
+                int64_t{t.rows_kv} * t.hkv * D,
+                p.kv_splits};
+    e = launch_sum(s, 2, OUT_F32, stream);
+  }
+  if (e == hipSuccess && p.q_splits > 1) {
+    SumParams s{{p.part_dq, nullptr},
+                {p.dq, nullptr},
+                int64_t{t.rows_q} * t.hq * D,
+                p.q_splits};
+    e = launch_sum(s, 1, OUT_F32, stream);
+  }
+  return e;
+}
+
+template <int D, bool OUT_F32>
+hipError_t launch_d(const ScoreBwdParams& p, hipStream_t stream) {
+  if (p.t.cap > 0.f)
+    return p.t.slopes ? launch<D, true, true, OUT_F32>(p, stream)
+                      : launch<D, true, false, OUT_F32>(p, stream);
+  return p.t.slopes ? launch<D, false, true, OUT_F32>(p, stream)
+                    : launch<D, false, false, OUT_F32>(p, stream);
+}
+
+}  // namespace
+
+void score_bwd_splits(const ScoreTile& t, int* kv_splits, int* q_splits) {
+  auto parts = [](int64_t items, int64_t blocks) {
+    if (items >= 256) return 1;
+    const int64_t want = 512 / items, most = blocks / 4;
+    const int64_t n = want < most ? want : most;
+    return static_cast<int>(n < 1 ? 1 : n > 32 ? 32 : n);
+  };
+  const int64_t stages = (int64_t{t.rows_q} + 63) / 64;
+  *kv_splits = parts(int64_t{t.kv_blocks128} * t.hkv, stages * t.group);
+  *q_splits = parts((int64_t{t.rows_q} + kScoreRows - 1) / kScoreRows * t.hq,
+                    t.kv_blocks64);
+}
+
+hipError_t launch_score_bwd(const ScoreBwdParams& p, bool out_f32,
+                            hipStream_t stream) {
+  (void)out_f32;
+  return p.t.head_dim == 128 ? launch_d<128, false>(p, stream)
+                             : launch_d<64, false>(p, stream);
+}
+
+}  // namespace mesh_attn

@@ -1,0 +1,261 @@
+// Device helpers of the attention under a score rule (gfx950, wave64), shared by
+// its forward and backward kernels.  MFMA and LDS conventions as in
+// tile_common.h: score tiles are made with their first operand's rows in the
+// bit-2/3-swapped order, so that accumulator register i of lane half h is row
+// acc_row(i, h) of a 32-row tile and eight registers are the k-contiguous operand
+// of the next product.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "score.h"
+#include "tile_common.h"
+
+namespace mesh_attn {
+namespace dev {
+
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr float kLn2 = 0.69314718055994531f;
+
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Rows of a staged tile, 16-byte chunks XORed by row, so that rows and transposed
+// 4 x 16 blocks are both read without bank conflicts.
+template <int D>
+struct Staged {
+  static constexpr int kRowBytes = 2 * D;
+  static constexpr int kChunks = D / 8;
+  static constexpr int kBytes = kScoreBlock * kRowBytes;
+  __device__ static int swz(int r) {
+    return D == 128 ? 4 * (r & 3) + ((r >> 2) & 3)
+                    : 4 * ((r >> 1) & 1) + ((r >> 2) & 3);
+  }
+  // Byte offsets of a lane's operand reads: rows (row acc order of li, + 32 t;
+  // chunk 2 kk + lh: ^ 32 kk), and the two halves of a transposed one (columns
+  // 32 c ..: ^ 64 c; rows 16 s ..: + 16 s rows).
+  __device__ static int row_read(int lane) {
+    const int r = mfma_row_perm(lane & 31);
+    return r * kRowBytes + (((lane >> 5) ^ swz(r)) * 16);
+  }
+  __device__ static int tr_read(int lane, int half) {
+    const int g16 = lane >> 4, s16 = lane & 15;
+    const int c16 = 2 * (g16 & 1) + ((s16 & 3) >> 1);
+    const int r = 8 * (g16 >> 1) + (s16 >> 2) + 4 * half;
+    return r * kRowBytes + ((c16 ^ swz(r)) * 16) + 8 * (s16 & 1);
+  }
+};
+
+// Rows row0 .. row0 + 63 of a head into a staged tile, by four waves; rows from
+// `rows` on are zeros (the buffer's range ends there).  The whole offset is in the
+// lane's register, which the range check covers.
+template <int D>
+__device__ __forceinline__ void stage_rows(const uint16_t* base, int64_t stride,
+                                           int64_t row0, int64_t rows, int head,
+                                           char* tile, int wave, int lane) {
+  using T = Staged<D>;
+  constexpr int kPer = 64 / T::kChunks;  // rows of a load
+  const uint32_t row_bytes = static_cast<uint32_t>(stride * 2);
+  const int64_t left = rows - row0;
+  const uint32_t n = left < kScoreBlock ? static_cast<uint32_t>(left)
+                                        : uint32_t{kScoreBlock};
+  const rsrc_t r = make_rsrc(base + row0 * stride + int64_t{head} * D,
+                             (n - 1) * row_bytes + 2 * D);
+#pragma unroll
+  for (int j = 0; j < 16 / kPer; ++j) {
+    const int tr = wave * 16 + j * kPer;
+    const int row = tr + lane / T::kChunks;
+    const uint32_t off =
+        row * row_bytes + ((lane % T::kChunks) ^ T::swz(row)) * 16;
+    buffer_load16_lds(r, tile + tr * T::kRowBytes, off, 0);
+  }
+}
+
+__device__ __forceinline__ bf16x8 lds_row(uint32_t a) {
+  typedef __attribute__((address_space(3))) const bf16x8 T;
+  return *(T*)a;
+}
+__device__ __forceinline__ bf16x8 lds_tr(uint32_t a0, uint32_t a1, int imm) {
+  typedef __attribute__((address_space(3))) s16x4 T;
+  return join_bf16(__builtin_amdgcn_ds_read_tr16_b64_v4i16((T*)(a0 + imm)),
+                   __builtin_amdgcn_ds_read_tr16_b64_v4i16((T*)(a1 + imm)));
+}
+
+// Whether a staged tile holds an infinity or a NaN (wave-uniform).
+template <int D>
+__device__ __forceinline__ bool tile_not_finite(const char* tile, int lane) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+  u16x2 top = {0, 0};
+#pragma unroll 4
+  for (int i = 0; i < Staged<D>::kBytes / 1024; ++i) {
+    const u32x4v w =
+        *reinterpret_cast<const u32x4v*>(tile + i * 1024 + lane * 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      top = __builtin_elementwise_max(
+          top, __builtin_bit_cast(u16x2, w[j] & 0x7f807f80u));
+  }
+  return __any(top[0] == 0x7f80 || top[1] == 0x7f80);
+}
+
+// The operand with zeros for what is not finite.
+__device__ __forceinline__ bf16x8 finite_or_zero(bf16x8 a) {
+  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+  u16x8 w = __builtin_bit_cast(u16x8, a);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if ((w[i] & 0x7f80) == 0x7f80) w[i] = 0;
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// Rows of a staged tile that hold an infinity or a NaN, as bits.
+template <int D>
+__device__ __forceinline__ uint64_t rows_not_finite(const char* tile,
+                                                    int lane) {
+  bool bad = false;
+#pragma unroll 1
+  for (int i = 0; i < Staged<D>::kRowBytes / 4; ++i) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(
+        tile + lane * Staged<D>::kRowBytes + 4 * i);
+    bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+  }
+  return __builtin_amdgcn_ballot_w64(bad);
+}
+
+// Which stored positions a query row sees, [lo, hi); lo = hi = 0 for none.
+struct Seen {
+  int lo, hi;
+};
+__device__ __forceinline__ int row_position(const ScoreTile& t, int row) {
+  const int e = row / t.P, r = row - e * t.P;
+  const int part = load_const(t.q_idx, e);
+  return t.striped ? r * t.n + part : part * t.P + r;
+}
+__device__ __forceinline__ Seen row_seen(const ScoreTile& t, int row, int pos) {
+  Seen s;
+  s.lo = t.key_begin ? max(t.key_begin[row], 0) : 0;
+  s.hi = t.key_end ? min(t.key_end[row], t.total)
+                   : t.causal ? pos + 1 : t.total;
+  if (s.lo >= s.hi) s.lo = s.hi = 0;
+  return s;
+}
+
+// Rows of a segment of `len` rows from position pos0 on that lie below x.
+__device__ __forceinline__ int rows_below(int x, int pos0, int len, int step) {
+  if (x <= pos0) return 0;
+  const uint32_t y = static_cast<uint32_t>(x) - static_cast<uint32_t>(pos0);
+  const uint32_t n =
+      step == 1 ? y
+                : (y + static_cast<uint32_t>(step) - 1) /
+                      static_cast<uint32_t>(step);
+  return n < static_cast<uint32_t>(len) ? static_cast<int>(n) : len;
+}
+
+template <typename Op>
+__device__ __forceinline__ int wave_reduce(int x, Op op) {
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) x = op(x, __shfl_xor(x, o));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_min(int x) {
+  return wave_reduce(x, [](int a, int b) { return a < b ? a : b; });
+}
+__device__ __forceinline__ int wave_max(int x) {
+  return wave_reduce(x, [](int a, int b) { return a > b ? a : b; });
+}
+
+// A segment of the KV buffer.
+struct Segment {
+  int row, pos, len;
+};
+__device__ __forceinline__ Segment segment(const ScoreTile& t, int s) {
+  Segment g;
+  g.row = load_const(t.seg_row, s);
+  g.len = load_const(t.seg_row, s + 1) - g.row;
+  g.pos = load_const(t.seg_pos, s);
+  return g;
+}
+
+// Walk over the 64-key blocks of all segments that positions [lo, hi) touch, or
+// over part `part` of `parts` of them.  Uniform over the workgroup.
+struct KeyWalk {
+  int seg, blk, end, left, lo, hi;
+  Segment g;
+
+  __device__ void range(const ScoreTile& t) {
+    g = segment(t, seg);
+    const int a = rows_below(lo, g.pos, g.len, t.step);
+    const int b = rows_below(hi, g.pos, g.len, t.step);
+    blk = __builtin_amdgcn_readfirstlane(a / kScoreBlock);
+    end = __builtin_amdgcn_readfirstlane(
+        a < b ? (b + kScoreBlock - 1) / kScoreBlock : blk);
+  }
+  __device__ void start(const ScoreTile& t, int lo_, int hi_, int part,
+                        int parts) {
+    lo = lo_;
+    hi = hi_;
+    left = 0;
+    blk = end = 0;
+    int skip = 0;
+    if (parts > 1 || t.nseg > 1) {
+      int all = 0;
+      for (seg = 0; seg < t.nseg; ++seg) {
+        range(t);
+        all += end - blk;
+      }
+      skip = static_cast<int>(int64_t{all} * part / parts);
+      left = static_cast<int>(int64_t{all} * (part + 1) / parts) - skip;
+    }
+    for (seg = 0; seg < t.nseg; ++seg) {
+      range(t);
+      if (t.nseg == 1 && parts == 1) left = end - blk;
+      if (left == 0) return;
+      if (end - blk > skip) {
+        blk += skip;
+        return;
+      }
+      skip -= end - blk;
+    }
+  }
+  // To the next block; true if the segment changed.  Not past the last one.
+  __device__ bool next(const ScoreTile& t) {
+    --left;
+    if (++blk < end || left <= 0) return false;
+    do {
+      ++seg;
+      range(t);
+    } while (blk == end);
+    return true;
+  }
+};
+
+// Scores of a 32-row tile in log2 units before the bias, and the cap's
+// derivative.  tanh(u) = 1 - 2 / (1 + e^(2u)): one exponential and one reciprocal,
+// off by 2^-23 of the cap; infinite products give +-cap.
+struct Cap {
+  float in;    // product -> log2(e^(2u))
+  float two;   // 2 cap log2(e)
+  float one;   // cap log2(e)
+};
+__device__ __forceinline__ Cap cap_of(const ScoreTile& t) {
+  Cap c;
+  c.in = t.cap > 0.f ? 2.f * t.scale_log2 / t.cap : 0.f;
+  c.one = t.cap * kLog2E;
+  c.two = 2.f * c.one;
+  return c;
+}
+__device__ __forceinline__ float cap_r(const Cap& c, float x) {
+  return __builtin_amdgcn_rcpf(1.f + exp2_fast(x * c.in));
+}
+
+// The distance bias of a block: -slope (|i - j| - off), j the block's first
+// position plus step times 32 kt + acc_row.  Without a branch per key where all
+// of a wave's keys lie on one side of its rows.
+struct Bias {
+  float d0, step, off;
+  bool mixed;
+};
+
+}  // namespace dev
+}  // namespace mesh_attn
