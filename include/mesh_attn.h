@@ -653,6 +653,45 @@ ma_status_t mesh_attn_score_bwd(const ma_problem_t* prob, const int32_t* q_idx,
                                 void* ws, size_t ws_bytes,
                                 hipStream_t stream);
 
+/* mesh_attn_cache_fwd under a score rule (above): new tokens of every request, one
+ * or a whole chunk, over the stored keys.  Arguments and results are
+ * mesh_attn_cache_fwd's, with the rule's arrays indexed by the query rows: row r
+ * at position p_r = positions[r] sees the stored keys at positions in
+ * [key_begin[r], key_end[r]) (without a key_end: up to its own) that lie below
+ * lens[b]; a NULL score is no rule.  No row of a request sees keys before the
+ * key_begin of the request's first row: they are not read, so that a window
+ * costs what it holds.  The workspace is that of mesh_attn_cache_fwd. */
+size_t mesh_attn_cache_score_fwd_workspace_size(const ma_cache_t* cache,
+                                                int32_t num_q_heads,
+                                                int32_t num_requests,
+                                                int64_t rows);
+ma_status_t mesh_attn_cache_score_fwd(
+    const ma_cache_t* cache, int32_t num_q_heads, float softmax_scale,
+    const ma_score_t* score, int32_t num_requests, int64_t rows, const void* q,
+    int64_t q_stride, const int32_t* positions, const int32_t* cu_new,
+    const int32_t* lens, const int32_t* block_table, const void* data, void* o,
+    ma_dtype_t o_dtype, float* lse, void* ws, size_t ws_bytes,
+    hipStream_t stream);
+
+/* mesh_attn_rope on Q and K and mesh_attn_cache_append of the rotated K and V in
+ * one call: what a prompt or a decode step does with its new tokens.
+ *   q, q_out   as in mesh_attn_rope, bf16, with the same results (q_out may be q
+ *              with the same stride, and must not overlap q, k or v otherwise).
+ *   k, v       [rows][Hkv][d] bf16, row strides in elements, as in
+ *              mesh_attn_cache_append; not changed.
+ *   slots, data  as there.
+ * The rotated K goes from its angles in float64 to 4 bits without a rounding in
+ * between, so that a stored value is the nearest to the exact one; values next to
+ * the border of two may differ from those of the two calls, which round K to bf16
+ * first.  rope->head_dim is the cache's; rows whose slot is out of range are
+ * rotated, not stored. */
+ma_status_t mesh_attn_cache_rope_append(
+    const ma_cache_t* cache, const ma_rope_t* rope, int64_t rows,
+    const int32_t* positions, int32_t q_heads, const void* q, int64_t q_stride,
+    void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride,
+    const void* v, int64_t v_stride, const int64_t* slots, void* data,
+    hipStream_t stream);
+
 /* Text of the last non-OK status returned on the calling thread ("" if none).
  * The pointer stays valid until the next library call on that thread. */
 const char* mesh_attn_last_error(void);

@@ -240,6 +240,14 @@ _SIGNATURES = {
     "mesh_attn_score_bwd": (_i32, [_PROB, _I32P, _i32, _I32P, _i32, _SCORE, _p,
                                    _i64, _p, _i64, _p, _i64, _p, _p, _p, _p,
                                    _p, _p, _i32, _p, _sz, _p]),
+    "mesh_attn_cache_score_fwd_workspace_size": (_sz, [_CACHE, _i32, _i32,
+                                                       _i64]),
+    "mesh_attn_cache_score_fwd": (_i32, [_CACHE, _i32, ctypes.c_float, _SCORE,
+                                         _i32, _i64, _p, _i64, _p, _p, _p, _p,
+                                         _p, _p, _i32, _p, _p, _sz, _p]),
+    "mesh_attn_cache_rope_append": (_i32, [_CACHE, ctypes.POINTER(Rope), _i64,
+                                           _p, _i32, _p, _i64, _p, _i64, _p,
+                                           _i64, _p, _i64, _p, _p, _p]),
     "mesh_attn_last_error": (ctypes.c_char_p, []),
 }
 
@@ -944,3 +952,74 @@ def mesh_attn_score_bwd(prob, q_idx, kv_idx, score, q, k, v, o, d_o, lse, dq,
         _stream_ptr(stream))
     _check("mesh_attn_score_bwd", st)
     return dq, dk, dv
+
+
+def mesh_attn_cache_score_fwd_workspace_size(cache, num_q_heads, num_requests,
+                                             rows):
+    return int(load_library().mesh_attn_cache_score_fwd_workspace_size(
+        ctypes.byref(Cache.make(cache)), int(num_q_heads), int(num_requests),
+        int(rows)))
+
+
+def mesh_attn_cache_score_fwd(cache, softmax_scale, score, q, positions, cu_new,
+                              lens, block_table, data, o, lse, ws=None,
+                              stream=None):
+    """``mesh_attn_cache_fwd`` under a score rule, whose ``key_begin`` and
+    ``key_end`` are indexed by the query rows."""
+    dev, torch = _device_index(stream, q, "q"), _torch_module
+    c, i32 = Cache.make(cache), torch.int32
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, heads, head_dim]")
+    rows, hq, d = q.shape[0], q.shape[1], c.head_dim
+    b = lens.numel()
+    s = _score_args(score, rows, hq, dev)
+    qp, qs = _heads(q, "q", rows, hq, d, torch.bfloat16, dev)
+    f32 = o.dtype is torch.float32
+    ws, wp, wn = _call_workspace(
+        ws, lambda: mesh_attn_cache_score_fwd_workspace_size(c, hq, b, rows),
+        dev, q, stream)
+    st = load_library().mesh_attn_cache_score_fwd(
+        c, hq, softmax_scale, s, b, rows, qp, qs,
+        _arg(positions, "positions", (rows,), i32, dev),
+        _arg(cu_new, "cu_new", (b + 1,), i32, dev),
+        _arg(lens, "lens", (b,), i32, dev),
+        _arg(block_table, "block_table", (b, c.max_pages), i32, dev),
+        _cache_data(c, data, dev),
+        _arg(o, "o", (rows, hq, d), torch.float32 if f32 else torch.bfloat16,
+             dev),
+        MA_FP32 if f32 else MA_BF16,
+        _arg(lse, "lse", (hq, rows), torch.float32, dev), wp, wn,
+        _stream_ptr(stream))
+    _check("mesh_attn_cache_score_fwd", st)
+    return o, lse
+
+
+# ---------------------------------------------------------------------------
+# Rotation and storage in one call
+# ---------------------------------------------------------------------------
+
+def mesh_attn_cache_rope_append(cache, rope, positions, q, q_out, k, v, slots,
+                                data, stream=None):
+    """Turns ``q [rows, Hq, d]`` by ``positions [num_axes, rows]`` (``[rows]``
+    does for one axis) into ``q_out`` (``q`` for in place), and stores the
+    turned ``k`` and ``v [rows, Hkv, d]`` in 4 bits at ``slots [rows]``; bf16,
+    row strides as they are."""
+    r, c = Rope.make(rope), Cache.make(cache)
+    dev, torch = _device_index(stream, q, "q"), _torch_module
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, heads, head_dim]")
+    rows, hq, d, bf = q.shape[0], q.shape[1], c.head_dim, torch.bfloat16
+    shape = (r.num_axes, rows)
+    if r.num_axes == 1 and positions.dim() == 1:
+        shape = (rows,)
+    qp, qs = _heads(q, "q", rows, hq, d, bf, dev)
+    qo, qos = _heads(q_out, "q_out", rows, hq, d, bf, dev)
+    kp, ks = _heads(k, "k", rows, c.num_kv_heads, d, bf, dev)
+    vp, vs = _heads(v, "v", rows, c.num_kv_heads, d, bf, dev)
+    st = load_library().mesh_attn_cache_rope_append(
+        c, r, rows, _arg(positions, "positions", shape, torch.int32, dev), hq,
+        qp, qs, qo, qos, kp, ks, vp, vs,
+        _arg(slots, "slots", (rows,), torch.int64, dev),
+        _cache_data(c, data, dev), _stream_ptr(stream))
+    _check("mesh_attn_cache_rope_append", st)
+    return q_out, data

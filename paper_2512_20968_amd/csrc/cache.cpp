@@ -13,6 +13,83 @@
 using namespace mesh_attn;
 using namespace mesh_attn::host;
 
+namespace {
+
+// Attention over the cache, with a score rule or without.
+ma_status_t cache_fwd(
+    const ma_cache_t* cache, int32_t num_q_heads, float softmax_scale,
+    bool rule, const ma_score_t* score, int32_t num_requests, int64_t rows, const void* q, int64_t q_stride,
+    const int32_t* positions, const int32_t* cu_new, const int32_t* lens,
+    const int32_t* block_table, const void* data, void* o, ma_dtype_t o_dtype,
+    float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  CacheFwdParams p;
+  MA_TRY(check_cache(cache, &p.c));
+  MA_TRY(check_q_heads(num_q_heads, p.c.hkv));
+  MA_TRY(check_requests(num_requests));
+  MA_TRY(check_rows(rows));
+  p.scale_log2 = softmax_scale * 1.4426950408889634f;
+  p.inv_scale_log2 = 1.f / p.scale_log2;
+  if (!(softmax_scale > 0.f) || !std::isfinite(p.scale_log2))
+    return fail(MA_ERR_INVALID_ARG, "softmax_scale must be positive and "
+                "finite");
+  if (rule) MA_TRY(check_score(score, softmax_scale));
+  if (o_dtype != MA_BF16 && o_dtype != MA_FP32)
+    return fail(MA_ERR_INVALID_ARG, "o_dtype %d invalid", (int)o_dtype);
+  if (rows * num_q_heads >= int64_t{1} << 30)
+    return fail(MA_ERR_INVALID_ARG, "rows * num_q_heads %lld not below 2^30",
+                static_cast<long long>(rows) * num_q_heads);
+  MA_TRY(check_stride("q_stride", q_stride, int64_t{num_q_heads} * p.c.d, 8));
+  if (rows == 0 || num_requests == 0) return ok();
+  const Arg args[] = {{"q", q, 16},
+                      {"positions", positions, 4},
+                      {"cu_new", cu_new, 4},
+                      {"lens", lens, 4},
+                      {"block_table", block_table, 4},
+                      {"data", data, 16},
+                      {"o", o, 16},
+                      {"lse", lse, 4}};
+  MA_TRY(check_args(args, 8));
+  const size_t need = cache_fwd_workspace(p.c, num_requests, rows);
+  if (need > 0) {
+    if (ws_bytes < need)
+      return fail(MA_ERR_WORKSPACE_TOO_SMALL,
+                  "workspace of %zu bytes, %zu needed", ws_bytes, need);
+    const Arg a{"ws", ws, 16};
+    MA_TRY(check_args(&a, 1));
+  }
+  p.q = static_cast<const uint16_t*>(q);
+  p.q_stride = q_stride;
+  p.positions = positions;
+  p.cu = cu_new;
+  p.lens = lens;
+  p.block_table = block_table;
+  p.data = static_cast<const uint8_t*>(data);
+  p.o = o;
+  p.lse = lse;
+  p.rows = rows;
+  p.hq = num_q_heads;
+  p.group = num_q_heads / p.c.hkv;
+  p.num_requests = num_requests;
+  p.rule = rule;
+  p.cap_in = p.cap_two = p.cap_u = 0.f;
+  p.slopes = nullptr;
+  p.key_begin = p.key_end = nullptr;
+  if (score) {
+    if (score->cap > 0.f) {
+      p.cap_in = 2.f * p.scale_log2 / score->cap;
+      p.cap_two = 2.f * score->cap * 1.4426950408889634f;
+      p.cap_u = softmax_scale / score->cap;
+    }
+    p.slopes = score->slopes;
+    p.key_begin = score->key_begin;
+    p.key_end = score->key_end;
+  }
+  return launched(launch_cache_fwd(p, o_dtype == MA_FP32, ws, stream),
+                  "cache_fwd launch");
+}
+
+}  // namespace
+
 extern "C" {
 
 size_t mesh_attn_cache_bytes(const ma_cache_t* cache) {
@@ -154,55 +231,29 @@ ma_status_t mesh_attn_cache_fwd(
     const int32_t* positions, const int32_t* cu_new, const int32_t* lens,
     const int32_t* block_table, const void* data, void* o, ma_dtype_t o_dtype,
     float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
-  CacheFwdParams p;
-  MA_TRY(check_cache(cache, &p.c));
-  MA_TRY(check_q_heads(num_q_heads, p.c.hkv));
-  MA_TRY(check_requests(num_requests));
-  MA_TRY(check_rows(rows));
-  p.scale_log2 = softmax_scale * 1.4426950408889634f;
-  p.inv_scale_log2 = 1.f / p.scale_log2;
-  if (!(softmax_scale > 0.f) || !std::isfinite(p.scale_log2))
-    return fail(MA_ERR_INVALID_ARG, "softmax_scale must be positive and "
-                "finite");
-  if (o_dtype != MA_BF16 && o_dtype != MA_FP32)
-    return fail(MA_ERR_INVALID_ARG, "o_dtype %d invalid", (int)o_dtype);
-  if (rows * num_q_heads >= int64_t{1} << 30)
-    return fail(MA_ERR_INVALID_ARG, "rows * num_q_heads %lld not below 2^30",
-                static_cast<long long>(rows) * num_q_heads);
-  MA_TRY(check_stride("q_stride", q_stride, int64_t{num_q_heads} * p.c.d, 8));
-  if (rows == 0 || num_requests == 0) return ok();
-  const Arg args[] = {{"q", q, 16},
-                      {"positions", positions, 4},
-                      {"cu_new", cu_new, 4},
-                      {"lens", lens, 4},
-                      {"block_table", block_table, 4},
-                      {"data", data, 16},
-                      {"o", o, 16},
-                      {"lse", lse, 4}};
-  MA_TRY(check_args(args, 8));
-  const size_t need = cache_fwd_workspace(p.c, num_requests, rows);
-  if (need > 0) {
-    if (ws_bytes < need)
-      return fail(MA_ERR_WORKSPACE_TOO_SMALL,
-                  "workspace of %zu bytes, %zu needed", ws_bytes, need);
-    const Arg a{"ws", ws, 16};
-    MA_TRY(check_args(&a, 1));
-  }
-  p.q = static_cast<const uint16_t*>(q);
-  p.q_stride = q_stride;
-  p.positions = positions;
-  p.cu = cu_new;
-  p.lens = lens;
-  p.block_table = block_table;
-  p.data = static_cast<const uint8_t*>(data);
-  p.o = o;
-  p.lse = lse;
-  p.rows = rows;
-  p.hq = num_q_heads;
-  p.group = num_q_heads / p.c.hkv;
-  p.num_requests = num_requests;
-  return launched(launch_cache_fwd(p, o_dtype == MA_FP32, ws, stream),
-                  "cache_fwd launch");
+  return cache_fwd(cache, num_q_heads, softmax_scale, false, nullptr,
+                   num_requests, rows, q, q_stride, positions, cu_new, lens,
+                   block_table, data, o, o_dtype, lse, ws, ws_bytes, stream);
+}
+
+size_t mesh_attn_cache_score_fwd_workspace_size(const ma_cache_t* cache,
+                                                int32_t num_q_heads,
+                                                int32_t num_requests,
+                                                int64_t rows) {
+  return mesh_attn_cache_fwd_workspace_size(cache, num_q_heads, num_requests,
+                                            rows);
+}
+
+ma_status_t mesh_attn_cache_score_fwd(
+    const ma_cache_t* cache, int32_t num_q_heads, float softmax_scale,
+    const ma_score_t* score, int32_t num_requests, int64_t rows, const void* q,
+    int64_t q_stride, const int32_t* positions, const int32_t* cu_new,
+    const int32_t* lens, const int32_t* block_table, const void* data, void* o,
+    ma_dtype_t o_dtype, float* lse, void* ws, size_t ws_bytes,
+    hipStream_t stream) {
+  return cache_fwd(cache, num_q_heads, softmax_scale, true, score,
+                   num_requests, rows, q, q_stride, positions, cu_new, lens,
+                   block_table, data, o, o_dtype, lse, ws, ws_bytes, stream);
 }
 
 ma_status_t mesh_attn_rope(const ma_rope_t* rope, int64_t rows,

@@ -80,7 +80,8 @@ hipError_t launch_cache_read(const LoadParams& p, hipStream_t stream);
 // A sequence of the attention whose partial results are to be joined: those of
 // `parts` runs from `start` on (0: none).
 struct CacheFold {
-  int32_t first, rr0, rr_end, kvh, parts, start, pad[2];
+  int32_t first, rr0, rr_end, kvh, parts, start;
+  int32_t local, pad;  // under a score rule: the request's stored keys
 };
 
 struct CacheFwdParams {
@@ -105,6 +106,13 @@ struct CacheFwdParams {
   int32_t unit_log2;  // keys of a unit
   int32_t seq_units;  // units that a sequence costs beside its keys
   int32_t max_units;  // most of a launch
+  // The score rule (rule = 1): cap_two = 2 cap log2(e), 0 without a cap; a
+  // product times cap_in is log2(e^(2u)), times cap_u u = score / cap.
+  int32_t rule;
+  float cap_in, cap_two, cap_u;
+  const float* slopes;
+  const int32_t* key_begin;
+  const int32_t* key_end;
   CacheFold* fold;           // [workgroup][2]: goes on in its run, starts in it
   float* part_o;             // [2 * workgroups][rows of a tile][d]
   float* part_ml;            // .. [2]: reference (log2 units) and sum

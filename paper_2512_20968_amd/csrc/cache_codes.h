@@ -58,5 +58,54 @@ struct Block {
   }
 };
 
+// Codes of 8 values and their group's scale code.
+struct Quant {
+  uint32_t codes, scale;
+};
+
+// Of the values of four neighbouring lanes, a group, this lane's.
+__device__ __forceinline__ Quant quantize8(float (&x)[8]) {
+  uint32_t top = 0;  // largest magnitude, as float bits (NaN above infinity)
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  top = max(top, uint32_t(__shfl_xor(int(top), 1)));
+  top = max(top, uint32_t(__shfl_xor(int(top), 2)));
+  const bool finite = top < 0x7f800000u;
+  int e = int(top >> 23) - 129 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+  e = min(max(e, -126), 125);
+  // 2^-e; a group that is not finite gets codes of 0 and the NaN scale.
+  const float inv = finite ? __uint_as_float(uint32_t(127 - e) << 23) : 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = finite ? x[i] * inv : 0.f;
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], 1.f, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], 1.f, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], 1.f, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], 1.f, 3);
+  return {w, finite ? uint32_t(e + 127) : kScaleNaN};
+}
+
+// Dims 8 chunk .. of K and V of token t into its (page, KV head) block.
+template <int D>
+__device__ __forceinline__ void store_quants(uint8_t* blk, int lg, int t,
+                                             int chunk, const Quant& k,
+                                             const Quant& v) {
+  using B = Block<D>;
+  *reinterpret_cast<uint32_t*>(blk + B::k_codes(lg, t) + chunk * 4) = k.codes;
+  if constexpr (D == 128) {
+    *reinterpret_cast<uint32_t*>(blk + B::v_codes(lg, t, chunk)) = v.codes;
+  } else {
+    *reinterpret_cast<uint16_t*>(blk + B::v_codes(lg, t, 2 * chunk)) =
+        static_cast<uint16_t>(v.codes);
+    *reinterpret_cast<uint16_t*>(blk + B::v_codes(lg, t, 2 * chunk + 1)) =
+        static_cast<uint16_t>(v.codes >> 16);
+  }
+  if ((chunk & 3) == 0) {
+    blk[B::k_scale(lg, t, chunk / 4)] = static_cast<uint8_t>(k.scale);
+    blk[B::v_scale(lg, t, chunk / 4)] = static_cast<uint8_t>(v.scale);
+  }
+}
+
 }  // namespace dev
 }  // namespace mesh_attn

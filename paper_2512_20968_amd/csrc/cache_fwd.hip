@@ -198,6 +198,101 @@ struct State {
   int vis[NQ];          // stored keys that the column's row sees
 };
 
+// Under a score rule: keys [lo, vis) are seen, and the distance bias is taken
+// relative to the nearest of them, `off` positions away, so that those of far keys
+// keep their digits.
+template <int NQ>
+struct RuleState {
+  int lo[NQ], qpos[NQ], off[NQ];
+  float slope[NQ];  // log2 units
+};
+
+// A row under the rule; `local`: stored keys of its request.
+struct RuleRow {
+  int lo, vis, qpos, off;
+};
+
+__device__ __forceinline__ int64_t key_position(const CacheFwdParams& p,
+                                                int64_t key) {
+  return p.c.share.striped ? key * p.c.share.n + p.c.share.p
+                           : p.c.share.first + key;
+}
+
+__device__ __forceinline__ RuleRow rule_row(const CacheFwdParams& p,
+                                            int64_t row, int local) {
+  RuleRow r;
+  r.qpos = p.positions[row];
+  const int64_t begin = p.key_begin ? max(p.key_begin[row], 0) : 0;
+  const int64_t end =
+      p.key_end ? max(p.key_end[row], 0) : int64_t{max(r.qpos, -1)} + 1;
+  r.vis = min(p.c.share.below(end), local);
+  r.lo = min(p.c.share.below(begin), r.vis);
+  r.off = 0;
+  if (p.slopes && r.lo < r.vis) {
+    const int at = p.c.share.below(max(r.qpos, 0));  // first not before it
+    const int64_t a = key_position(p, min(max(at, r.lo), r.vis - 1));
+    const int64_t b = key_position(p, min(max(at - 1, r.lo), r.vis - 1));
+    const int64_t da = a > r.qpos ? a - r.qpos : r.qpos - a;
+    const int64_t db = b > r.qpos ? b - r.qpos : r.qpos - b;
+    r.off = static_cast<int>(da < db ? da : db);
+  }
+  return r;
+}
+
+// Products of a step -> scores in log2 units: capped (tanh(u) = 1 - 2 / (1 +
+// e^(2u)); small arguments of a float32 O by its series) and biased.
+template <int NQ, bool EXACT>
+__device__ __forceinline__ void rule_step(const CacheFwdParams& p,
+                                          const RuleState<NQ>& rs,
+                                          f32x4 (&x)[NQ][2], int kb, int g) {
+  if (p.cap_two > 0.f) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = x[q][i >> 2][i & 3];
+        float y = fmaf(
+            -p.cap_two,
+            __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * p.cap_in)),
+            0.5f * p.cap_two);
+        if (EXACT) {
+          // Taylor; the first term left out is below 2^-25 of the sum.
+          const float u = v * p.cap_u, z = u * u;
+          float t = fmaf(z, -1382.f / 155925, 62.f / 2835);
+          t = fmaf(t, z, -17.f / 315);
+          t = fmaf(t, z, 2.f / 15);
+          t = fmaf(t, z, -1.f / 3);
+          t = fmaf(t * z, u, u);
+          y = fabsf(u) < 0.4f ? t * (0.5f * p.cap_two) : y;
+        }
+        x[q][i >> 2][i & 3] = y;
+      }
+  } else {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      x[q][0] *= p.scale_log2;
+      x[q][1] *= p.scale_log2;
+    }
+  }
+  if (p.slopes) {
+    const int k0 = static_cast<int>(key_position(p, kb + 8 * g));
+    const int step = p.c.share.striped ? p.c.share.n : 1;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // In 32 bits: what wraps is not seen.
+        const int d = static_cast<int>(static_cast<uint32_t>(rs.qpos[q]) -
+                                       static_cast<uint32_t>(k0) -
+                                       static_cast<uint32_t>(i) * step);
+        x[q][i >> 2][i & 3] =
+            fmaf(-rs.slope[q],
+                 static_cast<float>((d < 0 ? -d : d) - rs.off[q]),
+                 x[q][i >> 2][i & 3]);
+      }
+  }
+}
+
 // The reference may lag behind the maximum by this much (log2 units):
 // probabilities stay below 2^kLag, as exact relative to each other as below 1,
 // and the accumulators are rescaled a few times per item instead of whenever a
@@ -330,8 +425,10 @@ __device__ __forceinline__ void finish_step(State<D, NQ>& st,
 // invalid: hidden scores are -inf, and V of keys that no column may use counts
 // as 0.  A NaN group of V of a key that some rows see and others do not is taken
 // out of the product (0 * NaN is NaN) and given to those that see it.
-template <int D, int NQ>
-__device__ __forceinline__ u32x2 mask_step(State<D, NQ>& st, f32x4 (&x)[NQ][2],
+template <int D, int NQ, bool RULE>
+__device__ __forceinline__ u32x2 mask_step(State<D, NQ>& st,
+                                           const RuleState<NQ>& rs,
+                                           f32x4 (&x)[NQ][2],
                                            const StepData<D>& s, bool ok,
                                            int kb, int local, int g) {
   u32x2 vs = s.vs;
@@ -342,7 +439,9 @@ __device__ __forceinline__ u32x2 mask_step(State<D, NQ>& st, f32x4 (&x)[NQ][2],
   for (int q = 0; q < NQ; ++q)
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (!ok || kb + 8 * g + i >= st.vis[q]) x[q][i >> 2][i & 3] = -INFINITY;
+      if (!ok || kb + 8 * g + i >= st.vis[q] ||
+          (RULE && kb + 8 * g + i < rs.lo[q]))
+        x[q][i >> 2][i & 3] = -INFINITY;
   // Bit i: key 8 g + i of the lane's group of dims is NaN.
   uint32_t nan = 0;
 #pragma unroll
@@ -360,7 +459,10 @@ __device__ __forceinline__ u32x2 mask_step(State<D, NQ>& st, f32x4 (&x)[NQ][2],
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         const int seen = min(max(st.vis[q] - (kb + 8 * o), 0), 8);
-        hit[q] |= (bits & ((1u << seen) - 1)) != 0;
+        uint32_t those = (1u << seen) - 1;
+        if (RULE)
+          those &= ~((1u << min(max(rs.lo[q] - (kb + 8 * o), 0), 8)) - 1);
+        hit[q] |= (bits & those) != 0;
       }
     }
 #pragma unroll
@@ -402,15 +504,19 @@ __device__ __forceinline__ void score_step(const State<D, NQ>& st,
 }
 
 // One row's final results from its sums at reference m.
-template <int D, bool OUT_F32>
+template <int D, bool OUT_F32, bool RULE>
 __device__ __forceinline__ void store_row(const CacheFwdParams& p, int64_t row,
-                                          int head, int dim0,
+                                          int head, int local, int dim0,
                                           const float (&acc)[8], float m,
                                           float l) {
-  if (dim0 == 0)
+  if (dim0 == 0) {
+    if (RULE && p.slopes)  // the part of the bias that all keys share
+      m -= p.slopes[head] * 1.4426950408889634f *
+           static_cast<float>(rule_row(p, row, local).off);
     p.lse[int64_t{head} * p.rows + row] =
         l == 0.f ? -INFINITY
                  : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+  }
   const float inv = l > 0.f ? 1.f / l : l;  // 0 for no key; NaN stays
   const int64_t at = (row * p.hq + head) * D + dim0;
   if (OUT_F32) {
@@ -471,15 +577,48 @@ constexpr int kKeptRequests = 256;
 struct RequestRows {
   int first, end, local;
 };
+// Under a score rule: the first keys that none of the request's rows sees, whole
+// steps of them.  The units of its sequences are those behind them.
+struct RequestRule : RequestRows {
+  int skip;
+};
+template <bool RULE>
+struct RequestOf {
+  typedef RequestRows type;
+};
+template <>
+struct RequestOf<true> {
+  typedef RequestRule type;
+};
+template <bool RULE>
+using Request = typename RequestOf<RULE>::type;
 
-__device__ __forceinline__ RequestRows load_request(const CacheFwdParams& p,
-                                                    int b) {
+__device__ __forceinline__ int unit_keys(const RequestRows& r) {
+  return r.local;
+}
+__device__ __forceinline__ int unit_keys(const RequestRule& r) {
+  return r.local - r.skip;
+}
+__device__ __forceinline__ int skipped_keys(const RequestRows&) { return 0; }
+__device__ __forceinline__ int skipped_keys(const RequestRule& r) {
+  return r.skip;
+}
+
+template <bool RULE>
+__device__ __forceinline__ Request<RULE> load_request(const CacheFwdParams& p,
+                                                      int b) {
   const int rows = static_cast<int>(p.rows);
-  RequestRows r;
+  Request<RULE> r;
   const int a = p.cu[b], e = p.cu[b + 1];
   r.local = stored_keys(p, p.lens[b]);
   r.first = min(max(a, 0), rows);
   r.end = min(max(e, r.first), rows);
+  if constexpr (RULE) {
+    r.skip = 0;
+    if (p.key_begin && r.first < r.end)
+      r.skip = min(p.c.share.below(max(p.key_begin[r.first], 0)), r.local) &
+               ~(kStep - 1);
+  }
   return r;
 }
 
@@ -489,14 +628,14 @@ struct Sequences {
   int tiles, units;
 };
 
-template <int kRows>
+template <int kRows, typename R>
 __device__ __forceinline__ Sequences sequences_of(const CacheFwdParams& p,
-                                                  const RequestRows& r,
-                                                  bool split) {
+                                                  const R& r, bool split) {
   const uint32_t rr = uint32_t(r.end - r.first) * p.group;  // below 2^30
   const bool mine = r.local >= p.least_keys && r.local <= p.most_keys;
   return {mine ? int((rr + kRows - 1) / kRows) : 0,
-          split ? max((r.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1)
+          split ? max((unit_keys(r) + (1 << p.unit_log2) - 1) >> p.unit_log2,
+                      1)
                 : 1};
 }
 
@@ -517,13 +656,13 @@ struct Totals {
   int longest;
 };
 
-template <int kRows>
+template <int kRows, bool RULE>
 __device__ __forceinline__ bool whole_is_better(const CacheFwdParams& p,
                                                 Totals* s_totals) {
   if (threadIdx.x == 0) *s_totals = Totals{0, 0, 0, 0};
   __syncthreads();
   for (int b = threadIdx.x; b < p.num_requests; b += NT) {
-    const RequestRows r = load_request(p, b);
+    const Request<RULE> r = load_request<RULE>(p, b);
     const Sequences q = sequences_of<kRows>(p, r, true);
     if (q.tiles == 0) continue;
     const int64_t n = int64_t{q.tiles} * p.c.hkv;
@@ -549,9 +688,9 @@ __device__ __forceinline__ bool whole_is_better(const CacheFwdParams& p,
 // sums are capped at max_units, which rows that do not overlap cannot pass.
 // Returns the number of units; *longest is the longest sequence of a request
 // with several tiles (0: there is none).
-template <int kRows>
+template <int kRows, bool RULE>
 __device__ __forceinline__ int plan_units(const CacheFwdParams& p, bool split,
-                                          int* s_units, RequestRows* s_kept,
+                                          int* s_units, Request<RULE>* s_kept,
                                           int* s_wave, int* s_longest,
                                           int* longest) {
   const int B = p.num_requests, tid = threadIdx.x, lane = tid & 63;
@@ -563,7 +702,7 @@ __device__ __forceinline__ int plan_units(const CacheFwdParams& p, bool split,
     const int b = b0 + tid;
     int mine = 0;
     if (b < B) {
-      const RequestRows r = load_request(p, b);
+      const Request<RULE> r = load_request<RULE>(p, b);
       if (B <= kKeptRequests) s_kept[b] = r;
       const Sequences q = sequences_of<kRows>(p, r, split);
       const int64_t n = int64_t{q.tiles} * (q.units + cost) * p.c.hkv;
@@ -618,13 +757,14 @@ constexpr int kWavesPerSimd = D == 64 ? (NQ == 1 ? 4 : NQ == 2 ? 3 : 2)
 // run ends before the keys), the last of them before `end` in all units.
 struct Item {
   int b, first, rr0, rr_end, kvh, u0, u1, nu, local, end;
+  int skip;  // keys before the first unit
 };
 
 // The item at unit `at` of a run that ends at `stop`.
-template <int kRows, bool OWN>
+template <int kRows, bool OWN, bool RULE>
 __device__ __forceinline__ Item locate(const CacheFwdParams& p, bool split,
                                        const int* s_units,
-                                       const RequestRows* s_kept, int at,
+                                       const Request<RULE>* s_kept, int at,
                                        int stop) {
   const int B = p.num_requests, hkv = p.c.hkv;
   int lo = 0, hi = B;
@@ -637,13 +777,16 @@ __device__ __forceinline__ Item locate(const CacheFwdParams& p, bool split,
   }
   Item it;
   it.b = __builtin_amdgcn_readfirstlane(lo);
-  const RequestRows req =
-      B <= kKeptRequests ? s_kept[it.b] : load_request(p, it.b);
+  const Request<RULE> req =
+      B <= kKeptRequests ? s_kept[it.b] : load_request<RULE>(p, it.b);
   it.first = __builtin_amdgcn_readfirstlane(req.first);
   it.rr_end = __builtin_amdgcn_readfirstlane(req.end - req.first) * p.group;
   it.local = __builtin_amdgcn_readfirstlane(req.local);
-  it.nu =
-      split ? max((it.local + (1 << p.unit_log2) - 1) >> p.unit_log2, 1) : 1;
+  it.skip = RULE ? __builtin_amdgcn_readfirstlane(skipped_keys(req)) : 0;
+  it.nu = split ? max((it.local - it.skip + (1 << p.unit_log2) - 1) >>
+                          p.unit_log2,
+                      1)
+                : 1;
   const int off = at - __builtin_amdgcn_readfirstlane(s_units[it.b]);
   const int len = split ? it.nu + p.seq_units : 1, seq = off / len;
   const int v0 = off - seq * len;  // of the sequence's units with its cost
@@ -676,7 +819,8 @@ __device__ __forceinline__ Item locate(const CacheFwdParams& p, bool split,
 }
 
 // OWN: every wave has items of its own, whole sequences, and nothing to fold.
-template <int D, int NQ, bool OUT_F32, bool P16, bool OWN>
+// RULE: scores under a rule (mesh_attn_cache_score_fwd).
+template <int D, int NQ, bool OUT_F32, bool P16, bool OWN, bool RULE>
 __global__ __launch_bounds__(NT, (kWavesPerSimd<D, NQ>))
 void cache_fwd_kernel(CacheFwdParams p) {
   constexpr int kRows = 16 * NQ;
@@ -691,21 +835,21 @@ void cache_fwd_kernel(CacheFwdParams p) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
-  RequestRows* s_kept =
-      reinterpret_cast<RequestRows*>(s_units + p.num_requests + 1);
+  Request<RULE>* s_kept =
+      reinterpret_cast<Request<RULE>*>(s_units + p.num_requests + 1);
   bf16x8* s_q = s_q_all + (OWN && kQInLds<NQ> ? wave * kQ : 0);
   bool split = !OWN && p.split;
   if constexpr (kRows > 16 && !OWN) {
     __shared__ Totals s_totals;
     if (split && p.may_stay_whole)
       split = !__builtin_amdgcn_readfirstlane(
-          whole_is_better<kRows>(p, &s_totals));
+          whole_is_better<kRows, RULE>(p, &s_totals));
   }
 
   int longest;
   const int total = __builtin_amdgcn_readfirstlane(
-      plan_units<kRows>(p, split, s_units, s_kept, s_wave, &s_longest,
-                        &longest));
+      plan_units<kRows, RULE>(p, split, s_units, s_kept, s_wave, &s_longest,
+                              &longest));
   // Split: this workgroup's run.  Workgroup i runs on XCD i % 8; neighbouring
   // runs go to one XCD (the grid is a multiple of 8), whose L2 then serves the
   // tiles of a head, and the runs with work spread over all of them.
@@ -743,12 +887,13 @@ void cache_fwd_kernel(CacheFwdParams p) {
     p.fold[2 * run].parts = p.fold[2 * run + 1].parts = 0;
 
   State<D, NQ> st;
+  RuleState<NQ> rs;
   Item it, prev;
   bool have_prev = false;
   for (;;) {
     bool more = false;
     while (at < stop && !more) {
-      it = locate<kRows, OWN>(p, split, s_units, s_kept, at, stop);
+      it = locate<kRows, OWN, RULE>(p, split, s_units, s_kept, at, stop);
       if (split) {
         at = it.end;
       } else {
@@ -776,6 +921,12 @@ void cache_fwd_kernel(CacheFwdParams p) {
       piece_end = split ? min(int64_t{it.u1} << p.unit_log2,
                               int64_t{it.local})
                         : it.local;
+      if constexpr (RULE) {
+        kb += it.skip;
+        if (split)
+          piece_end = min((int64_t{it.u1} << p.unit_log2) + it.skip,
+                          int64_t{it.local});
+      }
       pg = load_pages<P16>(h, kb);
       if (kQInLds<NQ> && !OWN) lds_barrier();  // the last item's Q has been read
       const int t = fresh_tid(), r = t & 15, g = (t & 63) >> 4, lane = t & 63;
@@ -855,8 +1006,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
           }
           if (whole) {
             const TokenHead th = token_head(p, rr, prev.kvh);
-            store_row<D, OUT_F32>(p, prev.first + th.tok, th.head, dim0, acc,
-                                  ref, L);
+            store_row<D, OUT_F32, RULE>(p, prev.first + th.tok, th.head,
+                                        prev.local, dim0, acc, ref, L);
           } else {
             const int64_t pr = int64_t{slot} * kRows + 16 * q + row16;
             if (dim0 == 0) {
@@ -872,14 +1023,27 @@ void cache_fwd_kernel(CacheFwdParams p) {
     }
     if (!more) break;
 
-    int most_seen = 0, all_see = INT32_MAX;
+    int most_seen = 0, all_see = INT32_MAX, all_from = 0;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       const int r = fresh_tid() & 15;
       const bool valid = it.rr0 + 16 * q + r < it.rr_end;
-      st.vis[q] = valid ? min(p.c.share.below(int64_t{max(pos[q], -1)} + 1),
-                              it.local)
-                        : 0;
+      if constexpr (RULE) {
+        const uint32_t rr = valid ? it.rr0 + 16 * q + r : it.rr0;
+        const TokenHead th = token_head(p, rr, it.kvh);
+        const RuleRow row = rule_row(p, int64_t{it.first} + th.tok, it.local);
+        st.vis[q] = valid ? row.vis : 0;
+        rs.lo[q] = row.lo;
+        rs.qpos[q] = row.qpos;
+        rs.off[q] = row.off;
+        rs.slope[q] =
+            p.slopes ? p.slopes[th.head] * 1.4426950408889634f : 0.f;
+        if (valid) all_from = max(all_from, row.lo);
+      } else {
+        st.vis[q] = valid ? min(p.c.share.below(int64_t{max(pos[q], -1)} + 1),
+                                it.local)
+                          : 0;
+      }
       most_seen = max(most_seen, st.vis[q]);
       if (valid) all_see = min(all_see, st.vis[q]);
       st.limit[q] = -INFINITY;
@@ -891,9 +1055,11 @@ void cache_fwd_kernel(CacheFwdParams p) {
     for (int o = 1; o < 16; o *= 2) {
       most_seen = max(most_seen, __shfl_xor(most_seen, o));
       all_see = min(all_see, __shfl_xor(all_see, o));
+      if (RULE) all_from = max(all_from, __shfl_xor(all_from, o));
     }
     most_seen = __builtin_amdgcn_readfirstlane(most_seen);
     all_see = __builtin_amdgcn_readfirstlane(all_see);
+    if (RULE) all_from = __builtin_amdgcn_readfirstlane(all_from);
     if (kQInLds<NQ> && !OWN) lds_barrier();
 
     // The next step's K is loaded into the registers of this one's as soon as
@@ -916,10 +1082,11 @@ void cache_fwd_kernel(CacheFwdParams p) {
         if (more_keys) load_k<D, P16>(h, pn, next, r, &s);
         u32x2 vs = s.vs;
         const bool ok = lane_ok<P16>(h, pg, g);
-        if (kb + kStep > all_see || !__all(ok))
-          vs = mask_step<D, NQ>(st, x, s, ok, kb, h.local, g);
-        finish_step<D, NQ, OUT_F32>(st, x, s, p.scale_log2,
-                                    p.inv_scale_log2, vs);
+        if constexpr (RULE) rule_step<NQ, OUT_F32>(p, rs, x, kb, g);
+        if (kb + kStep > all_see || (RULE && kb < all_from) || !__all(ok))
+          vs = mask_step<D, NQ, RULE>(st, rs, x, s, ok, kb, h.local, g);
+        finish_step<D, NQ, OUT_F32>(st, x, s, RULE ? 1.f : p.scale_log2,
+                                    RULE ? 1.f : p.inv_scale_log2, vs);
         if (!more_keys) break;
         load_v<D, P16>(h, pn, next, g, &s);
         pg = pn;
@@ -944,9 +1111,9 @@ void cache_fwd_kernel(CacheFwdParams p) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               acc[i] = st.o[q][(8 * j + i) % (D / 16)][(8 * j + i) / (D / 16)];
-            store_row<D, OUT_F32>(
-                p, it.first + th.tok, th.head, g * (D / 4) + 8 * j, acc,
-                st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
+            store_row<D, OUT_F32, RULE>(
+                p, it.first + th.tok, th.head, it.local, g * (D / 4) + 8 * j,
+                acc, st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
           }
         }
       }
@@ -960,6 +1127,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
       f.rr0 = it.rr0;
       f.rr_end = it.rr_end;
       f.kvh = it.kvh;
+      if (RULE) f.local = it.local;
       f.start = goes_on ? (per * run - it.u0) / per : run;
       const int more_runs = goes_on ? (it.nu - it.u0 - 1) / per
                                     : (it.nu - it.u1 + per - 1) / per;
@@ -980,7 +1148,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
 // tokens of one head 17/46 us, 2 of 51K 19/56 us.
 constexpr int kFoldThreads = 512;
 
-template <int D, int NQ, bool OUT_F32>
+template <int D, int NQ, bool OUT_F32, bool RULE>
 __global__ __launch_bounds__(kFoldThreads)
 void cache_fold_kernel(CacheFwdParams p) {
   constexpr int kRows = 16 * NQ, kDimThreads = D / 8;
@@ -1045,8 +1213,8 @@ void cache_fold_kernel(CacheFwdParams p) {
     }
     if (pg == 0 && valid) {
       const TokenHead th = token_head(p, rr, f.kvh);
-      store_row<D, OUT_F32>(p, f.first + th.tok, th.head, dim0, acc,
-                            M == -INFINITY ? 0.f : M, L);
+      store_row<D, OUT_F32, RULE>(p, f.first + th.tok, th.head, f.local, dim0,
+                                  acc, M == -INFINITY ? 0.f : M, L);
     }
     __syncthreads();
   }
@@ -1093,7 +1261,7 @@ constexpr int64_t kBriefKeys = 512;
 constexpr int64_t kOwnGrid = 4;
 
 Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
-               int64_t rows, bool out_f32) {
+               int64_t rows, bool out_f32, bool rule) {
   const int group = hq / c.hkv;
   Shape s;
   // Rows of a request, were they all alike: the host knows no more.  A batch of
@@ -1102,7 +1270,8 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   const int64_t each = (rows + num_requests - 1) / num_requests * group;
   // Three bf16 parts of 64 rows' probabilities do not fit the registers: 1000
   // rows of 4 heads over 33K tokens take 1894 us in tiles of 32 rows, 2175 of 64.
-  s.nq = each <= 16 ? 1 : each <= 32 || out_f32 ? 2 : 4;
+  // Under a rule neither do a row's range, position and slope.
+  s.nq = each <= 16 ? 1 : each <= 32 || out_f32 || rule ? 2 : 4;
   // Most sequences that rows which do not overlap make.
   const int64_t seqs = (rows * group / (16 * s.nq) + num_requests) * c.hkv;
   const int slots = resident_groups(c.d, s.nq);
@@ -1161,20 +1330,20 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
 size_t fold_bytes(int groups) { return 2 * sizeof(CacheFold) * groups; }
 size_t part_rows(int groups, int nq) { return size_t{32} * nq * groups; }
 
-template <int D, int NQ, bool OUT_F32, bool OWN>
+template <int D, int NQ, bool OUT_F32, bool RULE, bool OWN>
 hipError_t launch_fwd(const CacheFwdParams& p, int groups, hipStream_t stream) {
   const size_t n = static_cast<size_t>(p.num_requests);
   const size_t lds =
-      (n + 1) * 4 + (n <= kKeptRequests ? n * sizeof(RequestRows) : 0);
+      (n + 1) * 4 + (n <= kKeptRequests ? n * sizeof(Request<RULE>) : 0);
   const auto kernel = p.c.page_log2 == 4
-                          ? cache_fwd_kernel<D, NQ, OUT_F32, true, OWN>
-                          : cache_fwd_kernel<D, NQ, OUT_F32, false, OWN>;
+                          ? cache_fwd_kernel<D, NQ, OUT_F32, true, OWN, RULE>
+                          : cache_fwd_kernel<D, NQ, OUT_F32, false, OWN, RULE>;
   hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(groups)), dim3(NT), lds,
                      stream, p);
   return hipGetLastError();
 }
 
-template <int D, int NQ, bool OUT_F32>
+template <int D, int NQ, bool OUT_F32, bool RULE>
 hipError_t launch(CacheFwdParams p, const Shape& s, hipStream_t stream) {
   hipError_t e = hipSuccess;
   p.split = 0;
@@ -1182,31 +1351,33 @@ hipError_t launch(CacheFwdParams p, const Shape& s, hipStream_t stream) {
   p.most_keys = INT32_MAX;
   if (s.own_keys >= 0) {
     if (s.cut) p.most_keys = s.own_keys;
-    e = launch_fwd<D, NQ, OUT_F32, true>(p, s.own_grid, stream);
+    e = launch_fwd<D, NQ, OUT_F32, RULE, true>(p, s.own_grid, stream);
     if (e != hipSuccess || !s.cut) return e;
     p.least_keys = s.own_keys + 1;
     p.most_keys = INT32_MAX;
   }
   if (!s.cut)
-    return launch_fwd<D, NQ, OUT_F32, false>(p, s.whole_grid, stream);
+    return launch_fwd<D, NQ, OUT_F32, RULE, false>(p, s.whole_grid, stream);
   p.split = 1;
-  e = launch_fwd<D, NQ, OUT_F32, false>(p, s.cut_grid, stream);
+  e = launch_fwd<D, NQ, OUT_F32, RULE, false>(p, s.cut_grid, stream);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((cache_fold_kernel<D, NQ, OUT_F32>),
+  hipLaunchKernelGGL((cache_fold_kernel<D, NQ, OUT_F32, RULE>),
                      dim3(static_cast<unsigned>(s.cut_grid)),
                      dim3(kFoldThreads), 0, stream, p);
   return hipGetLastError();
 }
 
-template <int D>
+template <int D, bool RULE>
 hipError_t launch_d(const CacheFwdParams& p, const Shape& s, bool out_f32,
                     hipStream_t stream) {
-  if (s.nq == 4) return launch<D, 4, false>(p, s, stream);
+  if constexpr (!RULE) {
+    if (s.nq == 4) return launch<D, 4, false, RULE>(p, s, stream);
+  }
   if (s.nq == 2)
-    return out_f32 ? launch<D, 2, true>(p, s, stream)
-                   : launch<D, 2, false>(p, s, stream);
-  return out_f32 ? launch<D, 1, true>(p, s, stream)
-                 : launch<D, 1, false>(p, s, stream);
+    return out_f32 ? launch<D, 2, true, RULE>(p, s, stream)
+                   : launch<D, 2, false, RULE>(p, s, stream);
+  return out_f32 ? launch<D, 1, true, RULE>(p, s, stream)
+                 : launch<D, 1, false, RULE>(p, s, stream);
 }
 
 }  // namespace
@@ -1228,7 +1399,7 @@ size_t cache_fwd_workspace(const CacheDims& c, int32_t num_requests,
 hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws,
                             hipStream_t stream) {
   const Shape s = shape_of(params.c, params.hq, params.num_requests,
-                           params.rows, out_f32);
+                           params.rows, out_f32, params.rule);
   CacheFwdParams p = params;
   p.unit_log2 = s.unit_log2;
   p.seq_units = kSeqUnits;
@@ -1247,8 +1418,11 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
                                         fold_bytes(s.cut_grid));
     p.part_ml = p.part_o + part_rows(s.cut_grid, s.nq) * p.c.d;
   }
-  return p.c.d == 128 ? launch_d<128>(p, s, out_f32, stream)
-                      : launch_d<64>(p, s, out_f32, stream);
+  if (p.rule)
+    return p.c.d == 128 ? launch_d<128, true>(p, s, out_f32, stream)
+                        : launch_d<64, true>(p, s, out_f32, stream);
+  return p.c.d == 128 ? launch_d<128, false>(p, s, out_f32, stream)
+                      : launch_d<64, false>(p, s, out_f32, stream);
 }
 
 }  // namespace mesh_attn

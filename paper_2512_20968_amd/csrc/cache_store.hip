@@ -28,36 +28,14 @@ using namespace dev;
 
 constexpr int NT = 256;
 
-// Codes of 8 values and their group's scale code.
-struct Quant {
-  uint32_t codes, scale;
-};
-
 __device__ __forceinline__ Quant quantize8(u32x4 raw) {
   float x[8];
-  uint32_t top = 0;  // largest magnitude, as float bits (NaN above infinity)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = raw[i] << 16, hi = raw[i] & 0xffff0000u;
-    x[2 * i] = __uint_as_float(lo);
-    x[2 * i + 1] = __uint_as_float(hi);
-    top = max(top, max(lo & 0x7fffffffu, hi & 0x7fffffffu));
+    x[2 * i] = __uint_as_float(raw[i] << 16);
+    x[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
   }
-  top = max(top, uint32_t(__shfl_xor(int(top), 1)));
-  top = max(top, uint32_t(__shfl_xor(int(top), 2)));
-  const bool finite = top < 0x7f800000u;
-  int e = int(top >> 23) - 129 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-  e = min(max(e, -126), 125);
-  // 2^-e; a group that is not finite gets codes of 0 and the NaN scale.
-  const float inv = finite ? __uint_as_float(uint32_t(127 - e) << 23) : 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = finite ? x[i] * inv : 0.f;
-  uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], 1.f, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], 1.f, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], 1.f, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], 1.f, 3);
-  return {w, finite ? uint32_t(e + 127) : kScaleNaN};
+  return dev::quantize8(x);
 }
 
 // Threads take (row, head, chunk of 8 dims), chunks fastest, then rows: a
@@ -78,7 +56,6 @@ __device__ __forceinline__ int64_t thread_row() {
 
 template <int D>
 __global__ __launch_bounds__(NT) void cache_append_kernel(StoreParams p) {
-  using B = Block<D>;
   const int64_t row = thread_row<D>();
   if (row >= p.rows) return;  // a group's four lanes alike
   const int lg = p.c.page_log2, chunk = threadIdx.x % (D / 8);
@@ -93,19 +70,7 @@ __global__ __launch_bounds__(NT) void cache_append_kernel(StoreParams p) {
   const int t = static_cast<int>(slot & (p.c.page_size() - 1));
   uint8_t* blk = p.data + ((slot >> lg) * p.c.hkv + head) *
                               int64_t{p.c.block_bytes()};
-  *reinterpret_cast<uint32_t*>(blk + B::k_codes(lg, t) + chunk * 4) = k.codes;
-  if constexpr (D == 128) {
-    *reinterpret_cast<uint32_t*>(blk + B::v_codes(lg, t, chunk)) = v.codes;
-  } else {
-    *reinterpret_cast<uint16_t*>(blk + B::v_codes(lg, t, 2 * chunk)) =
-        static_cast<uint16_t>(v.codes);
-    *reinterpret_cast<uint16_t*>(blk + B::v_codes(lg, t, 2 * chunk + 1)) =
-        static_cast<uint16_t>(v.codes >> 16);
-  }
-  if ((chunk & 3) == 0) {
-    blk[B::k_scale(lg, t, chunk / 4)] = static_cast<uint8_t>(k.scale);
-    blk[B::v_scale(lg, t, chunk / 4)] = static_cast<uint8_t>(v.scale);
-  }
+  store_quants<D>(blk, lg, t, chunk, k, v);
 }
 
 __device__ __forceinline__ u32x4 values8(uint32_t codes, uint32_t scale) {

@@ -18,6 +18,7 @@
 #include <stdint.h>
 
 #include "cache.h"
+#include "rope_turn.h"
 #include "tile_common.h"
 
 namespace mesh_attn {
@@ -65,34 +66,6 @@ struct Unit<false> {
         v, reinterpret_cast<bf16x8*>(static_cast<__bf16*>(base) + i));
   }
 };
-
-// cos and sin of a turn by per * pos (2^-64 turns, modulo 1).
-__device__ __forceinline__ void turn_of(uint64_t per, int32_t pos, float* c,
-                                        float* s) {
-  const uint64_t frac = per * static_cast<uint64_t>(int64_t{pos});
-  // Quadrant, and the signed rest in 2^-64 turns: at most an eighth.
-  const uint64_t near = frac + (uint64_t{1} << 61);
-  const uint32_t quad = static_cast<uint32_t>(near >> 62);
-  const int64_t rest =
-      static_cast<int64_t>(frac - (static_cast<uint64_t>(quad) << 62));
-  // Radians, |t| <= pi / 4: 2 pi 2^-34 a unit of the rest's upper bits.
-  const float t = static_cast<float>(static_cast<int32_t>(rest >> 30)) *
-                  static_cast<float>(6.283185307179586 * 0x1p-34);
-  // Taylor: the first terms left out are below 2^-29 of sin and 2^-33 of cos.
-  const float z = t * t;
-  float sn = fmaf(z, 1.f / 362880, -1.f / 5040);
-  sn = fmaf(sn, z, 1.f / 120);
-  sn = fmaf(sn, z, -1.f / 6);
-  sn = fmaf(sn * z, t, t);
-  float cs = fmaf(z, -1.f / 3628800, 1.f / 40320);
-  cs = fmaf(cs, z, -1.f / 720);
-  cs = fmaf(cs, z, 1.f / 24);
-  cs = fmaf(cs, z, -0.5f);
-  cs = fmaf(cs, z, 1.f);
-  const float a = (quad & 1) ? sn : cs, b = (quad & 1) ? cs : sn;
-  *c = (quad == 1 || quad == 2) ? -a : a;
-  *s = (quad & 2) ? -b : b;
-}
 
 // Units of a thread that are loaded together.
 constexpr int kBatch = 2;

@@ -321,4 +321,50 @@ ma_status_t mesh_attn_score_bwd(const ma_problem_t* prob, const int32_t* q_idx,
                   "score_bwd launch");
 }
 
+ma_status_t mesh_attn_cache_rope_append(
+    const ma_cache_t* cache, const ma_rope_t* rope, int64_t rows,
+    const int32_t* positions, int32_t q_heads, const void* q, int64_t q_stride,
+    void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride,
+    const void* v, int64_t v_stride, const int64_t* slots, void* data,
+    hipStream_t stream) {
+  RopeAppendParams p;
+  MA_TRY(check_cache(cache, &p.c));
+  MA_TRY(check_rope(rope, &p.t));
+  if (rope->head_dim != p.c.d)
+    return fail(MA_ERR_INVALID_ARG, "head_dim %d of the rotation, %d of the "
+                "cache", rope->head_dim, p.c.d);
+  MA_TRY(check_rows(rows));
+  if (q_heads < 1 || q_heads > 65535)
+    return fail(MA_ERR_INVALID_ARG, "q_heads %d outside [1, 65535]", q_heads);
+  const int64_t qw = int64_t{q_heads} * p.c.d, kw = int64_t{p.c.hkv} * p.c.d;
+  MA_TRY(check_stride("q_stride", q_stride, qw, 8));
+  MA_TRY(check_stride("q_out_stride", q_out_stride, qw, 8));
+  MA_TRY(check_stride("k_stride", k_stride, kw, 8));
+  MA_TRY(check_stride("v_stride", v_stride, kw, 8));
+  if (q == q_out && q_stride != q_out_stride)
+    return fail(MA_ERR_INVALID_ARG, "in place with different strides");
+  if (rows == 0) return ok();
+  const Arg args[] = {{"positions", positions, 4}, {"q", q, 16},
+                      {"q_out", q_out, 16},        {"k", k, 16},
+                      {"v", v, 16},                {"slots", slots, 8},
+                      {"data", data, 16}};
+  MA_TRY(check_args(args, 7));
+  p.positions = positions;
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.q_out = static_cast<uint16_t*>(q_out);
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.q_out_stride = q_out_stride;
+  p.slots = slots;
+  p.data = static_cast<uint8_t*>(data);
+  p.rows = rows;
+  p.hq = q_heads;
+  p.rot = rope->rotary_dim;
+  p.interleaved = rope->interleaved;
+  return launched(launch_rope_append(p, stream), "rope_append launch");
+}
+
 }  // extern "C"
