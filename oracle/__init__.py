@@ -22,6 +22,8 @@ against the paper by eye, not for speed:
   canonical run list built from it.
 * ``cache``      -- the paged 4-bit key/value cache (quantization, layout, page
   tables), attention over it and rotary positions.
+* ``score``      -- attention under a score rule (cap, distance bias, ranges of
+  keys) and its gradients.
 * ``tiling``     -- the Q/KV partition index lists of a GPU's tile under basic
   2-D tiling (Section 3.2) and under KV Partition Rotation (Section 3.3).
 
@@ -54,4 +56,5 @@ from .worklist import (  # noqa: F401
     kv_major_run_list,
 )
 from . import cache  # noqa: F401
+from . import score  # noqa: F401
 from .tiling import basic_tile, kvr_tile  # noqa: F401
