@@ -81,7 +81,7 @@ hipError_t launch_cache_read(const LoadParams& p, hipStream_t stream);
 // `parts` runs from `start` on (0: none).
 struct CacheFold {
   int32_t first, rr0, rr_end, kvh, parts, start;
-  int32_t local, pad;  // under a score rule: the request's stored keys
+  int32_t from, local;  // under a score rule: the request's stored keys
 };
 
 struct CacheFwdParams {

@@ -207,7 +207,7 @@ struct RuleState {
   float slope[NQ];  // log2 units
 };
 
-// A row under the rule; `local`: stored keys of its request.
+// A row under the rule; of its request, the stored keys are [from, local).
 struct RuleRow {
   int lo, vis, qpos, off;
 };
@@ -219,14 +219,14 @@ __device__ __forceinline__ int64_t key_position(const CacheFwdParams& p,
 }
 
 __device__ __forceinline__ RuleRow rule_row(const CacheFwdParams& p,
-                                            int64_t row, int local) {
+                                            int64_t row, int from, int local) {
   RuleRow r;
   r.qpos = p.positions[row];
   const int64_t begin = p.key_begin ? max(p.key_begin[row], 0) : 0;
   const int64_t end =
       p.key_end ? max(p.key_end[row], 0) : int64_t{max(r.qpos, -1)} + 1;
   r.vis = min(p.c.share.below(end), local);
-  r.lo = min(p.c.share.below(begin), r.vis);
+  r.lo = min(max(p.c.share.below(begin), from), r.vis);
   r.off = 0;
   if (p.slopes && r.lo < r.vis) {
     const int at = p.c.share.below(max(r.qpos, 0));  // first not before it
@@ -506,13 +506,14 @@ __device__ __forceinline__ void score_step(const State<D, NQ>& st,
 // One row's final results from its sums at reference m.
 template <int D, bool OUT_F32, bool RULE>
 __device__ __forceinline__ void store_row(const CacheFwdParams& p, int64_t row,
-                                          int head, int local, int dim0,
+                                          int head, int from, int local,
+                                          int dim0,
                                           const float (&acc)[8], float m,
                                           float l) {
   if (dim0 == 0) {
     if (RULE && p.slopes)  // the part of the bias that all keys share
       m -= p.slopes[head] * 1.4426950408889634f *
-           static_cast<float>(rule_row(p, row, local).off);
+           static_cast<float>(rule_row(p, row, from, local).off);
     p.lse[int64_t{head} * p.rows + row] =
         l == 0.f ? -INFINITY
                  : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
@@ -577,10 +578,10 @@ constexpr int kKeptRequests = 256;
 struct RequestRows {
   int first, end, local;
 };
-// Under a score rule: the first keys that none of the request's rows sees, whole
-// steps of them.  The units of its sequences are those behind them.
+// Under a score rule no row sees the keys before `from`; the units of the
+// request's sequences begin at the step that holds it.
 struct RequestRule : RequestRows {
-  int skip;
+  int from;
 };
 template <bool RULE>
 struct RequestOf {
@@ -597,11 +598,11 @@ __device__ __forceinline__ int unit_keys(const RequestRows& r) {
   return r.local;
 }
 __device__ __forceinline__ int unit_keys(const RequestRule& r) {
-  return r.local - r.skip;
+  return r.local - (r.from & ~(kStep - 1));
 }
-__device__ __forceinline__ int skipped_keys(const RequestRows&) { return 0; }
-__device__ __forceinline__ int skipped_keys(const RequestRule& r) {
-  return r.skip;
+__device__ __forceinline__ int first_key(const RequestRows&) { return 0; }
+__device__ __forceinline__ int first_key(const RequestRule& r) {
+  return r.from;
 }
 
 template <bool RULE>
@@ -614,10 +615,9 @@ __device__ __forceinline__ Request<RULE> load_request(const CacheFwdParams& p,
   r.first = min(max(a, 0), rows);
   r.end = min(max(e, r.first), rows);
   if constexpr (RULE) {
-    r.skip = 0;
+    r.from = 0;
     if (p.key_begin && r.first < r.end)
-      r.skip = min(p.c.share.below(max(p.key_begin[r.first], 0)), r.local) &
-               ~(kStep - 1);
+      r.from = min(p.c.share.below(max(p.key_begin[r.first], 0)), r.local);
   }
   return r;
 }
@@ -757,7 +757,7 @@ constexpr int kWavesPerSimd = D == 64 ? (NQ == 1 ? 4 : NQ == 2 ? 3 : 2)
 // run ends before the keys), the last of them before `end` in all units.
 struct Item {
   int b, first, rr0, rr_end, kvh, u0, u1, nu, local, end;
-  int skip;  // keys before the first unit
+  int from, skip;  // first key; keys before the first unit
 };
 
 // The item at unit `at` of a run that ends at `stop`.
@@ -782,7 +782,8 @@ __device__ __forceinline__ Item locate(const CacheFwdParams& p, bool split,
   it.first = __builtin_amdgcn_readfirstlane(req.first);
   it.rr_end = __builtin_amdgcn_readfirstlane(req.end - req.first) * p.group;
   it.local = __builtin_amdgcn_readfirstlane(req.local);
-  it.skip = RULE ? __builtin_amdgcn_readfirstlane(skipped_keys(req)) : 0;
+  it.from = RULE ? __builtin_amdgcn_readfirstlane(first_key(req)) : 0;
+  it.skip = it.from & ~(kStep - 1);
   it.nu = split ? max((it.local - it.skip + (1 << p.unit_log2) - 1) >>
                           p.unit_log2,
                       1)
@@ -1007,7 +1008,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
           if (whole) {
             const TokenHead th = token_head(p, rr, prev.kvh);
             store_row<D, OUT_F32, RULE>(p, prev.first + th.tok, th.head,
-                                        prev.local, dim0, acc, ref, L);
+                                        prev.from, prev.local, dim0, acc, ref, L);
           } else {
             const int64_t pr = int64_t{slot} * kRows + 16 * q + row16;
             if (dim0 == 0) {
@@ -1031,7 +1032,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
       if constexpr (RULE) {
         const uint32_t rr = valid ? it.rr0 + 16 * q + r : it.rr0;
         const TokenHead th = token_head(p, rr, it.kvh);
-        const RuleRow row = rule_row(p, int64_t{it.first} + th.tok, it.local);
+        const RuleRow row =
+            rule_row(p, int64_t{it.first} + th.tok, it.from, it.local);
         st.vis[q] = valid ? row.vis : 0;
         rs.lo[q] = row.lo;
         rs.qpos[q] = row.qpos;
@@ -1112,8 +1114,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
             for (int i = 0; i < 8; ++i)
               acc[i] = st.o[q][(8 * j + i) % (D / 16)][(8 * j + i) / (D / 16)];
             store_row<D, OUT_F32, RULE>(
-                p, it.first + th.tok, th.head, it.local, g * (D / 4) + 8 * j,
-                acc, st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
+                p, it.first + th.tok, th.head, it.from, it.local,
+                g * (D / 4) + 8 * j, acc, st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
           }
         }
       }
@@ -1127,7 +1129,10 @@ void cache_fwd_kernel(CacheFwdParams p) {
       f.rr0 = it.rr0;
       f.rr_end = it.rr_end;
       f.kvh = it.kvh;
-      if (RULE) f.local = it.local;
+      if (RULE) {
+        f.from = it.from;
+        f.local = it.local;
+      }
       f.start = goes_on ? (per * run - it.u0) / per : run;
       const int more_runs = goes_on ? (it.nu - it.u0 - 1) / per
                                     : (it.nu - it.u1 + per - 1) / per;
@@ -1213,8 +1218,8 @@ void cache_fold_kernel(CacheFwdParams p) {
     }
     if (pg == 0 && valid) {
       const TokenHead th = token_head(p, rr, f.kvh);
-      store_row<D, OUT_F32, RULE>(p, f.first + th.tok, th.head, f.local, dim0,
-                                  acc, M == -INFINITY ? 0.f : M, L);
+      store_row<D, OUT_F32, RULE>(p, f.first + th.tok, th.head, f.from,
+                                  f.local, dim0, acc, M == -INFINITY ? 0.f : M, L);
     }
     __syncthreads();
   }
