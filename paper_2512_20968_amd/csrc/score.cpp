@@ -189,7 +189,7 @@ BwdBytes bwd_bytes(const ScoreTile& t, int kv_splits, int q_splits) {
   b.q = q_splits == 1 ? 0
                       : up256(4 * static_cast<size_t>(t.rows_q) * t.hq *
                               t.head_dim * q_splits);
-  b.all = 2 * b.rows + 3 * b.ints + b.stages + 2 * b.kv + b.q;
+  b.all = 2 * b.rows + 4 * b.ints + b.stages + 2 * b.kv + b.q;
   return b;
 }
 
@@ -313,6 +313,7 @@ ma_status_t mesh_attn_score_bwd(const ma_problem_t* prob, const int32_t* q_idx,
   p.lo = reinterpret_cast<int32_t*>(take(b.ints));
   p.hi = reinterpret_cast<int32_t*>(take(b.ints));
   p.pos = reinterpret_cast<int32_t*>(take(b.ints));
+  p.pos_rel = reinterpret_cast<float*>(take(b.ints));
   p.stages = reinterpret_cast<ScoreStage*>(take(b.stages));
   p.part_dk = reinterpret_cast<float*>(take(b.kv));
   p.part_dv = reinterpret_cast<float*>(take(b.kv));

@@ -54,6 +54,7 @@ static_assert(sizeof(ScoreFwdParams) <= 4096, "kernel arguments");
 // = 0: there is none), and what all of them see.
 struct ScoreStage {
   int32_t lo_min, hi_max, lo_max, hi_min;
+  int32_t pos, pad[3];  // its first row's position
 };
 
 struct ScoreBwdParams {
@@ -65,10 +66,11 @@ struct ScoreBwdParams {
   void* dk;
   void* dv;
   float* delta;   // [hq][rows_pad]: <dO, O>
-  float* lse2;    // [hq][rows_pad]: LSE log2(e); +inf for rows that see no key
+  float* lse2;    // [hq][rows_pad]: (LSE - cap) log2(e); +inf: sees no key
   int32_t* lo;    // [rows_pad]: a row's begin, end and position
   int32_t* hi;
   int32_t* pos;
+  float* pos_rel;      // position less that of the stage's first row
   ScoreStage* stages;  // [rows_pad / 64]
   // Partial dK, dV of stages cut into kv_splits parts: [split][rows_kv][hkv][d].
   float* part_dk;

@@ -49,6 +49,8 @@ __global__ __launch_bounds__(NT) void score_prep_kernel(ScoreBwdParams p,
     p.hi[my] = my < t.rows_q ? s.hi : 0;
     p.pos[my] = pos;
     ScoreStage g;
+    g.pos = __builtin_amdgcn_readfirstlane(pos);
+    p.pos_rel[my] = static_cast<float>(pos - g.pos);
     const bool some = s.lo < s.hi;
     g.lo_min = wave_min(some ? s.lo : INT32_MAX);
     g.hi_max = wave_max(s.hi);
@@ -78,15 +80,24 @@ __global__ __launch_bounds__(NT) void score_prep_kernel(ScoreBwdParams p,
 #pragma unroll
   for (int o = kLanes / 2; o > 0; o /= 2) s += __shfl_xor(s, o);
   if (sub == 0 && row < p.rows_pad) {
-    const float lse = valid ? p.lse[int64_t{h} * t.rows_q + row] : -INFINITY;
+    float lse = valid ? p.lse[int64_t{h} * t.rows_q + row] : -INFINITY;
     const int64_t at = int64_t{h} * p.rows_pad + row;
+    // A D that is not finite makes the probabilities NaN instead, which hidden
+    // pairs do not have.
+    if (!(fabsf(s) < INFINITY)) {
+      s = 0.f;
+      if (lse != -INFINITY) lse = NAN;
+    }
     p.delta[at] = s;
-    p.lse2[at] = lse == -INFINITY ? INFINITY : lse * kLog2E;
+    // Without the cap's constant part (see probability()).
+    p.lse2[at] = lse == -INFINITY
+                     ? INFINITY
+                     : fmaf(lse, kLog2E, -t.cap * kLog2E);
   }
 }
 
-// Scores x -> probability and, in *g, its product with the cap's derivative.
-// `far`: |i - j|.
+// Scores x -> probability and, in *g, its product with a quarter of the cap's
+// derivative 4 r (1 - r).  lse2: LSE less the cap; far: |i - j|.
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ float probability(const Cap& cap, float scale_log2,
                                              float slope, float x, float far,
@@ -94,8 +105,8 @@ __device__ __forceinline__ float probability(const Cap& cap, float scale_log2,
   float y, d = 1.f;
   if (CAP) {
     const float r = cap_r(cap, x);
-    y = fmaf(-cap.two, r, cap.one - lse2);
-    d = fmaf(-4.f * r, r, 4.f * r);
+    y = fmaf(-cap.two, r, -lse2);
+    d = fmaf(-r, r, r);
   } else {
     y = fmaf(x, scale_log2, -lse2);
   }
@@ -103,6 +114,39 @@ __device__ __forceinline__ float probability(const Cap& cap, float scale_log2,
   const float e = exp2_fast(y);
   *g = CAP ? e * d : e;
   return e;
+}
+
+// The factor of dQ and dK that the sums lack.
+template <bool CAP>
+__device__ __forceinline__ float grad_scale(const ScoreTile& t) {
+  return CAP ? 4.f * t.scale : t.scale;
+}
+
+template <int N>
+__device__ __forceinline__ bool not_finite(const bf16x8 (&f)[N]) {
+  typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const u32x4v w = __builtin_bit_cast(u32x4v, f[i]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      bad |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
+  }
+  return bad;
+}
+
+// Order of a block of N MFMAs with R LDS operand reads each: the reads of AHEAD
+// MFMAs in flight ahead of the MFMA that uses them.
+template <int N, int R, int AHEAD>
+__device__ __forceinline__ void pipeline_reads() {
+  __builtin_amdgcn_sched_group_barrier(0x100, R * AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < N - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -118,7 +162,7 @@ struct KvLayout {
 };
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // Eight values from LDS byte address a.
 template <typename V8, typename V4>
@@ -127,7 +171,11 @@ __device__ __forceinline__ V8 lds_eight(uint32_t a) {
   const V4 lo = *(T*)a, hi = *(T*)(a + 16);
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-typedef int i32x4 __attribute__((ext_vector_type(4)));
+template <typename V4>
+__device__ __forceinline__ V4 lds_four(uint32_t a) {
+  typedef __attribute__((address_space(3))) const V4 T;
+  return *(T*)a;
+}
 
 __device__ __forceinline__ void stage_words(const void* src, char* dst,
                                             int lane) {
@@ -138,7 +186,8 @@ __device__ __forceinline__ void stage_words(const void* src, char* dst,
 }
 
 template <int D, bool CAP, bool BIAS, bool OUT_F32>
-__global__ __launch_bounds__(NT, 2) void score_dkdv_kernel(ScoreBwdParams p) {
+__global__ __launch_bounds__(NT, D == 128 ? 2 : 3)
+void score_dkdv_kernel(ScoreBwdParams p) {
   using L = KvLayout<D>;
   using T = Staged<D>;
   constexpr int kRow = T::kRowBytes;
@@ -164,7 +213,7 @@ __global__ __launch_bounds__(NT, 2) void score_dkdv_kernel(ScoreBwdParams p) {
   const int key0 = blk * kScoreRows, my_key = key0 + wave * 32 + li;
   const bool valid = my_key < g.len;
   const int key = min(my_key, g.len - 1);
-  const int kpos = g.pos + key * t.step;
+  const int kpos = valid ? g.pos + key * t.step : INT32_MAX;
   const int wg_first = g.pos + key0 * t.step;
   const int wg_last =
       g.pos + (min(key0 + kScoreRows, g.len) - 1) * t.step;
@@ -173,6 +222,7 @@ __global__ __launch_bounds__(NT, 2) void score_dkdv_kernel(ScoreBwdParams p) {
   const int wave_last = __builtin_amdgcn_readfirstlane(
       g.pos + (min(key0 + wave * 32 + 32, g.len) - 1) * t.step);
   const bool wave_whole = key0 + wave * 32 + 32 <= g.len;
+  const bool wg_whole = key0 + kScoreRows <= g.len;
 
   bf16x8 kf[D / 16], vf[D / 16];
   {
@@ -230,6 +280,10 @@ __global__ __launch_bounds__(NT, 2) void score_dkdv_kernel(ScoreBwdParams p) {
     return at;
   };
   auto load = [&](int at, int buf) {
+    // Not known to be the same from call to call: the loads' offsets are made
+    // here instead of being held in registers through the loop.
+    int lane = tid & 63;
+    asm volatile("" : "+v"(lane));
     char* dst = smem + buf * L::kStage;
     const int gh = at / stages, s = at - gh * stages;
     const int h = hk * t.group + gh;
@@ -243,7 +297,7 @@ __global__ __launch_bounds__(NT, 2) void score_dkdv_kernel(ScoreBwdParams p) {
     if (wave == 1) stage_words(p.delta + hr, f + 256, lane);
     if (wave == 2) stage_words(p.lo + row, f + 512, lane);
     if (wave == 3) stage_words(p.hi + row, f + 768, lane);
-    if (BIAS && wave == 0) stage_words(p.pos + row, f + 1024, lane);
+    if (BIAS && wave == 0) stage_words(p.pos_rel + row, f + 1024, lane);
   };
 
   int cur = __builtin_amdgcn_readfirstlane(next_stage());
@@ -257,123 +311,158 @@ __global__ __launch_bounds__(NT, 2) void score_dkdv_kernel(ScoreBwdParams p) {
     wait_vmem();
     __syncthreads();
     int buf = 0;
+    const bool keys_bad = __any(not_finite(kf) || not_finite(vf));
+    // Operand addresses with the stage's base in them.
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
-    const uint32_t ra = lds0 + T::row_read(lane);
-    const uint32_t t0 = lds0 + T::tr_read(lane, 0);
-    const uint32_t t1 = lds0 + T::tr_read(lane, 1);
-    const uint32_t fa = lds0 + L::kFloats + lh * 32;
+    uint32_t ra = lds0 + T::row_read(lane);
+    uint32_t t0 = lds0 + T::tr_read(lane, 0);
+    uint32_t t1 = lds0 + T::tr_read(lane, 1);
+    uint32_t fa = lds0 + L::kFloats + lh * 32;
     for (;;) {
       const int nxt = __builtin_amdgcn_readfirstlane(next_stage());
       if (nxt >= 0) load(nxt, buf ^ 1);
-      const uint32_t sb = buf * L::kStage;
       const int gh = cur / stages;
       const ScoreStage st = load_const(p.stages, cur - gh * stages);
       const float slope =
           BIAS ? load_const(t.slopes, hk * t.group + gh) * kLog2E : 0.f;
+      // 0 times an infinity or a NaN of a row that does not see the key is NaN:
+      // in stages that some of the workgroup's pairs are hidden in, rows that
+      // hold one give NaN to the keys that they see, and zeros to the products.
+      uint64_t bad = 0;
+      if (!wg_whole || st.lo_max > wg_first || st.hi_min <= wg_last) {
+        char* at = smem + buf * L::kStage;
+        if (tile_not_finite<D>(at, lane) ||
+            tile_not_finite<D>(at + L::kTile, lane)) {
+          bad = rows_not_finite<D>(at, lane) |
+                rows_not_finite<D>(at + L::kTile, lane);
+          lds_barrier();  // every wave has looked
+          clear_not_finite<D>(at, tid);
+          clear_not_finite<D>(at + L::kTile, tid);
+          lds_barrier();
+        }
+      }
       const bool touched = st.lo_min <= wave_last && st.hi_max > wave_first;
       if (touched) {
         const bool full = wave_whole && st.lo_max <= wave_first &&
                           st.hi_min > wave_last;
-        // 0 times an infinity or a NaN of a row that does not see the key is
-        // NaN: rows that hold one give NaN to the keys that they see, and zeros
-        // to the products.
-        uint64_t bad = 0;
-        if (!full) {
-          const bool q_bad = tile_not_finite<D>(smem + sb, lane);
-          const bool o_bad = tile_not_finite<D>(smem + sb + L::kTile, lane);
-          if (q_bad || o_bad)
-            bad = rows_not_finite<D>(smem + sb, lane) |
-                  rows_not_finite<D>(smem + sb + L::kTile, lane);
-        }
+        const bool fix = bad != 0 || (!full && keys_bad);
+        const float kpos_rel = BIAS ? static_cast<float>(kpos - st.pos) : 0.f;
 #pragma unroll
         for (int qt = 0; qt < 2; ++qt) {
           f32x16 x;
-          zero(x);
+          auto scores = [&](const bf16x8 (&f)[D / 16], int tile) {
+            zero(x);
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            x = mfma32(lds_row((ra ^ (32 * kk)) + sb + qt * 32 * kRow), kf[kk],
-                       x);
+            for (int kk = 0; kk < D / 16; ++kk)
+              x = mfma32(lds_row((ra ^ (32 * kk)) + tile + qt * 32 * kRow),
+                         f[kk], x);
+            pipeline_reads<D / 16, 1, 3>();
+          };
+          scores(kf, 0);
+          // Four queries at a time: more would not fit the registers.
+          bf16x4 p4[4], d4[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t at = fa + 4 * (qt * 32 + (i >> 1) * 16 + (i & 1) * 4);
+            f32x4 lse = lds_four<f32x4>(at);
+            if (!full) {
+              const i32x4 lo = lds_four<i32x4>(at + 512);
+              const i32x4 hi = lds_four<i32x4>(at + 768);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (kpos < lo[e] || kpos >= hi[e]) lse[e] = INFINITY;
+            }
+            f32x4 e4, g4, pos;
+            if (BIAS) pos = lds_four<f32x4>(at + 1024);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float far = BIAS ? fabsf(pos[e] - kpos_rel) : 0.f;
+              float g1;
+              e4[e] = probability<CAP, BIAS>(cap, t.scale_log2, slope,
+                                             x[i * 4 + e], far, lse[e], &g1);
+              g4[e] = g1;
+            }
+            if (fix) {
+              const uint32_t b4 = static_cast<uint32_t>(
+                  bad >> (qt * 32 + (i >> 1) * 16 + 8 * lh + (i & 1) * 4));
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float nan = (b4 >> e) & 1 ? NAN : 0.f;
+                const bool hidden = lse[e] == INFINITY;
+                e4[e] = hidden ? 0.f : e4[e] + nan;
+                g4[e] = hidden ? 0.f : g4[e] + nan;
+              }
+            }
+            p4[i] = __builtin_convertvector(e4, bf16x4);
+            // Unpacked below instead of rounded again.
+            asm("" : "+v"(p4[i]));
+            if (CAP) {
+              d4[i] = __builtin_convertvector(g4, bf16x4);
+              asm("" : "+v"(d4[i]));
+            }
+            if (D == 128) __builtin_amdgcn_sched_barrier(0);
+          }
+          scores(vf, L::kTile);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t at =
+                fa + 256 + 4 * (qt * 32 + (i >> 1) * 16 + (i & 1) * 4);
+            const f32x4 dlt = lds_four<f32x4>(at);
+            f32x4 g4 = __builtin_convertvector(CAP ? d4[i] : p4[i], f32x4);
+            f32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = x[i * 4 + e] - dlt[e];
+            if (fix) {  // a hidden pair's product with a NaN of dO V^T is 0
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (g4[e] == 0.f) y[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g4[e] *= y[e];
+            d4[i] = __builtin_convertvector(g4, bf16x4);
+            if (D == 128) __builtin_amdgcn_sched_barrier(0);
+          }
           bf16x8 pf[2], ds[2];
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
-            const uint32_t at = fa + sb + 4 * (qt * 32 + hh * 16);
-            const f32x8 lse = lds_eight<f32x8, f32x4>(at);
-            f32x8 e8, g8;
-            i32x8 pos;
-            if (BIAS) pos = lds_eight<i32x8, i32x4>(at + 1024);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float far =
-                  BIAS ? fabsf(static_cast<float>(pos[e] - kpos)) : 0.f;
-              float g1;
-              e8[e] = probability<CAP, BIAS>(cap, t.scale_log2, slope,
-                                             x[hh * 8 + e], far, lse[e], &g1);
-              g8[e] = g1;
-            }
-            if (!full) {
-              const i32x8 lo = lds_eight<i32x8, i32x4>(at + 512);
-              const i32x8 hi = lds_eight<i32x8, i32x4>(at + 768);
-              const uint32_t b8 = static_cast<uint32_t>(
-                  bad >> (qt * 32 + hh * 16 + 8 * lh)) & 255u;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const bool sees = valid && lo[e] <= kpos && kpos < hi[e];
-                const float nan = (b8 >> e) & 1 ? NAN : 0.f;
-                e8[e] = sees ? e8[e] + nan : 0.f;
-                g8[e] = sees ? g8[e] + nan : 0.f;
-              }
-            }
-            pf[hh] = __builtin_convertvector(e8, bf16x8);
-            if (CAP) ds[hh] = __builtin_convertvector(g8, bf16x8);
-          }
-          f32x16 y;
-          zero(y);
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            y = mfma32(lds_row((ra ^ (32 * kk)) + sb + L::kTile +
-                               qt * 32 * kRow),
-                       vf[kk], y);
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            const uint32_t at = fa + sb + 256 + 4 * (qt * 32 + hh * 16);
-            const f32x8 dlt = lds_eight<f32x8, f32x4>(at);
-            f32x8 g8 = __builtin_convertvector(CAP ? ds[hh] : pf[hh], f32x8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float d = y[hh * 8 + e] - dlt[e];
-              // A hidden pair's product with a NaN of dO V^T is 0.
-              g8[e] = full || g8[e] != 0.f ? g8[e] * d : 0.f;
-            }
-            ds[hh] = __builtin_convertvector(g8, bf16x8);
+            pf[hh] = __builtin_shufflevector(p4[2 * hh], p4[2 * hh + 1], 0, 1,
+                                             2, 3, 4, 5, 6, 7);
+            ds[hh] = __builtin_shufflevector(d4[2 * hh], d4[2 * hh + 1], 0, 1,
+                                             2, 3, 4, 5, 6, 7);
           }
 #pragma unroll
           for (int c = 0; c < D / 32; ++c)
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
+              const uint32_t a0 = t0 ^ (64 * c), a1 = t1 ^ (64 * c);
               const int at = (2 * qt + hh) * 16 * kRow;
-              bf16x8 a = lds_tr((t0 ^ (64 * c)) + sb, (t1 ^ (64 * c)) + sb,
-                                L::kTile + at);
-              bf16x8 b = lds_tr((t0 ^ (64 * c)) + sb, (t1 ^ (64 * c)) + sb, at);
-              if (bad) {
-                a = finite_or_zero(a);
-                b = finite_or_zero(b);
-              }
-              acc_v[c] = mfma32(pf[hh], a, acc_v[c]);
-              acc_k[c] = mfma32(ds[hh], b, acc_k[c]);
+              acc_v[c] = mfma32(pf[hh], lds_tr(a0, a1, L::kTile + at), acc_v[c]);
+              acc_k[c] = mfma32(ds[hh], lds_tr(a0, a1, at), acc_k[c]);
             }
+          pipeline_reads<D / 8, 2, 2>();
         }
       }
       if (nxt < 0) break;
       wait_vmem();
       lds_barrier();
+      const int d = buf ? -L::kStage : L::kStage;
+      ra += d;
+      t0 += d;
+      t1 += d;
+      fa += d;
       buf ^= 1;
       cur = nxt;
     }
   }
 
   // Register i of chunk c: key 8 (i / 4) + 4 lh + i % 4 of the wave, dim 32 c + li.
+  {
+  int lane = tid & 63;
+  asm volatile("" : "+v"(lane));
+  const int li = lane & 31, lh = lane >> 5;
   const bool whole = p.kv_splits == 1;
   const int64_t all_out = int64_t{t.rows_kv} * t.hkv * D;
+  const float out_scale = grad_scale<CAP>(t);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int k = key0 + wave * 32 + 8 * (i >> 2) + 4 * lh + (i & 3);
@@ -381,7 +470,7 @@ __global__ __launch_bounds__(NT, 2) void score_dkdv_kernel(ScoreBwdParams p) {
     const int64_t at = ((int64_t{g.row} + k) * t.hkv + hk) * D + li;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
-      const float dv = acc_v[c][i], dk = acc_k[c][i] * t.scale;
+      const float dv = acc_v[c][i], dk = acc_k[c][i] * out_scale;
       if (!whole) {
         p.part_dv[part * all_out + at + 32 * c] = dv;
         p.part_dk[part * all_out + at + 32 * c] = dk;
@@ -393,6 +482,7 @@ __global__ __launch_bounds__(NT, 2) void score_dkdv_kernel(ScoreBwdParams p) {
         static_cast<__bf16*>(p.dk)[at + 32 * c] = static_cast<__bf16>(dk);
       }
     }
+  }
   }
 }
 
@@ -566,6 +656,7 @@ void score_dq_kernel(ScoreBwdParams p) {
   const bool whole = p.q_splits == 1;
   const int64_t o0 = (int64_t{my_row} * t.hq + h) * D;
   const int64_t all = int64_t{t.rows_q} * t.hq * D;
+  const float out_scale = grad_scale<CAP>(t);
 #pragma unroll
   for (int c = 0; c < D / 32; ++c)
 #pragma unroll
@@ -573,7 +664,7 @@ void score_dq_kernel(ScoreBwdParams p) {
       const int dim = c * 32 + g * 8 + lh * 4;
       f32x4 x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = acc[c][4 * g + e] * t.scale;
+      for (int e = 0; e < 4; ++e) x[e] = acc[c][4 * g + e] * out_scale;
       if (!whole) {
         *reinterpret_cast<f32x4*>(p.part_dq + part * all + o0 + dim) = x;
       } else if (OUT_F32) {

@@ -123,6 +123,16 @@ __device__ __forceinline__ uint64_t rows_not_finite(const char* tile,
   return __builtin_amdgcn_ballot_w64(bad);
 }
 
+// Zeros for what is not finite in a staged tile, by the whole workgroup.
+template <int D>
+__device__ __forceinline__ void clear_not_finite(char* tile, int tid) {
+#pragma unroll 1
+  for (int i = tid; i < Staged<D>::kBytes / 16; i += kThreads) {
+    bf16x8* at = reinterpret_cast<bf16x8*>(tile + 16 * i);
+    *at = finite_or_zero(*at);
+  }
+}
+
 // Which stored positions a query row sees, [lo, hi); lo = hi = 0 for none.
 struct Seen {
   int lo, hi;
