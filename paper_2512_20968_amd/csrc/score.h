@@ -78,6 +78,7 @@ struct ScoreBwdParams {
   // Partial dQ of keys cut into q_splits parts: [split][rows_q][hq][d].
   float* part_dq;
   int32_t rows_pad, kv_splits, q_splits;
+  int32_t kv_items;  // workgroups of dK/dV, those of dQ come behind
 };
 static_assert(sizeof(ScoreBwdParams) <= 4096, "kernel arguments");
 

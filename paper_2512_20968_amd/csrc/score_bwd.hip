@@ -186,17 +186,15 @@ __device__ __forceinline__ void stage_words(const void* src, char* dst,
 }
 
 template <int D, bool CAP, bool BIAS, bool OUT_F32>
-__global__ __launch_bounds__(NT, D == 128 ? 2 : 3)
-void score_dkdv_kernel(ScoreBwdParams p) {
+__device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
+                                          int id) {
   using L = KvLayout<D>;
   using T = Staged<D>;
   constexpr int kRow = T::kRowBytes;
-  extern __shared__ __align__(16) char smem[];
   const ScoreTile& t = p.t;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  int id = blockIdx.x;
   const int hk = id % t.hkv;
   id /= t.hkv;
   const int part = id % p.kv_splits;
@@ -497,17 +495,15 @@ struct QLayout {
 };
 
 template <int D, bool CAP, bool BIAS, bool OUT_F32>
-__global__ __launch_bounds__(NT, D == 128 ? 2 : 3)
-void score_dq_kernel(ScoreBwdParams p) {
+__device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
+                                        int id) {
   using L = QLayout<D>;
   using T = Staged<D>;
   constexpr int kRow = T::kRowBytes;
-  extern __shared__ __align__(16) char smem[];
   const ScoreTile& t = p.t;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qblocks = (t.rows_q + kScoreRows - 1) / kScoreRows;
-  int id = blockIdx.x;
   const int hk = id % t.hkv;
   id /= t.hkv;
   const int h = hk * t.group + id % t.group;
@@ -678,6 +674,19 @@ void score_dq_kernel(ScoreBwdParams p) {
     }
 }
 
+// Both passes in one launch: the dK/dV items first, the longest of a causal tile
+// at their front, and dQ items wherever one of them ends.
+template <int D, bool CAP, bool BIAS, bool OUT_F32>
+__global__ __launch_bounds__(NT, D == 128 ? 2 : 3)
+void score_bwd_kernel(ScoreBwdParams p) {
+  extern __shared__ __align__(16) char smem[];
+  const int id = blockIdx.x;
+  if (id < p.kv_items)
+    dkdv_item<D, CAP, BIAS, OUT_F32>(p, smem, id);
+  else
+    dq_item<D, CAP, BIAS, OUT_F32>(p, smem, id - p.kv_items);
+}
+
 // ---------------------------------------------------------------------------
 // Sums of partial gradients, four elements a thread, in the parts' order.
 // ---------------------------------------------------------------------------
@@ -727,11 +736,10 @@ hipError_t launch_sum(const SumParams& p, int arrays, bool out_f32,
 
 template <int D, bool CAP, bool BIAS, bool OUT_F32>
 hipError_t launch(const ScoreBwdParams& p, hipStream_t stream) {
-  constexpr auto dkdv = score_dkdv_kernel<D, CAP, BIAS, OUT_F32>;
-  constexpr auto dq = score_dq_kernel<D, CAP, BIAS, OUT_F32>;
-  constexpr int kv_lds = KvLayout<D>::kLds, q_lds = QLayout<D>::kLds;
-  hipError_t e = ensure_dynamic_lds<dkdv>(kv_lds);
-  if (e == hipSuccess) e = ensure_dynamic_lds<dq>(q_lds);
+  constexpr auto kernel = score_bwd_kernel<D, CAP, BIAS, OUT_F32>;
+  constexpr int lds = KvLayout<D>::kLds;
+  static_assert(lds >= QLayout<D>::kLds, "one launch for both passes");
+  hipError_t e = ensure_dynamic_lds<kernel>(lds);
   if (e != hipSuccess) return e;
   const ScoreTile& t = p.t;
   const int range_groups = (p.rows_pad / 64 + NT / 64 - 1) / (NT / 64);
@@ -742,15 +750,12 @@ hipError_t launch(const ScoreBwdParams& p, hipStream_t stream) {
       dim3(NT), 0, stream, p, range_groups);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t kv_items = int64_t{t.kv_blocks128} * t.hkv * p.kv_splits;
-  hipLaunchKernelGGL(dkdv, dim3(static_cast<unsigned>(kv_items)), dim3(NT),
-                     kv_lds, stream, p);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  ScoreBwdParams q = p;
+  q.kv_items = t.kv_blocks128 * t.hkv * p.kv_splits;
   const int64_t q_items =
       (int64_t{t.rows_q} + kScoreRows - 1) / kScoreRows * t.hq * p.q_splits;
-  hipLaunchKernelGGL(dq, dim3(static_cast<unsigned>(q_items)), dim3(NT), q_lds,
-                     stream, p);
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(q.kv_items + q_items)),
+                     dim3(NT), lds, stream, q);
   e = hipGetLastError();
   if (e == hipSuccess && p.kv_splits > 1) {
     SumParams s{{p.part_dk, p.part_dv},
@@ -780,17 +785,22 @@ hipError_t launch_d(const ScoreBwdParams& p, hipStream_t stream) {
 
 }  // namespace
 
+// Parts so that dK/dV has 512 items, two for each of 256 compute units, and dQ 128
+// beside them.  Microseconds of (head dim 64, 3001 rows, 12/4 heads; documents in
+// 4096 rows of 32/8 heads of 128; 8192 causal rows of those) for dK/dV 256 / 512 /
+// 1024: 68, 213, 2214 / 60, 175, 2163 / 69, 194, 2163; dQ 512 instead of 128: 65,
+// 173, 2173.
 void score_bwd_splits(const ScoreTile& t, int* kv_splits, int* q_splits) {
-  auto parts = [](int64_t items, int64_t blocks) {
-    if (items >= 256) return 1;
-    const int64_t want = 512 / items, most = blocks / 4;
+  auto parts = [](int64_t items, int64_t blocks, int64_t target) {
+    const int64_t want = (target + items - 1) / items, most = blocks / 4;
     const int64_t n = want < most ? want : most;
     return static_cast<int>(n < 1 ? 1 : n > 32 ? 32 : n);
   };
   const int64_t stages = (int64_t{t.rows_q} + 63) / 64;
-  *kv_splits = parts(int64_t{t.kv_blocks128} * t.hkv, stages * t.group);
+  *kv_splits = parts(int64_t{t.kv_blocks128} * t.hkv, stages * t.group,
+                     512);
   *q_splits = parts((int64_t{t.rows_q} + kScoreRows - 1) / kScoreRows * t.hq,
-                    t.kv_blocks64);
+                    t.kv_blocks64, 128);
 }
 
 hipError_t launch_score_bwd(const ScoreBwdParams& p, bool out_f32,
