@@ -65,7 +65,7 @@ struct ScoreBwdParams {
   void* dq;
   void* dk;
   void* dv;
-  float* delta;   // [hq][rows_pad]: <dO, O>
+  float* delta;   // [hq][rows_pad]: -<dO, O>
   float* lse2;    // [hq][rows_pad]: (LSE - cap) log2(e); +inf: sees no key
   int32_t* lo;    // [rows_pad]: a row's begin, end and position
   int32_t* hi;

@@ -88,7 +88,7 @@ __global__ __launch_bounds__(NT) void score_prep_kernel(ScoreBwdParams p,
       s = 0.f;
       if (lse != -INFINITY) lse = NAN;
     }
-    p.delta[at] = s;
+    p.delta[at] = -s;
     // Without the cap's constant part (see probability()).
     p.lse2[at] = lse == -INFINITY
                      ? INFINITY
@@ -134,19 +134,6 @@ __device__ __forceinline__ bool not_finite(const bf16x8 (&f)[N]) {
       bad |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
   }
   return bad;
-}
-
-// Order of a block of N MFMAs with R LDS operand reads each: the reads of AHEAD
-// MFMAs in flight ahead of the MFMA that uses them.
-template <int N, int R, int AHEAD>
-__device__ __forceinline__ void pipeline_reads() {
-  __builtin_amdgcn_sched_group_barrier(0x100, R * AHEAD, 0);
-#pragma unroll
-  for (int i = 0; i < N - AHEAD; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
-  }
-  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -349,13 +336,13 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
         for (int qt = 0; qt < 2; ++qt) {
           f32x16 x;
           auto scores = [&](const bf16x8 (&f)[D / 16], int tile) {
-            zero(x);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
               x = mfma32(lds_row((ra ^ (32 * kk)) + tile + qt * 32 * kRow),
                          f[kk], x);
             pipeline_reads<D / 16, 1, 3>();
           };
+          zero(x);
           scores(kf, 0);
           // Four queries at a time: more would not fit the registers.
           bf16x4 p4[4], d4[4];
@@ -400,16 +387,21 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
             }
             if (D == 128) __builtin_amdgcn_sched_barrier(0);
           }
+          // dO V^T - D: the accumulators start with -D.
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 dlt = lds_four<f32x4>(
+                fa + 256 + 4 * (qt * 32 + (i >> 1) * 16 + (i & 1) * 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i * 4 + e] = dlt[e];
+          }
           scores(vf, L::kTile);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t at =
-                fa + 256 + 4 * (qt * 32 + (i >> 1) * 16 + (i & 1) * 4);
-            const f32x4 dlt = lds_four<f32x4>(at);
             f32x4 g4 = __builtin_convertvector(CAP ? d4[i] : p4[i], f32x4);
             f32x4 y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = x[i * 4 + e] - dlt[e];
+            for (int e = 0; e < 4; ++e) y[e] = x[i * 4 + e];
             if (fix) {  // a hidden pair's product with a NaN of dO V^T is 0
 #pragma unroll
               for (int e = 0; e < 4; ++e)
@@ -516,7 +508,7 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
   const int qpos = p.pos[row];
   const Seen seen{p.lo[row], p.hi[row]};
   const int64_t hr = int64_t{h} * p.rows_pad + row;
-  const float lse2 = p.lse2[hr], dlt = p.delta[hr];
+  const float lse2 = p.lse2[hr], neg_delta = p.delta[hr];
   bf16x8 qf[D / 16], dof[D / 16];
   {
     const uint16_t* qs = t.q + row * t.q_stride + int64_t{h} * D + lh * 8;
@@ -537,6 +529,9 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
       load_const(p.stages, min(2 * qblk + 1, p.rows_pad / kScoreBlock - 1));
   const int lo_min = min(s0.lo_min, s1.lo_min);
   const int hi_max = max(s0.hi_max, s1.hi_max);
+  // (Rows behind the last one see nothing here: their stages count as masked.)
+  const int lo_max = max(s0.lo_max, s1.lo_max);
+  const int hi_min = min(s0.hi_min, s1.hi_min);
   KeyWalk w;
   w.start(t, lo_min < hi_max ? lo_min : 0, lo_min < hi_max ? hi_max : 0, part,
           p.q_splits);
@@ -560,27 +555,27 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
       some_b = wave_max(b);
     };
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
-    const uint32_t ra = lds0 + T::row_read(lane);
-    const uint32_t t0 = lds0 + T::tr_read(lane, 0);
-    const uint32_t t1 = lds0 + T::tr_read(lane, 1);
-    auto compute = [&](int k0, int pos0, int buf) {
-      const uint32_t sb = buf * L::kStage;
+    uint32_t ra = lds0 + T::row_read(lane);
+    uint32_t t0 = lds0 + T::tr_read(lane, 0);
+    uint32_t t1 = lds0 + T::tr_read(lane, 1);
+    // bad: keys that are not finite, cleared in LDS: the rows that see them get
+    // NaN.
+    auto compute = [&](int k0, int pos0, uint64_t bad) {
       const bool full = all_a <= k0 && k0 + kScoreBlock <= all_b;
-      uint64_t bad = 0;
-      if (!full && tile_not_finite<D>(smem + sb, lane))
-        bad = rows_not_finite<D>(smem + sb, lane);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
         f32x16 x, y;
         zero(x);
-        zero(y);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = neg_delta;
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          x = mfma32(lds_row((ra ^ (32 * kk)) + sb + kt * 32 * kRow), qf[kk], x);
+          x = mfma32(lds_row((ra ^ (32 * kk)) + kt * 32 * kRow), qf[kk], x);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          y = mfma32(lds_row((ra ^ (32 * kk)) + sb + L::kTile + kt * 32 * kRow),
+          y = mfma32(lds_row((ra ^ (32 * kk)) + L::kTile + kt * 32 * kRow),
                      dof[kk], y);
+        pipeline_reads<D / 8, 1, 3>();
         const float d0 = BIAS ? static_cast<float>(int64_t{qpos} - pos0 -
                                                    int64_t{t.step} *
                                                        (32 * kt + 8 * lh))
@@ -598,9 +593,9 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
             float g1;
             probability<CAP, BIAS>(cap, t.scale_log2, slope, x[hh * 8 + e], far,
                                    lse2, &g1);
-            g8[e] = g1 * (y[hh * 8 + e] - dlt);
+            g8[e] = g1 * y[hh * 8 + e];
           }
-          if (!full) {
+          if (!full || bad != 0) {
             const int j0 = k0 + 32 * kt + 16 * hh + 8 * lh;
             const uint32_t b8 = static_cast<uint32_t>(
                 bad >> (32 * kt + 16 * hh + 8 * lh)) & 255u;
@@ -617,11 +612,11 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
-            bf16x8 k = lds_tr((t0 ^ (64 * c)) + sb, (t1 ^ (64 * c)) + sb,
-                              (2 * kt + hh) * 16 * kRow);
-            if (bad) k = finite_or_zero(k);
+            const bf16x8 k = lds_tr(t0 ^ (64 * c), t1 ^ (64 * c),
+                                    (2 * kt + hh) * 16 * kRow);
             acc[c] = mfma32(k, ds[hh], acc[c]);
           }
+        pipeline_reads<D / 16, 2, 2>();
       }
     };
     load(0);
@@ -637,14 +632,32 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
     for (;;) {
       const int k0 = w.blk * kScoreBlock;
       const int pos0 = w.g.pos + k0 * t.step;
+      const bool all_see =
+          lo_max <= pos0 && pos0 + int64_t{t.step} * (kScoreBlock - 1) < hi_min &&
+          k0 + kScoreBlock <= w.g.len;
       const bool more = w.left > 1;
       const bool changed = more && w.next(t);
       if (more) load(buf ^ 1);
-      if (some_a < k0 + kScoreBlock && k0 < some_b) compute(k0, pos0, buf);
+      // 0 times an infinity or a NaN of a hidden key is NaN.
+      uint64_t bad = 0;
+      if (!all_see) {
+        char* at = smem + buf * L::kStage;
+        if (tile_not_finite<D>(at, lane)) {
+          bad = rows_not_finite<D>(at, lane);
+          lds_barrier();  // every wave has looked
+          clear_not_finite<D>(at, tid);
+          lds_barrier();
+        }
+      }
+      if (some_a < k0 + kScoreBlock && k0 < some_b) compute(k0, pos0, bad);
       if (!more) break;
       if (changed) enter_segment();
       wait_vmem();
       lds_barrier();
+      const int step = buf ? -L::kStage : L::kStage;
+      ra += step;
+      t0 += step;
+      t1 += step;
       buf ^= 1;
     }
   }

@@ -34,7 +34,7 @@ template <int D>
 struct Layout {
   static constexpr int kTile = Staged<D>::kBytes;
   static constexpr int kStage = 2 * kTile;  // K, V
-  static constexpr int kLds = 2 * kStage + 8 * 4;  // .. the waves' key ranges
+  static constexpr int kLds = 2 * kStage + 16 * 4;  // .. the waves' key ranges
 };
 
 // EXACT (float32 O): the probabilities enter the second product as a sum of three
@@ -48,8 +48,8 @@ void score_fwd_kernel(ScoreFwdParams p) {
   constexpr int kRow = T::kRowBytes;
   extern __shared__ __align__(16) char smem[];
   // (The dynamic LDS starts at 0: operand addresses are XORed.)
-  int* s_lo = reinterpret_cast<int*>(smem + 2 * L::kStage);
-  int* s_hi = s_lo + 4;
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  i32x4* s_range = reinterpret_cast<i32x4*>(smem + 2 * L::kStage);
   const ScoreTile& t = p.t;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -72,12 +72,10 @@ void score_fwd_kernel(ScoreFwdParams p) {
   const int qpos = row_position(t, row);
   const Seen seen = row_seen(t, row, qpos);
   {
-    const int lo = wave_min(seen.lo < seen.hi ? seen.lo : INT32_MAX);
-    const int hi = wave_max(seen.hi);
-    if (lane == 0) {
-      s_lo[wave] = lo;
-      s_hi[wave] = hi;
-    }
+    // Positions that some row sees, and those that all rows see.
+    const i32x4 r = {wave_min(seen.lo < seen.hi ? seen.lo : INT32_MAX),
+                     wave_max(seen.hi), wave_max(seen.lo), wave_min(seen.hi)};
+    if (lane == 0) s_range[wave] = r;
   }
   bf16x8 qf[D / 16];
   {
@@ -91,8 +89,16 @@ void score_fwd_kernel(ScoreFwdParams p) {
   for (int c = 0; c < D / 32; ++c) zero(oacc[c]);
   float m = -INFINITY, l = 0.f;
   const Cap cap = cap_of(t);
-  // Scores are kept as products (scaled in the exponent) or in log2 units.
-  const float unit = CAP || BIAS ? 1.f : t.scale_log2;
+  // What is kept of a score: its product (scaled in the exponent), the r of the
+  // cap (x = one - two r, the least of which is the largest score), or, with a
+  // bias or a float32 O, x itself in log2 units.
+  constexpr bool kAsR = CAP && !BIAS && !EXACT;
+  const float unit = kAsR ? -cap.two : CAP || BIAS ? 1.f : t.scale_log2;
+  const float base = kAsR ? cap.one : 0.f;
+  // Scores under a moderate cap need no running maximum: all probabilities lie
+  // between 2^-120 and 2^40 around a fixed reference.
+  const bool fixed = kAsR && cap.two <= 160.f;
+  if (fixed) m = fminf(cap.one, 120.f - cap.one);
   const float slope = BIAS ? t.slopes[h] * kLog2E : 0.f;
   const int pos_min = BIAS ? wave_min(qpos) : 0;
   const int pos_max = BIAS ? wave_max(qpos) : 0;
@@ -116,12 +122,19 @@ void score_fwd_kernel(ScoreFwdParams p) {
     off = nearest == INT64_MAX ? 0 : static_cast<int>(nearest);
   }
   __syncthreads();
-  const int lo_min =
-      __builtin_amdgcn_readfirstlane(min(min(s_lo[0], s_lo[1]),
-                                         min(s_lo[2], s_lo[3])));
-  const int hi_max =
-      __builtin_amdgcn_readfirstlane(max(max(s_hi[0], s_hi[1]),
-                                         max(s_hi[2], s_hi[3])));
+  i32x4 range = s_range[0];
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
+    const i32x4 r = s_range[i];
+    range[0] = min(range[0], r[0]);
+    range[1] = max(range[1], r[1]);
+    range[2] = max(range[2], r[2]);
+    range[3] = min(range[3], r[3]);
+  }
+  const int lo_min = __builtin_amdgcn_readfirstlane(range[0]);
+  const int hi_max = __builtin_amdgcn_readfirstlane(range[1]);
+  const int lo_max = __builtin_amdgcn_readfirstlane(range[2]);
+  const int hi_min = __builtin_amdgcn_readfirstlane(range[3]);
   KeyWalk w;
   w.start(t, lo_min < hi_max ? lo_min : 0, lo_min < hi_max ? hi_max : 0, part,
           p.splits);
@@ -147,28 +160,58 @@ void score_fwd_kernel(ScoreFwdParams p) {
       some_b = wave_max(b);
     };
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
-    const uint32_t kra = lds0 + T::row_read(lane);
-    const uint32_t vt0 = lds0 + L::kTile + T::tr_read(lane, 0);
-    const uint32_t vt1 = lds0 + L::kTile + T::tr_read(lane, 1);
+    // Operand addresses with the stage's base in them.
+    uint32_t kra = lds0 + T::row_read(lane);
+    uint32_t vt0 = lds0 + T::tr_read(lane, 0);
+    uint32_t vt1 = lds0 + T::tr_read(lane, 1);
 
-    // One block from stage buffer `buf`: its first key is k0 of the segment.
-    auto compute = [&](int k0, int pos0, int buf) {
-      const uint32_t sb = buf * L::kStage;
+    // Values of a block that some of the workgroup's rows do not see, and that
+    // are not finite, go straight to the rows that see them; the products get
+    // zeros (0 times an infinity or a NaN is NaN).
+    auto take_not_finite = [&](int k0, char* vt) {
+#pragma unroll 1
+      for (int j = 0; j < kScoreBlock; ++j) {
+        if (j < a - k0 || j >= b - k0) continue;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const bf16x4 v4 = *reinterpret_cast<const bf16x4*>(
+                vt + j * kRow + (((4 * c + g) ^ T::swz(j)) * 16) + 8 * lh);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = static_cast<float>(v4[e]);
+              oacc[c][4 * g + e] += v - v == 0.f ? 0.f : v;
+            }
+          }
+      }
+      lds_barrier();  // every wave has read it
+      clear_not_finite<D>(vt, tid);
+      lds_barrier();
+    };
+
+    // One block: its first key is k0 of the segment, at position pos0.
+    auto compute = [&](int k0, int pos0) {
       f32x16 sc[2];
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
         zero(sc[kt]);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          sc[kt] = mfma32(lds_row(((kra ^ (32 * kk)) + sb) + kt * 32 * kRow),
-                          qf[kk], sc[kt]);
+          sc[kt] = mfma32(lds_row((kra ^ (32 * kk)) + kt * 32 * kRow), qf[kk],
+                          sc[kt]);
       }
+      pipeline_reads<D / 8, 1, 3>();
       if (CAP) {
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const float x = sc[kt][i];
+            if (kAsR) {
+              sc[kt][i] = cap_r(cap, x);
+              continue;
+            }
             float y = fmaf(-cap.two, cap_r(cap, x), cap.one);
             if (EXACT) {
               // Taylor; the first term left out is below 2^-25 of the sum.
@@ -221,7 +264,6 @@ void score_fwd_kernel(ScoreFwdParams p) {
         }
       }
       const bool full = all_a <= k0 && k0 + kScoreBlock <= all_b;
-      bool clean = true;
       if (!full) {
         const int x = a - k0 - 8 * lh, y = b - k0 - 8 * lh;
 #pragma unroll
@@ -229,35 +271,38 @@ void score_fwd_kernel(ScoreFwdParams p) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int j = 32 * kt + acc_row(i, 0);
-            if (j < x || j >= y) sc[kt][i] = -INFINITY;
+            if (j < x || j >= y) sc[kt][i] = kAsR ? INFINITY : -INFINITY;
           }
-        // 0 times an infinity or a NaN of a hidden key is NaN.
-        clean = !tile_not_finite<D>(smem + sb + L::kTile, lane);
       }
-      float mx = -INFINITY;
+      if (!fixed) {
+        float top = sc[0][0];
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kt][i]);
-      mx = max_with_other_half(mx) * unit;
-      if (__builtin_amdgcn_ballot_w64(mx > m + kLag)) {
-        const float mn = fmaxf(m, mx);
-        const float alpha =
-            mn == -INFINITY ? 1.f : exp2_fast(m - mn);
-        l *= alpha;
+          for (int i = 0; i < 16; ++i)
+            top = kAsR ? fminf(top, sc[kt][i]) : fmaxf(top, sc[kt][i]);
+        const float mx = max_with_other_half(fmaf(top, unit, base));
+        if (__builtin_amdgcn_ballot_w64(mx > m + kLag)) {
+          const float mn = fmaxf(m, mx);
+          // (Sums before the first score are 0, or what take_not_finite() put
+          // there, which a factor of 0 must not meet.)
+          const float alpha =
+              m == -INFINITY ? 1.f : fmaxf(exp2_fast(m - mn), 0x1p-126f);
+          l *= alpha;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c)
+          for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) oacc[c][i] *= alpha;
-        m = mn;
+            for (int i = 0; i < 16; ++i) oacc[c][i] *= alpha;
+          m = mn;
+        }
       }
-      const float ref = m == -INFINITY ? 0.f : m;
+      const float ref = base - (m == -INFINITY ? 0.f : m);
       float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          sc[kt][i] = exp2_fast(fmaf(sc[kt][i], unit, -ref));
+          sc[kt][i] = exp2_fast(fmaf(sc[kt][i], unit, ref));
           sum[i & 1] += sc[kt][i];
         }
       l += sum[0] + sum[1];
@@ -287,37 +332,17 @@ void score_fwd_kernel(ScoreFwdParams p) {
           for (int i = 0; i < 8; ++i) pb[0][ss][i] = static_cast<__bf16>(e[i]);
         }
       }
-      if (!clean) {
-        // What is not finite goes straight to the rows that see it.
-        const char* vt = smem + sb + L::kTile;
-#pragma unroll 1
-        for (int j = 0; j < kScoreBlock; ++j) {
-          if (j < a - k0 || j >= b - k0) continue;
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const bf16x4 v4 = *reinterpret_cast<const bf16x4*>(
-                  vt + j * kRow + (((4 * c + g) ^ T::swz(j)) * 16) + 8 * lh);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float v = static_cast<float>(v4[e]);
-                oacc[c][4 * g + e] += v - v == 0.f ? 0.f : v;
-              }
-            }
-        }
-      }
 #pragma unroll
       for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int ss = 0; ss < 4; ++ss) {
-          bf16x8 v = lds_tr((vt0 ^ (64 * c)) + sb, (vt1 ^ (64 * c)) + sb,
-                            ss * 16 * kRow);
-          if (!clean) v = finite_or_zero(v);
+          const bf16x8 v = lds_tr(vt0 ^ (64 * c), vt1 ^ (64 * c),
+                                  L::kTile + ss * 16 * kRow);
 #pragma unroll
           for (int n = 0; n < (EXACT ? 3 : 1); ++n)
             oacc[c] = mfma32(v, pb[n][ss], oacc[c]);
         }
+      if (!EXACT) pipeline_reads<D / 8, 2, 3>();
     };
 
     load(0);
@@ -330,14 +355,25 @@ void score_fwd_kernel(ScoreFwdParams p) {
     for (;;) {
       const int k0 = w.blk * kScoreBlock;
       const int pos0 = w.g.pos + k0 * t.step;
+      const bool all_see =
+          lo_max <= pos0 && pos0 + int64_t{t.step} * (kScoreBlock - 1) < hi_min &&
+          k0 + kScoreBlock <= w.g.len;
       const bool more = w.left > 1;
       const bool changed = more && w.next(t);
       if (more) load(buf ^ 1);
-      if (some_a < k0 + kScoreBlock && k0 < some_b) compute(k0, pos0, buf);
+      if (!all_see) {
+        char* vt = smem + buf * L::kStage + L::kTile;
+        if (tile_not_finite<D>(vt, lane)) take_not_finite(k0, vt);
+      }
+      if (some_a < k0 + kScoreBlock && k0 < some_b) compute(k0, pos0);
       if (!more) break;
       if (changed) enter_segment();
       wait_vmem();
       lds_barrier();  // the next stage has landed; this one has been read
+      const int step = buf ? -L::kStage : L::kStage;
+      kra += step;
+      vt0 += step;
+      vt1 += step;
       buf ^= 1;
     }
   }

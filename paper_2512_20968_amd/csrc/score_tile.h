@@ -81,6 +81,19 @@ __device__ __forceinline__ bf16x8 lds_tr(uint32_t a0, uint32_t a1, int imm) {
                    __builtin_amdgcn_ds_read_tr16_b64_v4i16((T*)(a1 + imm)));
 }
 
+// Order of a block of N MFMAs with R LDS operand reads each: the reads of AHEAD
+// MFMAs in flight ahead of the MFMA that uses them.
+template <int N, int R, int AHEAD>
+__device__ __forceinline__ void pipeline_reads() {
+  __builtin_amdgcn_sched_group_barrier(0x100, R * AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < N - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
 // Whether a staged tile holds an infinity or a NaN (wave-uniform).
 template <int D>
 __device__ __forceinline__ bool tile_not_finite(const char* tile, int lane) {
