@@ -314,10 +314,12 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
       // in stages that some of the workgroup's pairs are hidden in, rows that
       // hold one give NaN to the keys that they see, and zeros to the products.
       uint64_t bad = 0;
-      if (!wg_whole || st.lo_max > wg_first || st.hi_min <= wg_last) {
+      if (__builtin_expect(
+              !wg_whole || st.lo_max > wg_first || st.hi_min <= wg_last, 0)) {
         char* at = smem + buf * L::kStage;
-        if (tile_not_finite<D>(at, lane) ||
-            tile_not_finite<D>(at + L::kTile, lane)) {
+        if (__builtin_expect(tile_not_finite<D>(at, lane) ||
+                                 tile_not_finite<D>(at + L::kTile, lane),
+                             0)) {
           bad = rows_not_finite<D>(at, lane) |
                 rows_not_finite<D>(at + L::kTile, lane);
           lds_barrier();  // every wave has looked
@@ -350,7 +352,7 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
           for (int i = 0; i < 4; ++i) {
             const uint32_t at = fa + 4 * (qt * 32 + (i >> 1) * 16 + (i & 1) * 4);
             f32x4 lse = lds_four<f32x4>(at);
-            if (!full) {
+            if (__builtin_expect(!full, 0)) {
               const i32x4 lo = lds_four<i32x4>(at + 512);
               const i32x4 hi = lds_four<i32x4>(at + 768);
 #pragma unroll
@@ -367,7 +369,7 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
                                              x[i * 4 + e], far, lse[e], &g1);
               g4[e] = g1;
             }
-            if (fix) {
+            if (__builtin_expect(fix, 0)) {
               const uint32_t b4 = static_cast<uint32_t>(
                   bad >> (qt * 32 + (i >> 1) * 16 + 8 * lh + (i & 1) * 4));
 #pragma unroll
@@ -402,7 +404,7 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
             f32x4 y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = x[i * 4 + e];
-            if (fix) {  // a hidden pair's product with a NaN of dO V^T is 0
+            if (__builtin_expect(fix, 0)) {  // a hidden pair's product with a NaN of dO V^T is 0
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 if (g4[e] == 0.f) y[e] = 0.f;
@@ -642,7 +644,7 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
       uint64_t bad = 0;
       if (!all_see) {
         char* at = smem + buf * L::kStage;
-        if (tile_not_finite<D>(at, lane)) {
+        if (__builtin_expect(tile_not_finite<D>(at, lane), 0)) {
           bad = rows_not_finite<D>(at, lane);
           lds_barrier();  // every wave has looked
           clear_not_finite<D>(at, tid);

@@ -342,7 +342,7 @@ void score_fwd_kernel(ScoreFwdParams p) {
           for (int n = 0; n < (EXACT ? 3 : 1); ++n)
             oacc[c] = mfma32(v, pb[n][ss], oacc[c]);
         }
-      if (!EXACT) pipeline_reads<D / 8, 2, 3>();
+      pipeline_reads<D / 8, 2, EXACT ? 2 : 3, EXACT ? 3 : 1>();
     };
 
     load(0);
@@ -363,7 +363,8 @@ void score_fwd_kernel(ScoreFwdParams p) {
       if (more) load(buf ^ 1);
       if (!all_see) {
         char* vt = smem + buf * L::kStage + L::kTile;
-        if (tile_not_finite<D>(vt, lane)) take_not_finite(k0, vt);
+        if (__builtin_expect(tile_not_finite<D>(vt, lane), 0))
+          take_not_finite(k0, vt);
       }
       if (some_a < k0 + kScoreBlock && k0 < some_b) compute(k0, pos0);
       if (!more) break;

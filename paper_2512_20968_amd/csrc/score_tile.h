@@ -81,17 +81,17 @@ __device__ __forceinline__ bf16x8 lds_tr(uint32_t a0, uint32_t a1, int imm) {
                    __builtin_amdgcn_ds_read_tr16_b64_v4i16((T*)(a1 + imm)));
 }
 
-// Order of a block of N MFMAs with R LDS operand reads each: the reads of AHEAD
-// MFMAs in flight ahead of the MFMA that uses them.
-template <int N, int R, int AHEAD>
+// Order of a block of N groups of G MFMAs with R LDS operand reads each: the
+// reads of AHEAD groups in flight ahead of the group that uses them.
+template <int N, int R, int AHEAD, int G = 1>
 __device__ __forceinline__ void pipeline_reads() {
   __builtin_amdgcn_sched_group_barrier(0x100, R * AHEAD, 0);
 #pragma unroll
   for (int i = 0; i < N - AHEAD; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, G, 0);
     __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
   }
-  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+  __builtin_amdgcn_sched_group_barrier(0x008, G * AHEAD, 0);
 }
 
 // Whether a staged tile holds an infinity or a NaN (wave-uniform).
