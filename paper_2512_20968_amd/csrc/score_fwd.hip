@@ -439,11 +439,17 @@ hipError_t launch_d(const ScoreFwdParams& p, hipStream_t stream) {
 
 }  // namespace
 
+// As many parts as fill the places of the 256 compute units (two workgroups each
+// at head dim 128, three at 64).  Microseconds for 1 / this / twice as many:
+// 3002 rows over 6004 striped keys, 12 heads of 64, float32 O 90 / 66 / 70; the
+// same causal, bf16 161 / 82 / 77; 2000 causal rows, 4/2 heads of 64 44 / 22 / 22;
+// 4096 causal rows, 8 heads of 128 101 / 73 / 77; 500 rows over 8000 keys, 8 of
+// 128 183 / 39 / 56; window of 1024 in 4096 rows, 16/8 of 128 57 / 57 / 79.
 int score_fwd_splits(const ScoreTile& t) {
   const int64_t items =
       (int64_t{t.rows_q} + kScoreRows - 1) / kScoreRows * t.hq;
-  if (items >= 256) return 1;
-  const int64_t want = 512 / items, most = t.kv_blocks64 / 4;
+  const int64_t places = t.head_dim == 128 ? 512 : 768;
+  const int64_t want = (places + items - 1) / items, most = t.kv_blocks64 / 4;
   const int64_t n = want < most ? want : most;
   return static_cast<int>(n < 1 ? 1 : n > 64 ? 64 : n);
 }

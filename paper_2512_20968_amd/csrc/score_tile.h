@@ -175,11 +175,18 @@ __device__ __forceinline__ int rows_below(int x, int pos0, int len, int step) {
   return n < static_cast<uint32_t>(len) ? static_cast<int>(n) : len;
 }
 
+// x of all lanes joined by op (idempotent: a lane without a source joins its own),
+// in the vector unit: sums over 2, 4, 8 and 16 lanes of a row, then over the rows.
+// (Twelve of these through LDS permutes were a third of a short call.)
 template <typename Op>
 __device__ __forceinline__ int wave_reduce(int x, Op op) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) x = op(x, __shfl_xor(x, o));
-  return __builtin_amdgcn_readfirstlane(x);
+  x = op(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xa, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
 }
 __device__ __forceinline__ int wave_min(int x) {
   return wave_reduce(x, [](int a, int b) { return a < b ? a : b; });
