@@ -205,11 +205,12 @@ template <int NQ>
 struct RuleState {
   int lo[NQ], qpos[NQ], off[NQ];
   float slope[NQ];  // log2 units
+  int before;       // stored keys that lie before all rows of the wave
 };
 
 // A row under the rule; of its request, the stored keys are [from, local).
 struct RuleRow {
-  int lo, vis, qpos, off;
+  int lo, vis, qpos, off, nearest;  // the key that `off` is the distance to
 };
 
 __device__ __forceinline__ int64_t key_position(const CacheFwdParams& p,
@@ -227,7 +228,7 @@ __device__ __forceinline__ RuleRow rule_row(const CacheFwdParams& p,
       p.key_end ? max(p.key_end[row], 0) : int64_t{max(r.qpos, -1)} + 1;
   r.vis = min(p.c.share.below(end), local);
   r.lo = min(max(p.c.share.below(begin), from), r.vis);
-  r.off = 0;
+  r.off = r.nearest = 0;
   if (p.slopes && r.lo < r.vis) {
     const int at = p.c.share.below(max(r.qpos, 0));  // first not before it
     const int64_t a = key_position(p, min(max(at, r.lo), r.vis - 1));
@@ -235,56 +236,73 @@ __device__ __forceinline__ RuleRow rule_row(const CacheFwdParams& p,
     const int64_t da = a > r.qpos ? a - r.qpos : r.qpos - a;
     const int64_t db = b > r.qpos ? b - r.qpos : r.qpos - b;
     r.off = static_cast<int>(da < db ? da : db);
+    r.nearest = min(max(da < db ? at : at - 1, r.lo), r.vis - 1);
   }
   return r;
 }
 
 // Products of a step -> scores in log2 units: capped (tanh(u) = 1 - 2 / (1 +
 // e^(2u)); small arguments of a float32 O by its series) and biased.
+template <bool EXACT>
+__device__ __forceinline__ float capped(const CacheFwdParams& p, float v,
+                                        float add) {
+  const float r =
+      __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * p.cap_in));
+  const float y = fmaf(-p.cap_two, r, fmaf(0.5f, p.cap_two, add));
+  if (!EXACT) return y;
+  // Taylor; the first term left out is below 2^-25 of the sum.
+  const float u = v * p.cap_u, z = u * u;
+  float t = fmaf(z, -1382.f / 155925, 62.f / 2835);
+  t = fmaf(t, z, -17.f / 315);
+  t = fmaf(t, z, 2.f / 15);
+  t = fmaf(t, z, -1.f / 3);
+  t = fmaf(t * z, u, u);
+  return fabsf(u) < 0.4f ? fmaf(t, 0.5f * p.cap_two, add) : y;
+}
+
 template <int NQ, bool EXACT>
 __device__ __forceinline__ void rule_step(const CacheFwdParams& p,
                                           const RuleState<NQ>& rs,
                                           f32x4 (&x)[NQ][2], int kb, int g) {
-  if (p.cap_two > 0.f) {
+  const int step = p.c.share.striped ? p.c.share.n : 1;
+  const int k0 =
+      p.slopes ? static_cast<int>(key_position(p, kb + 8 * g)) : 0;
+  // In 32 bits: what wraps is not seen.
+  const auto behind = [&](int q) {
+    return static_cast<int>(static_cast<uint32_t>(rs.qpos[q]) -
+                            static_cast<uint32_t>(k0));
+  };
+  // All keys before all rows: one more term per score.
+  const bool before = p.slopes && kb + kStep <= rs.before;
 #pragma unroll
-    for (int q = 0; q < NQ; ++q)
+  for (int q = 0; q < NQ; ++q) {
+    const float add =
+        before ? -rs.slope[q] * static_cast<float>(behind(q) - rs.off[q]) : 0.f;
+    if (p.cap_two > 0.f) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v = x[q][i >> 2][i & 3];
-        float y = fmaf(
-            -p.cap_two,
-            __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * p.cap_in)),
-            0.5f * p.cap_two);
-        if (EXACT) {
-          // Taylor; the first term left out is below 2^-25 of the sum.
-          const float u = v * p.cap_u, z = u * u;
-          float t = fmaf(z, -1382.f / 155925, 62.f / 2835);
-          t = fmaf(t, z, -17.f / 315);
-          t = fmaf(t, z, 2.f / 15);
-          t = fmaf(t, z, -1.f / 3);
-          t = fmaf(t * z, u, u);
-          y = fabsf(u) < 0.4f ? t * (0.5f * p.cap_two) : y;
-        }
-        x[q][i >> 2][i & 3] = y;
-      }
-  } else {
+      for (int i = 0; i < 8; ++i)
+        x[q][i >> 2][i & 3] = capped<EXACT>(p, x[q][i >> 2][i & 3], add);
+    } else {
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      x[q][0] *= p.scale_log2;
-      x[q][1] *= p.scale_log2;
+      for (int i = 0; i < 8; ++i)
+        x[q][i >> 2][i & 3] = fmaf(x[q][i >> 2][i & 3], p.scale_log2, add);
     }
   }
-  if (p.slopes) {
-    const int k0 = static_cast<int>(key_position(p, kb + 8 * g));
-    const int step = p.c.share.striped ? p.c.share.n : 1;
+  if (before) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const float each = rs.slope[q] * static_cast<float>(step);
+#pragma unroll
+      for (int i = 1; i < 8; ++i)
+        x[q][i >> 2][i & 3] =
+            fmaf(each, static_cast<float>(i), x[q][i >> 2][i & 3]);
+    }
+  } else if (p.slopes) {
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        // In 32 bits: what wraps is not seen.
-        const int d = static_cast<int>(static_cast<uint32_t>(rs.qpos[q]) -
-                                       static_cast<uint32_t>(k0) -
-                                       static_cast<uint32_t>(i) * step);
+        const int d = behind(q) - i * step;
         x[q][i >> 2][i & 3] =
             fmaf(-rs.slope[q],
                  static_cast<float>((d < 0 ? -d : d) - rs.off[q]),
@@ -1025,10 +1043,12 @@ void cache_fwd_kernel(CacheFwdParams p) {
     if (!more) break;
 
     int most_seen = 0, all_see = INT32_MAX, all_from = 0;
+    if (RULE) rs.before = INT32_MAX;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       const int r = fresh_tid() & 15;
       const bool valid = it.rr0 + 16 * q + r < it.rr_end;
+      bool sure = true;  // the nearest key is there
       if constexpr (RULE) {
         const uint32_t rr = valid ? it.rr0 + 16 * q + r : it.rr0;
         const TokenHead th = token_head(p, rr, it.kvh);
@@ -1040,7 +1060,13 @@ void cache_fwd_kernel(CacheFwdParams p) {
         rs.off[q] = row.off;
         rs.slope[q] =
             p.slopes ? p.slopes[th.head] * 1.4426950408889634f : 0.f;
-        if (valid) all_from = max(all_from, row.lo);
+        if (p.slopes && row.lo < row.vis)
+          sure = valid_page(h, h.table[row.nearest >> h.lg]);
+        if (valid) {
+          all_from = max(all_from, row.lo);
+          rs.before =
+              min(rs.before, p.c.share.below(int64_t{max(row.qpos, -1)} + 1));
+        }
       } else {
         st.vis[q] = valid ? min(p.c.share.below(int64_t{max(pos[q], -1)} + 1),
                                 it.local)
@@ -1050,6 +1076,15 @@ void cache_fwd_kernel(CacheFwdParams p) {
       if (valid) all_see = min(all_see, st.vis[q]);
       st.limit[q] = -INFINITY;
       st.neg_ref[q] = st.l[q] = 0.f;
+      // Under a moderate cap, with a bias that falls, the largest probability
+      // lies between 2^-kLow and 2^40 around a fixed reference.  (A float32 O's
+      // third parts are 2^16 smaller, and must stay normal numbers.)
+      constexpr float kLow = OUT_F32 ? 100.f : 120.f;
+      if (RULE && p.cap_two > 0.f && p.cap_two <= kLow + 40.f &&
+          !(rs.slope[q] < 0.f) && sure) {
+        st.limit[q] = INFINITY;
+        st.neg_ref[q] = -fminf(0.5f * p.cap_two, kLow - 0.5f * p.cap_two);
+      }
 #pragma unroll
       for (int m = 0; m < D / 16; ++m) st.o[q][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -1057,11 +1092,17 @@ void cache_fwd_kernel(CacheFwdParams p) {
     for (int o = 1; o < 16; o *= 2) {
       most_seen = max(most_seen, __shfl_xor(most_seen, o));
       all_see = min(all_see, __shfl_xor(all_see, o));
-      if (RULE) all_from = max(all_from, __shfl_xor(all_from, o));
+      if (RULE) {
+        all_from = max(all_from, __shfl_xor(all_from, o));
+        rs.before = min(rs.before, __shfl_xor(rs.before, o));
+      }
     }
     most_seen = __builtin_amdgcn_readfirstlane(most_seen);
     all_see = __builtin_amdgcn_readfirstlane(all_see);
-    if (RULE) all_from = __builtin_amdgcn_readfirstlane(all_from);
+    if (RULE) {
+      all_from = __builtin_amdgcn_readfirstlane(all_from);
+      rs.before = __builtin_amdgcn_readfirstlane(rs.before);
+    }
     if (kQInLds<NQ> && !OWN) lds_barrier();
 
     // The next step's K is loaded into the registers of this one's as soon as
@@ -1275,8 +1316,12 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   const int64_t each = (rows + num_requests - 1) / num_requests * group;
   // Three bf16 parts of 64 rows' probabilities do not fit the registers: 1000
   // rows of 4 heads over 33K tokens take 1894 us in tiles of 32 rows, 2175 of 64.
-  // Under a rule neither do a row's range, position and slope.
-  s.nq = each <= 16 ? 1 : each <= 32 || out_f32 || rule ? 2 : 4;
+  // Under a rule neither do a row's range, position and slope at head dim 128 (70
+  // to 110 registers in memory: 2 x 1000 rows of 4 heads over 16500 keys with cap
+  // and bias take 1610 us in tiles of 64 rows, 1180 of 32).
+  s.nq = each <= 16                                         ? 1
+         : each <= 32 || out_f32 || (rule && c.d == 128) ? 2
+                                                            : 4;
   // Most sequences that rows which do not overlap make.
   const int64_t seqs = (rows * group / (16 * s.nq) + num_requests) * c.hkv;
   const int slots = resident_groups(c.d, s.nq);
@@ -1375,7 +1420,7 @@ hipError_t launch(CacheFwdParams p, const Shape& s, hipStream_t stream) {
 template <int D, bool RULE>
 hipError_t launch_d(const CacheFwdParams& p, const Shape& s, bool out_f32,
                     hipStream_t stream) {
-  if constexpr (!RULE) {
+  if constexpr (!RULE || D == 64) {
     if (s.nq == 4) return launch<D, 4, false, RULE>(p, s, stream);
   }
   if (s.nq == 2)

@@ -95,11 +95,14 @@ void score_fwd_kernel(ScoreFwdParams p) {
   constexpr bool kAsR = CAP && !BIAS && !EXACT;
   const float unit = kAsR ? -cap.two : CAP || BIAS ? 1.f : t.scale_log2;
   const float base = kAsR ? cap.one : 0.f;
-  // Scores under a moderate cap need no running maximum: all probabilities lie
-  // between 2^-120 and 2^40 around a fixed reference.
-  const bool fixed = kAsR && cap.two <= 160.f;
-  if (fixed) m = fminf(cap.one, 120.f - cap.one);
   const float slope = BIAS ? t.slopes[h] * kLog2E : 0.f;
+  // Scores under a moderate cap need no running maximum: with a bias that falls
+  // (relative to the nearest key, so that one weighs as without), the largest
+  // probability lies between 2^-kLow and 2^40 around a fixed reference.  (A float32
+  // O's third parts are 2^16 smaller, and must stay normal numbers.)
+  constexpr float kLow = EXACT ? 100.f : 120.f;
+  const bool fixed = CAP && !(slope < 0.f) && cap.two <= kLow + 40.f;
+  if (fixed) m = fminf(cap.one, kLow - cap.one);
   const int pos_min = BIAS ? wave_min(qpos) : 0;
   const int pos_max = BIAS ? wave_max(qpos) : 0;
   // The distance to the row's nearest key: biases are taken relative to it, so

@@ -151,6 +151,10 @@ struct Seen {
   int lo, hi;
 };
 __device__ __forceinline__ int row_position(const ScoreTile& t, int row) {
+  // (The first partition's number comes with the other arguments; a table entry is
+  // another round trip to memory.)
+  if (t.rows_q == t.P)
+    return t.striped ? row * t.n + t.q_idx[0] : t.q_idx[0] * t.P + row;
   const int e = row / t.P, r = row - e * t.P;
   const int part = load_const(t.q_idx, e);
   return t.striped ? r * t.n + part : part * t.P + r;
@@ -200,6 +204,7 @@ struct Segment {
   int row, pos, len;
 };
 __device__ __forceinline__ Segment segment(const ScoreTile& t, int s) {
+  if (t.nseg == 1) return {0, t.seg_pos[0], t.rows_kv};
   Segment g;
   g.row = load_const(t.seg_row, s);
   g.len = load_const(t.seg_row, s + 1) - g.row;

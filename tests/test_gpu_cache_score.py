@@ -208,6 +208,24 @@ def test_bad_pages_and_nan(dtype):
     b.check(b.run(dtype))
 
 
+def test_a_steep_bias_over_a_bad_last_page():
+    """The nearest keys of a request are hidden by their page: the bias of the
+    others is beyond float32's smallest weight."""
+    c = cache_of(num_pages=60)
+    for cap in (0.0, 4.0):
+        rule = {"cap": cap, "slopes": np.float32([60.0, 90.0, 0.5, 20.0])}
+        b = Scored(c, [100, 96 + 16], [1, 30], rule)
+        b.table[0, 6], b.table[1, 6] = -1, 60
+        o, lse = b.run()
+        assert torch.isfinite(lse).all()
+        for r in (0, 30):  # heads 0 and 1 pick the last key with a page
+            k, v = (torch.empty(1, 2, 64, dtype=torch.bfloat16, device="cuda")
+                    for _ in range(2))
+            s = b.table[int(r > 0), 5] * 16 + 15
+            ma.mesh_attn_cache_read(c, i64([s]), b.data, k, v)
+            assert (o[r, :2] - v[0, 0].float()).abs().max() <= 2.0 ** -14 * 6
+
+
 def test_keys_before_the_first_rows_begin_are_not_seen():
     c = cache_of(num_pages=60)
     b = Scored(c, [150], [4], {"key_begin": np.array([70, 10, 90, 0])})
