@@ -636,9 +636,11 @@ size_t mesh_attn_score_bwd_workspace_size(const ma_problem_t* prob, int32_t nq,
  *   dV_j = sum_i P_ij dO_i,  dS_ij = P_ij (<dO_i, v_j> - D_i) (1 - T_ij^2),
  *   dQ_i = s sum_j dS_ij k_j,  dK_j = s sum_i dS_ij q_i.
  *   o, d_o      [nq*P][Hq][d] bf16, dense;  lse [Hq][nq*P] float32.
- *   dq          [nq*P][Hq][d];  dk, dv [nkv*P][Hkv][d], dense, grad_dtype: bf16
- *               (sums in float32, rounded once; P and dS enter the products in
- *               bf16).  MA_FP32 is not served (MA_ERR_UNSUPPORTED).
+ *   dq          [nq*P][Hq][d];  dk, dv [nkv*P][Hkv][d], dense, grad_dtype: the
+ *               float32 sums themselves (partials of several GPUs to be added)
+ *               or rounded once to bf16.  As in mesh_attn_tile_bwd, P and dS enter
+ *               the products in bf16 either way, off by 2^-8 of each at most (dS
+ *               twice that).
  * Rows that see no key have dQ = 0 and give nothing to dK, dV; a NaN or an
  * infinity of a pair that is seen gives NaN to its row's dQ and its key's dK or dV
  * and to no other.  Deterministic (no atomics); may be captured. */

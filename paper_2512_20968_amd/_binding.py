@@ -924,9 +924,9 @@ def mesh_attn_score_fwd(prob, q_idx, kv_idx, score, q, k, v, o, lse, ws=None,
 
 def mesh_attn_score_bwd(prob, q_idx, kv_idx, score, q, k, v, o, d_o, lse, dq,
                         dk, dv, ws=None, stream=None):
-    """dQ, dK, dV (bf16) of a tile under a score rule, from the final O (bf16)
-    and LSE; buffers as in ``mesh_attn_score_fwd``, ``o``, ``d_o`` and the
-    gradients dense."""
+    """dQ, dK, dV (all bf16 or all float32) of a tile under a score rule, from
+    the final O (bf16) and LSE; buffers as in ``mesh_attn_score_fwd``, ``o``,
+    ``d_o`` and the gradients dense."""
     dev, torch = _device_index(stream, q, "q"), _torch_module
     pr = Problem.make(prob)
     qa, qp, nq = _idx(q_idx)
@@ -934,6 +934,7 @@ def mesh_attn_score_bwd(prob, q_idx, kv_idx, score, q, k, v, o, d_o, lse, dq,
     P, hq, hkv, d = (pr.partition_len, pr.num_q_heads, pr.num_kv_heads,
                      pr.head_dim)
     rows, keys, bf = nq * P, nkv * P, torch.bfloat16
+    gt = torch.float32 if dq.dtype is torch.float32 else bf
     s = _score_args(score, rows, hq, dev)
     qq, qs = _heads(q, "q", rows, hq, d, bf, dev)
     kk, ks = _heads(k, "k", keys, hkv, d, bf, dev)
@@ -946,9 +947,10 @@ def mesh_attn_score_bwd(prob, q_idx, kv_idx, score, q, k, v, o, d_o, lse, dq,
         _arg(o, "o", (rows, hq, d), bf, dev),
         _arg(d_o, "d_o", (rows, hq, d), bf, dev),
         _arg(lse, "lse", (hq, rows), torch.float32, dev),
-        _arg(dq, "dq", (rows, hq, d), bf, dev),
-        _arg(dk, "dk", (keys, hkv, d), bf, dev),
-        _arg(dv, "dv", (keys, hkv, d), bf, dev), MA_BF16, wp, wn,
+        _arg(dq, "dq", (rows, hq, d), gt, dev),
+        _arg(dk, "dk", (keys, hkv, d), gt, dev),
+        _arg(dv, "dv", (keys, hkv, d), gt, dev),
+        MA_BF16 if gt is bf else MA_FP32, wp, wn,
         _stream_ptr(stream))
     _check("mesh_attn_score_bwd", st)
     return dq, dk, dv

@@ -276,8 +276,6 @@ ma_status_t mesh_attn_score_bwd(const ma_problem_t* prob, const int32_t* q_idx,
                     k_stride, v, v_stride, &p.t));
   if (grad_dtype != MA_BF16 && grad_dtype != MA_FP32)
     return fail(MA_ERR_INVALID_ARG, "grad_dtype %d invalid", (int)grad_dtype);
-  if (grad_dtype == MA_FP32)
-    return fail(MA_ERR_UNSUPPORTED, "float32 gradients are not served");
   const Arg args[] = {{"o", o, 16},   {"d_o", d_o, 16}, {"lse", lse, 16},
                       {"dq", dq, 16}, {"dk", dk, 16},   {"dv", dv, 16},
                       {"ws", ws, 16}};

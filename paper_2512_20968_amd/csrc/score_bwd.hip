@@ -820,7 +820,9 @@ void score_bwd_splits(const ScoreTile& t, int* kv_splits, int* q_splits) {
 
 hipError_t launch_score_bwd(const ScoreBwdParams& p, bool out_f32,
                             hipStream_t stream) {
-  (void)out_f32;
+  if (out_f32)
+    return p.t.head_dim == 128 ? launch_d<128, true>(p, stream)
+                               : launch_d<64, true>(p, stream);
   return p.t.head_dim == 128 ? launch_d<128, false>(p, stream)
                              : launch_d<64, false>(p, stream);
 }

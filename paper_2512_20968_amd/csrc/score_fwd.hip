@@ -383,7 +383,9 @@ void score_fwd_kernel(ScoreFwdParams p) {
   }
 
   // O = acc / l, LSE = (m + log2 l - slope off) ln 2; 0 and -inf without a key.
-  const float lt = l + __shfl_xor(l, 32);
+  float lt = l + __shfl_xor(l, 32);
+  // A part without the row's nearest key may weigh next to nothing.
+  if (lt < 0x1p-126f) lt = 0.f;
   const float inv = lt > 0.f ? 1.f / lt : lt;
   float lse = lt == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(lt);
   if (m == -INFINITY && lt != 0.f) lse = lt;  // NaN

@@ -189,7 +189,8 @@ class Bounds:
             tol[2][:, hk] += (p * (U + e + 2.0 ** -20)).T @ np.abs(do[:, h])
         for name, got, x, t in zip(("dq", "dk", "dv"), (dq, dk, dv), want,
                                    tol):
-            off = np.abs(np64(got) - x) - 1.1 * (t + U * np.abs(x))
+            last = U if got.dtype is torch.bfloat16 else 16 * E
+            off = np.abs(np64(got) - x) - 1.1 * (t + last * np.abs(x))
             assert off.max(initial=-1) <= 1e-30, (name, off.max())
 
 
@@ -203,8 +204,9 @@ def run_forward(prob, q_idx, kv_idx, rule, q, k, v, dtype=torch.bfloat16,
                                   **kw)
 
 
-def run_backward(prob, q_idx, kv_idx, rule, q, k, v, o, do, lse, **kw):
-    out = [torch.full(x.shape, 3.0, dtype=torch.bfloat16, device="cuda")
+def run_backward(prob, q_idx, kv_idx, rule, q, k, v, o, do, lse,
+                 grads=torch.bfloat16, **kw):
+    out = [torch.full(x.shape, 3.0, dtype=grads, device="cuda")
            for x in (q, k, v)]
     return ma.mesh_attn_score_bwd(prob, q_idx, kv_idx, rule, q, k, v, o, do,
                                   lse, *out, **kw)

@@ -22,8 +22,14 @@ def check(prob, q_idx, kv_idx, rule, ins, dtype=torch.bfloat16, backward=True):
     want.check_forward(o, lse, dtype is torch.float32)
     if backward:
         ob = o.to(torch.bfloat16)
-        grads = run_backward(prob, q_idx, kv_idx, dev, q, k, v, ob, do, lse)
+        # float32 gradients beside a float32 O, bf16 ones beside a bf16 O.
+        grads = run_backward(prob, q_idx, kv_idx, dev, q, k, v, ob, do, lse,
+                             grads=dtype)
         want.check_backward(ob, lse, do, *grads)
+        if dtype is torch.float32:  # bf16 ones are their roundings
+            for a, b in zip(grads, run_backward(prob, q_idx, kv_idx, dev, q, k,
+                                                v, ob, do, lse)):
+                assert torch.equal(a.to(torch.bfloat16), b)
 
 
 # -- sizes, rules, layouts ----------------------------------------------------
