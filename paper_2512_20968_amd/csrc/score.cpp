@@ -174,7 +174,7 @@ size_t fwd_bytes(const ScoreTile& t, int splits) {
 }
 
 struct BwdBytes {
-  size_t rows, ints, stages, kv, q, all;
+  size_t rows, ints, stages, counts, kv, q, all;
 };
 
 BwdBytes bwd_bytes(const ScoreTile& t, int kv_splits, int q_splits) {
@@ -183,13 +183,17 @@ BwdBytes bwd_bytes(const ScoreTile& t, int kv_splits, int q_splits) {
   b.rows = up256(4 * pad * t.hq);
   b.ints = up256(4 * pad);
   b.stages = up256(sizeof(ScoreStage) * (pad / 64));
+  b.counts = kv_splits == 1
+                 ? 0
+                 : up256(4 * static_cast<size_t>(t.rows_kv) * t.hkv);
   b.kv = kv_splits == 1 ? 0
                         : up256(4 * static_cast<size_t>(t.rows_kv) * t.hkv *
                                 t.head_dim * kv_splits);
   b.q = q_splits == 1 ? 0
                       : up256(4 * static_cast<size_t>(t.rows_q) * t.hq *
                               t.head_dim * q_splits);
-  b.all = 2 * b.rows + 4 * b.ints + b.stages + 2 * b.kv + b.q;
+  b.all = 2 * b.rows + 4 * b.ints + b.stages + b.counts +
+          2 * b.kv + b.q;
   return b;
 }
 
@@ -313,6 +317,7 @@ ma_status_t mesh_attn_score_bwd(const ma_problem_t* prob, const int32_t* q_idx,
   p.pos = reinterpret_cast<int32_t*>(take(b.ints));
   p.pos_rel = reinterpret_cast<float*>(take(b.ints));
   p.stages = reinterpret_cast<ScoreStage*>(take(b.stages));
+  p.kv_parts = reinterpret_cast<int32_t*>(take(b.counts));
   p.part_dk = reinterpret_cast<float*>(take(b.kv));
   p.part_dv = reinterpret_cast<float*>(take(b.kv));
   p.part_dq = reinterpret_cast<float*>(take(b.q));

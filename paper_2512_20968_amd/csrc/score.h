@@ -72,12 +72,16 @@ struct ScoreBwdParams {
   int32_t* pos;
   float* pos_rel;      // position less that of the stage's first row
   ScoreStage* stages;  // [rows_pad / 64]
-  // Partial dK, dV of stages cut into kv_splits parts: [split][rows_kv][hkv][d].
+  // Partial dK, dV of 128 keys whose stages are cut into parts of about
+  // part_stages, at most kv_splits of them: [part][rows_kv][hkv][d]; how many there
+  // are: [rows_kv][hkv].
+  int32_t* kv_parts;
   float* part_dk;
   float* part_dv;
   // Partial dQ of keys cut into q_splits parts: [split][rows_q][hq][d].
   float* part_dq;
   int32_t rows_pad, kv_splits, q_splits;
+  int32_t part_stages;
   int32_t kv_items;  // workgroups of dK/dV, those of dQ come behind
 };
 static_assert(sizeof(ScoreBwdParams) <= 4096, "kernel arguments");

@@ -26,6 +26,10 @@ using namespace dev;
 
 constexpr int NT = 256;
 
+// Stages of a part of a dK/dV item, so that the keys of a long document do not take
+// much longer than the rest.
+constexpr int kPartStages = 8;
+
 // ---------------------------------------------------------------------------
 // 1. prep
 // ---------------------------------------------------------------------------
@@ -145,7 +149,8 @@ struct KvLayout {
   // Q, dO, then LSE, D, begin, end and position of 64 rows.
   static constexpr int kFloats = 2 * kTile;
   static constexpr int kStage = 2 * kTile + 5 * kScoreBlock * 4;
-  static constexpr int kLds = 2 * kStage;
+  static constexpr int kFlags = 2 * kStage;  // of the waves
+  static constexpr int kLds = kFlags + 16;
 };
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
@@ -178,14 +183,18 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
   using L = KvLayout<D>;
   using T = Staged<D>;
   constexpr int kRow = T::kRowBytes;
+  int* s_flags = reinterpret_cast<int*>(smem + KvLayout<D>::kFlags);
   const ScoreTile& t = p.t;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   const int hk = id % t.hkv;
   id /= t.hkv;
-  const int part = id % p.kv_splits;
-  int blk = id / p.kv_splits;
+  // First parts first.  (With the parts of a block side by side, four of which one
+  // has work, the items that have some all went to the same quarter of the compute
+  // units: 842 us instead of 570.)
+  const int part = id / t.kv_blocks128;
+  int blk = id - part * t.kv_blocks128;
   Segment g;
   for (int s = 0; s < t.nseg; ++s) {
     g = segment(t, s);
@@ -228,41 +237,55 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
   }
   const Cap cap = cap_of(t);
 
-  // The stages of this part that see some of the keys, 64 of them looked at at a
-  // time, for each head of the group.
+  // The stages that see some of the keys, 64 of them looked at at a time, for each
+  // head of the group.
   const int stages = p.rows_pad / kScoreBlock;
-  const int64_t all = int64_t{stages} * t.group;
-  const int first = static_cast<int>(all * part / p.kv_splits);
-  const int stop = static_cast<int>(all * (part + 1) / p.kv_splits);
-  int base = first / stages * stages + first % stages / 64 * 64;
-  uint64_t bits = 0;
-  auto look = [&]() {  // bits of the stages base ..
-    const int s = base % stages + lane, at = base + lane;
+  auto look = [&](int s0) {  // bits of the stages s0 ..
+    const int s = s0 + lane;
     bool yes = false;
-    if (s < stages && at >= first && at < stop) {
+    if (s < stages) {
       const ScoreStage st = p.stages[s];
       yes = st.lo_min <= wg_last && st.hi_max > wg_first &&
             st.lo_min < st.hi_max;
     }
     return __builtin_amdgcn_ballot_w64(yes);
   };
+  // This part's share of them.
+  int skip = 0, take = INT32_MAX, parts = 1;
+  if (p.kv_splits > 1) {
+    int n = 0;
+    for (int s0 = 0; s0 < stages; s0 += 64) n += __builtin_popcountll(look(s0));
+    n *= t.group;
+    parts = min(max((n + p.part_stages - 1) / p.part_stages, 1), p.kv_splits);
+    if (part >= parts) return;
+    skip = static_cast<int>(int64_t{n} * part / parts);
+    take = static_cast<int>(int64_t{n} * (part + 1) / parts) - skip;
+    if (part == 0 && tid < kScoreRows && key0 + tid < g.len)
+      p.kv_parts[(int64_t{g.row} + key0 + tid) * t.hkv + hk] = parts;
+  }
+  int gh_next = 0, s_next = -64;  // where `bits` are from
+  uint64_t bits = 0;
   // The next stage as group head * stages + stage; -1: there is none.
   auto next_stage = [&]() {
+    if (take == 0) return -1;
     while (bits == 0) {
-      if (base >= stop) return -1;
-      bits = look();
-      if (bits != 0) break;
-      const int s = base % stages;
-      base = s + 64 >= stages ? base - s + stages : base + 64;
+      s_next += 64;
+      if (s_next >= stages) {
+        s_next = 0;
+        if (++gh_next >= t.group) return -1;
+      }
+      bits = look(s_next);
+      const int n = __builtin_popcountll(bits);
+      if (n <= skip) {
+        skip -= n;
+        bits = 0;
+      }
     }
+    for (; skip > 0; --skip) bits &= bits - 1;
     const int i = __builtin_ctzll(bits);
     bits &= bits - 1;
-    const int at = base + i;
-    if (bits == 0) {
-      const int s = base % stages;
-      base = s + 64 >= stages ? base - s + stages : base + 64;
-    }
-    return at;
+    --take;
+    return gh_next * stages + s_next + i;
   };
   auto load = [&](int at, int buf) {
     // Not known to be the same from call to call: the loads' offsets are made
@@ -317,9 +340,7 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
       if (__builtin_expect(
               !wg_whole || st.lo_max > wg_first || st.hi_min <= wg_last, 0)) {
         char* at = smem + buf * L::kStage;
-        if (__builtin_expect(tile_not_finite<D>(at, lane) ||
-                                 tile_not_finite<D>(at + L::kTile, lane),
-                             0)) {
+        if (__builtin_expect(tiles_not_finite<D, 2>(at, tid, s_flags), 0)) {
           bad = rows_not_finite<D>(at, lane) |
                 rows_not_finite<D>(at + L::kTile, lane);
           lds_barrier();  // every wave has looked
@@ -452,7 +473,7 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
   int lane = tid & 63;
   asm volatile("" : "+v"(lane));
   const int li = lane & 31, lh = lane >> 5;
-  const bool whole = p.kv_splits == 1;
+  const bool whole = parts == 1;
   const int64_t all_out = int64_t{t.rows_kv} * t.hkv * D;
   const float out_scale = grad_scale<CAP>(t);
 #pragma unroll
@@ -494,6 +515,7 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
   using L = QLayout<D>;
   using T = Staged<D>;
   constexpr int kRow = T::kRowBytes;
+  int* s_flags = reinterpret_cast<int*>(smem + KvLayout<D>::kFlags);
   const ScoreTile& t = p.t;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -644,7 +666,7 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
       uint64_t bad = 0;
       if (!all_see) {
         char* at = smem + buf * L::kStage;
-        if (__builtin_expect(tile_not_finite<D>(at, lane), 0)) {
+        if (__builtin_expect(tiles_not_finite<D, 1>(at, tid, s_flags), 0)) {
           bad = rows_not_finite<D>(at, lane);
           lds_barrier();  // every wave has looked
           clear_not_finite<D>(at, tid);
@@ -710,6 +732,10 @@ struct SumParams {
   void* dst[2];
   int64_t n;  // elements of one, a multiple of 4
   int32_t parts;
+  // Parts of every `d` elements, or null: `parts` of all.  One part: the result is
+  // there.
+  const int32_t* counts;
+  int32_t d;
 };
 
 template <bool OUT_F32>
@@ -719,9 +745,12 @@ __global__ __launch_bounds__(NT) void score_sum_kernel(SumParams p) {
   const int64_t stride = int64_t{gridDim.x} * NT * 4;
   for (int64_t i = (int64_t{blockIdx.x} * NT + threadIdx.x) * 4; i < p.n;
        i += stride) {
+    const int parts =
+        p.counts ? p.counts[static_cast<uint64_t>(i) / uint32_t(p.d)] : p.parts;
+    if (parts == 1) continue;
     f32x4 s = *reinterpret_cast<const f32x4*>(src + i);
 #pragma unroll 4
-    for (int k = 1; k < p.parts; ++k) {
+    for (int k = 1; k < parts; ++k) {
       const f32x4 x = *reinterpret_cast<const f32x4*>(src + k * p.n + i);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[e] += x[e];
@@ -766,6 +795,7 @@ hipError_t launch(const ScoreBwdParams& p, hipStream_t stream) {
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   ScoreBwdParams q = p;
+  q.part_stages = kPartStages;
   q.kv_items = t.kv_blocks128 * t.hkv * p.kv_splits;
   const int64_t q_items =
       (int64_t{t.rows_q} + kScoreRows - 1) / kScoreRows * t.hq * p.q_splits;
@@ -776,14 +806,18 @@ hipError_t launch(const ScoreBwdParams& p, hipStream_t stream) {
     SumParams s{{p.part_dk, p.part_dv},
                 {p.dk, p.dv},
                 int64_t{t.rows_kv} * t.hkv * D,
-                p.kv_splits};
+                p.kv_splits,
+                p.kv_parts,
+                D};
     e = launch_sum(s, 2, OUT_F32, stream);
   }
   if (e == hipSuccess && p.q_splits > 1) {
     SumParams s{{p.part_dq, nullptr},
                 {p.dq, nullptr},
                 int64_t{t.rows_q} * t.hq * D,
-                p.q_splits};
+                p.q_splits,
+                nullptr,
+                D};
     e = launch_sum(s, 1, OUT_F32, stream);
   }
   return e;
@@ -800,11 +834,14 @@ hipError_t launch_d(const ScoreBwdParams& p, hipStream_t stream) {
 
 }  // namespace
 
-// Parts so that dK/dV has 512 items, two for each of 256 compute units, and dQ 128
-// beside them.  Microseconds of (head dim 64, 3001 rows, 12/4 heads; documents in
-// 4096 rows of 32/8 heads of 128; 8192 causal rows of those) for dK/dV 256 / 512 /
-// 1024: 68, 213, 2214 / 60, 175, 2163 / 69, 194, 2163; dQ 512 instead of 128: 65,
-// 173, 2173.
+// Most parts so that dK/dV has 512 items, two for each of 256 compute units, and
+// dQ 128 beside them; of dK/dV's, a block of keys has as many as it has stages for.
+// Microseconds for dK/dV whole / cut so / for 1024 items:
+//   documents in 4096 rows of 32/8 heads of 128     204/178/188
+//   4096 and 8192 causal rows of those      853/606/582, 2101/2103/2096
+//   prefixes in 3001 rows of 12/4 heads of 64        164/ 55/ 55
+//   1000 causal rows of 8 heads of 128                70/ 56/ 55
+// and for parts of 16 stages 170, 607, 2097, 75, 74.
 void score_bwd_splits(const ScoreTile& t, int* kv_splits, int* q_splits) {
   auto parts = [](int64_t items, int64_t blocks, int64_t target) {
     const int64_t want = (target + items - 1) / items, most = blocks / 4;

@@ -34,7 +34,7 @@ template <int D>
 struct Layout {
   static constexpr int kTile = Staged<D>::kBytes;
   static constexpr int kStage = 2 * kTile;  // K, V
-  static constexpr int kLds = 2 * kStage + 16 * 4;  // .. the waves' key ranges
+  static constexpr int kLds = 2 * kStage + 20 * 4;  // .. the waves' ranges, flags
 };
 
 // EXACT (float32 O): the probabilities enter the second product as a sum of three
@@ -366,7 +366,10 @@ void score_fwd_kernel(ScoreFwdParams p) {
       if (more) load(buf ^ 1);
       if (!all_see) {
         char* vt = smem + buf * L::kStage + L::kTile;
-        if (__builtin_expect(tile_not_finite<D>(vt, lane), 0))
+        if (__builtin_expect(
+                tiles_not_finite<D, 1>(vt, tid,
+                                       reinterpret_cast<int*>(s_range + 4)),
+                0))
           take_not_finite(k0, vt);
       }
       if (some_a < k0 + kScoreBlock && k0 < some_b) compute(k0, pos0);

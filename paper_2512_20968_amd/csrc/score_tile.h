@@ -94,22 +94,30 @@ __device__ __forceinline__ void pipeline_reads() {
   __builtin_amdgcn_sched_group_barrier(0x008, G * AHEAD, 0);
 }
 
-// Whether a staged tile holds an infinity or a NaN (wave-uniform).
-template <int D>
-__device__ __forceinline__ bool tile_not_finite(const char* tile, int lane) {
+// Whether some of `tiles` staged tiles one after the other hold an infinity or a
+// NaN: every wave looks at a quarter, the answers meet in s_flags.  For all waves
+// of the workgroup together; between two calls lies another barrier.
+template <int D, int tiles>
+__device__ __forceinline__ bool tiles_not_finite(const char* tile, int tid,
+                                                 int* s_flags) {
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+  typedef int i32x4v __attribute__((ext_vector_type(4)));
   u16x2 top = {0, 0};
-#pragma unroll 4
-  for (int i = 0; i < Staged<D>::kBytes / 1024; ++i) {
-    const u32x4v w =
-        *reinterpret_cast<const u32x4v*>(tile + i * 1024 + lane * 16);
+#pragma unroll
+  for (int i = 0; i < tiles * Staged<D>::kBytes / (16 * kThreads); ++i) {
+    const u32x4v w = *reinterpret_cast<const u32x4v*>(
+        tile + (i * kThreads + tid) * 16);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       top = __builtin_elementwise_max(
           top, __builtin_bit_cast(u16x2, w[j] & 0x7f807f80u));
   }
-  return __any(top[0] == 0x7f80 || top[1] == 0x7f80);
+  const bool any = __any(top[0] == 0x7f80 || top[1] == 0x7f80);
+  if ((tid & 63) == 0) s_flags[tid >> 6] = any;
+  lds_barrier();
+  const i32x4v f = *reinterpret_cast<const i32x4v*>(s_flags);
+  return __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]) != 0;
 }
 
 // The operand with zeros for what is not finite.
