@@ -745,9 +745,12 @@ __global__ __launch_bounds__(NT) void score_sum_kernel(SumParams p) {
   const int64_t stride = int64_t{gridDim.x} * NT * 4;
   for (int64_t i = (int64_t{blockIdx.x} * NT + threadIdx.x) * 4; i < p.n;
        i += stride) {
+    // (At most `parts`, whatever is read.)
     const int parts =
-        p.counts ? p.counts[static_cast<uint64_t>(i) / uint32_t(p.d)] : p.parts;
-    if (parts == 1) continue;
+        p.counts ? min(p.counts[static_cast<uint64_t>(i) / uint32_t(p.d)],
+                       p.parts)
+                 : p.parts;
+    if (parts <= 1) continue;
     f32x4 s = *reinterpret_cast<const f32x4*>(src + i);
 #pragma unroll 4
     for (int k = 1; k < parts; ++k) {
