@@ -38,7 +38,10 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # The present kernels' assembly has no join that runs vector instructions before
 # its restore, with this flag or without; what the register allocator puts there
 # changes with any edit, so the flag stays.
+# (The backward under a score rule, which has a few spilled registers too, is built
+# the same way.)
 EXTRA = {"cache_fwd.hip": ["-mllvm", "-amdgpu-remove-redundant-endcf=0"],
+         "score_bwd.hip": ["-mllvm", "-amdgpu-remove-redundant-endcf=0"],
          "tile_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "tile_fwd.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers"]}
 

@@ -15,6 +15,18 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// c and the sum of eight bf16, exact products: what a second product's operand adds
+// up to.
+__device__ __forceinline__ float add_eight(const bf16x8& x, float c) {
+  const bf16x2 one = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bf16x2 y = {x[2 * i], x[2 * i + 1]};
+    c = __builtin_amdgcn_fdot2_f32_bf16(y, one, c, false);
+  }
+  return c;
+}
+
 constexpr uint32_t kScaleNaN = 255;  // scale code of a group of NaN
 
 // The scale 2^(code - 127) as a float: the code is its exponent field.

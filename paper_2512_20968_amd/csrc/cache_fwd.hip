@@ -20,6 +20,15 @@
 // in all.  The same with float32 O, in tiles of 32 rows: 1892 us; 64 matrix and 282
 // vector instructions a step, for half the rows.
 //
+// Under a score rule (mesh_attn_cache_score_fwd) a step's scores are capped, biased
+// and put in log2 units between the products, rows see a range of keys, and a
+// request's units begin at the first key that its rows see.  64 requests seen
+// through windows of 4096 tokens, 8 KV heads of 4 query heads, head dim 128: 37 us,
+// 3.1 TB/s, by the round trips of 512 sequences of 4 steps; 2 x 1000 rows over 16500
+// keys with cap and bias 970 us, 0.54 PFLOP/s, by the vector unit: tiles of 32 rows
+// (a row's range, position and slope do not fit beside 64), twice the conversions,
+// and a reciprocal and two exponentials per score.
+//
 // MFMA conventions (16x16x32): lane l holds, for A, row l % 16 and the k-values
 // of quarter l / 16; for B, column l % 16 and the same quarter; accumulator
 // register i holds row 4 (l / 16) + i of column l % 16.  The order of the
@@ -205,6 +214,9 @@ template <int NQ>
 struct RuleState {
   int lo[NQ], qpos[NQ], off[NQ];
   float slope[NQ];  // log2 units
+  // This lane's share of the sum of what the probabilities are rounded to (bf16
+  // O): O is divided by it, so that the rounding of a row's largest ones falls out.
+  float rounded[NQ];
   int before;       // stored keys that lie before all rows of the wave
 };
 
@@ -353,8 +365,9 @@ __device__ __forceinline__ void split_probs(const float (&p)[8],
 
 // The rest of a step once its scores x are there: keys 8 g + 4 t + i of column
 // r.
-template <int D, int NQ, bool EXACT>
+template <int D, int NQ, bool EXACT, bool RULE>
 __device__ __forceinline__ void finish_step(State<D, NQ>& st,
+                                            RuleState<NQ>& rs,
                                             f32x4 (&x)[NQ][2],
                                             const StepData<D>& s,
                                             float scale_log2,
@@ -386,6 +399,7 @@ __device__ __forceinline__ void finish_step(State<D, NQ>& st,
                           : fmaxf((m + kLag) * inv_scale_log2, -3e38f);
       st.neg_ref[q] = still ? 0.f : -m;
       st.l[q] *= f;
+      if constexpr (RULE && !EXACT) rs.rounded[q] *= f;
 #pragma unroll
       for (int m16 = 0; m16 < D / 16; ++m16) st.o[q][m16] *= f;
     }
@@ -399,6 +413,8 @@ __device__ __forceinline__ void finish_step(State<D, NQ>& st,
           fmaf(x[q][i >> 2][i & 3], scale_log2, st.neg_ref[q]));
     st.l[q] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     split_probs<EXACT>(p, &ph[q]);
+    if constexpr (RULE && !EXACT)
+      rs.rounded[q] = add_eight(ph[q].part[0], rs.rounded[q]);
   }
   float scale[8];
 #pragma unroll
@@ -587,6 +603,18 @@ __device__ __forceinline__ int32_t stored_keys(const CacheFwdParams& p,
 // starts in run w and goes on after it; cache_fold_kernel joins them.  Not split:
 // every sequence is one unit, and no piece is split.
 constexpr int kWaveKeys = kWaves * kStep;  // keys of a step of each wave
+
+// The factor that makes O's sums those of the unrounded probabilities' sum l.
+template <int NQ, bool EXACT, bool RULE>
+__device__ __forceinline__ float unrounded(const RuleState<NQ>& rs, int q,
+                                           float l) {
+  if constexpr (RULE && !EXACT) {
+    const float r = across_quarters(
+        rs.rounded[q], [](float a, float b) { return a + b; });
+    return r > 0.f ? l / r : 1.f;
+  }
+  return 1.f;
+}
 
 // What the prefix sums leave in LDS per request: its first unit, and, for up to
 // kKeptRequests requests, what an item needs (another round trip to memory
@@ -993,6 +1021,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
         if (prev.rr0 + 16 * q >= prev.rr_end) break;
         const float l = across_quarters(
             st.l[q], [](float a, float b) { return a + b; });
+        const float factor = unrounded<NQ, OUT_F32, RULE>(rs, q, l);
         lds_barrier();
         if (g == 0) {
           s_m[wave][r] =
@@ -1003,7 +1032,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int m = 0; m < D / 16; ++m)
-            s_o[wave][r][g * (D / 4) + i * (D / 16) + m] = st.o[q][m][i];
+            s_o[wave][r][g * (D / 4) + i * (D / 16) + m] =
+                RULE && !OUT_F32 ? st.o[q][m][i] * factor : st.o[q][m][i];
         lds_barrier();
         const int row16 = tid / (D / 8), dim0 = tid % (D / 8) * 8;
         const int rr = prev.rr0 + 16 * q + row16;
@@ -1076,6 +1106,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
       if (valid) all_see = min(all_see, st.vis[q]);
       st.limit[q] = -INFINITY;
       st.neg_ref[q] = st.l[q] = 0.f;
+      if (RULE) rs.rounded[q] = 0.f;
       // Under a moderate cap, with a bias that falls, the largest probability
       // lies between 2^-kLow and 2^40 around a fixed reference.  (A float32 O's
       // third parts are 2^16 smaller, and must stay normal numbers.)
@@ -1128,8 +1159,9 @@ void cache_fwd_kernel(CacheFwdParams p) {
         if constexpr (RULE) rule_step<NQ, OUT_F32>(p, rs, x, kb, g);
         if (kb + kStep > all_see || (RULE && kb < all_from) || !__all(ok))
           vs = mask_step<D, NQ, RULE>(st, rs, x, s, ok, kb, h.local, g);
-        finish_step<D, NQ, OUT_F32>(st, x, s, RULE ? 1.f : p.scale_log2,
-                                    RULE ? 1.f : p.inv_scale_log2, vs);
+        finish_step<D, NQ, OUT_F32, RULE>(st, rs, x, s,
+                                          RULE ? 1.f : p.scale_log2,
+                                          RULE ? 1.f : p.inv_scale_log2, vs);
         if (!more_keys) break;
         load_v<D, P16>(h, pn, next, g, &s);
         pg = pn;
@@ -1145,6 +1177,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
         if (it.rr0 + 16 * q >= it.rr_end) continue;
         const float l = across_quarters(
             st.l[q], [](float a, float b) { return a + b; });
+        const float factor = unrounded<NQ, OUT_F32, RULE>(rs, q, l);
         const int rr = it.rr0 + 16 * q + r;
         const TokenHead th = token_head(p, rr, it.kvh);
         if (rr < it.rr_end) {
@@ -1153,7 +1186,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
             float acc[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              acc[i] = st.o[q][(8 * j + i) % (D / 16)][(8 * j + i) / (D / 16)];
+              acc[i] = st.o[q][(8 * j + i) % (D / 16)][(8 * j + i) / (D / 16)] *
+                       (RULE && !OUT_F32 ? factor : 1.f);
             store_row<D, OUT_F32, RULE>(
                 p, it.first + th.tok, th.head, it.from, it.local,
                 g * (D / 4) + 8 * j, acc, st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
@@ -1387,7 +1421,8 @@ hipError_t launch_fwd(const CacheFwdParams& p, int groups, hipStream_t stream) {
       (n + 1) * 4 + (n <= kKeptRequests ? n * sizeof(Request<RULE>) : 0);
   const auto kernel = p.c.page_log2 == 4
                           ? cache_fwd_kernel<D, NQ, OUT_F32, true, OWN, RULE>
-                          : cache_fwd_kernel<D, NQ, OUT_F32, false, OWN, RULE>;
+                          : cache_fwd_kernel<D, NQ, OUT_F32, false, OWN,
+                                             RULE>;
   hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(groups)), dim3(NT), lds,
                      stream, p);
   return hipGetLastError();

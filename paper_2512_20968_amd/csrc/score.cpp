@@ -31,14 +31,19 @@ ma_status_t check_score_problem(const ma_problem_t* prob, int32_t nq,
     return fail(nq < 1 || nkv < 1 ? MA_ERR_INVALID_ARG : MA_ERR_UNSUPPORTED,
                 "lists of %d and %d partitions: need 1 to %d", nq, nkv,
                 kScoreMaxList);
-  const int64_t most = int64_t{1} << 28;
-  const int64_t q = int64_t{nq} * prob->partition_len;
-  const int64_t kv = int64_t{nkv} * prob->partition_len;
+  if (prob->num_q_heads > 65535)
+    return fail(MA_ERR_UNSUPPORTED, "num_q_heads %d above 65535",
+                prob->num_q_heads);
+  // The backward's first launch has d / 8 lanes for every head of every row, in
+  // stages of 64, counted in 32 bits.
+  const int64_t most = int64_t{1} << 27;
+  const int64_t q = int64_t{nq} * prob->partition_len + 63;
+  const int64_t kv = int64_t{nkv} * prob->partition_len + 63;
   if (nq > prob->num_partitions || nkv > prob->num_partitions)
     return fail(MA_ERR_INVALID_ARG, "lists of %d and %d partitions of %d", nq,
                 nkv, prob->num_partitions);
   if (q > most / prob->num_q_heads || kv > most / prob->num_kv_heads)
-    return fail(MA_ERR_UNSUPPORTED, "rows times heads above 2^28");
+    return fail(MA_ERR_UNSUPPORTED, "rows times heads above 2^27");
   return MA_OK;
 }
 

@@ -5,13 +5,23 @@
 // (4 r (1 - r) with the r of cap_r()):  dV = P^T dO,  dS = P T' (dO V^T - D),
 // D = <dO, O>,  dK = s dS^T Q,  dQ = s dS K.
 //
-// Three launches, and one more for each pass whose items are cut:
+// Two launches, and one more for each pass whose items are cut:
 //  1. prep: D and LSE log2(e) of every (row, head); every row's range and
 //     position; what each stage of 64 rows sees.
 //  2. dK/dV: a workgroup per (128 keys, KV head), four waves of 32 keys; it walks
 //     the stages of 64 query rows that see some of its keys for every query head
-//     of the group.  K, V, dK and dV stay in registers.
-//  3. dQ: a workgroup per (128 rows, head), four waves of 32 rows, as the forward.
+//     of the group.  K, V, dK and dV stay in registers, which leaves room for the
+//     exponentials of four queries at a time.
+//  3. dQ, in the same launch: a workgroup per (128 rows, head), four waves of 32
+//     rows, as the forward.
+// The scores are made in both passes: seven products for the five that the
+// gradients need.
+//
+// Bound by the matrix and the vector unit together (8192 causal rows of 32/8 heads
+// of 128, matrix unit busy 41 % of the time, vector unit 52 %): with a cap 2070 us,
+// 0.66 PFLOP/s of the five products, 0.93 of the seven, where a large product
+// reaches 1.22; without 1880 us.  Documents in 4096 rows 160 us, of which prep is
+// 14 (a read of O and dO at the card's rate) and the sum of parts 13.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -156,13 +166,7 @@ struct KvLayout {
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// Eight values from LDS byte address a.
-template <typename V8, typename V4>
-__device__ __forceinline__ V8 lds_eight(uint32_t a) {
-  typedef __attribute__((address_space(3))) const V4 T;
-  const V4 lo = *(T*)a, hi = *(T*)(a + 16);
-  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-}
+// Four values from LDS byte address a.
 template <typename V4>
 __device__ __forceinline__ V4 lds_four(uint32_t a) {
   typedef __attribute__((address_space(3))) const V4 T;
@@ -469,18 +473,17 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
   }
 
   // Register i of chunk c: key 8 (i / 4) + 4 lh + i % 4 of the wave, dim 32 c + li.
-  {
-  int lane = tid & 63;
-  asm volatile("" : "+v"(lane));
-  const int li = lane & 31, lh = lane >> 5;
+  int last = tid & 63;  // made again, as in load()
+  asm volatile("" : "+v"(last));
+  const int li2 = last & 31, lh2 = last >> 5;
   const bool whole = parts == 1;
   const int64_t all_out = int64_t{t.rows_kv} * t.hkv * D;
   const float out_scale = grad_scale<CAP>(t);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int k = key0 + wave * 32 + 8 * (i >> 2) + 4 * lh + (i & 3);
+    const int k = key0 + wave * 32 + 8 * (i >> 2) + 4 * lh2 + (i & 3);
     if (k >= g.len) continue;
-    const int64_t at = ((int64_t{g.row} + k) * t.hkv + hk) * D + li;
+    const int64_t at = ((int64_t{g.row} + k) * t.hkv + hk) * D + li2;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       const float dv = acc_v[c][i], dk = acc_k[c][i] * out_scale;
@@ -495,7 +498,6 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
         static_cast<__bf16*>(p.dk)[at + 32 * c] = static_cast<__bf16>(dk);
       }
     }
-  }
   }
 }
 

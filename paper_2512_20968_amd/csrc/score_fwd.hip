@@ -27,7 +27,10 @@ constexpr int NT = 256;
 
 // The reference of a row's probabilities may lag behind its maximum by this much
 // (log2 units): they stay below 2^8, and the sums are rescaled a few times per
-// row instead of whenever its maximum grows.
+// row instead of whenever its maximum grows.  The first block's maximum is taken as
+// it is: what is rounded of a row's only key, or of one that outweighs the rest,
+// is 1.  (A fixed reference, which a moderate cap allows, saves 3 % and adds a
+// rounding of 2^-8 to such rows.)
 constexpr float kLag = 8.f;
 
 template <int D>
@@ -96,13 +99,6 @@ void score_fwd_kernel(ScoreFwdParams p) {
   const float unit = kAsR ? -cap.two : CAP || BIAS ? 1.f : t.scale_log2;
   const float base = kAsR ? cap.one : 0.f;
   const float slope = BIAS ? t.slopes[h] * kLog2E : 0.f;
-  // Scores under a moderate cap need no running maximum: with a bias that falls
-  // (relative to the nearest key, so that one weighs as without), the largest
-  // probability lies between 2^-kLow and 2^40 around a fixed reference.  (A float32
-  // O's third parts are 2^16 smaller, and must stay normal numbers.)
-  constexpr float kLow = EXACT ? 100.f : 120.f;
-  const bool fixed = CAP && !(slope < 0.f) && cap.two <= kLow + 40.f;
-  if (fixed) m = fminf(cap.one, kLow - cap.one);
   const int pos_min = BIAS ? wave_min(qpos) : 0;
   const int pos_max = BIAS ? wave_max(qpos) : 0;
   // The distance to the row's nearest key: biases are taken relative to it, so
@@ -277,27 +273,25 @@ void score_fwd_kernel(ScoreFwdParams p) {
             if (j < x || j >= y) sc[kt][i] = kAsR ? INFINITY : -INFINITY;
           }
       }
-      if (!fixed) {
-        float top = sc[0][0];
+      float top = sc[0][0];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+      for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            top = kAsR ? fminf(top, sc[kt][i]) : fmaxf(top, sc[kt][i]);
-        const float mx = max_with_other_half(fmaf(top, unit, base));
-        if (__builtin_amdgcn_ballot_w64(mx > m + kLag)) {
-          const float mn = fmaxf(m, mx);
-          // (Sums before the first score are 0, or what take_not_finite() put
-          // there, which a factor of 0 must not meet.)
-          const float alpha =
-              m == -INFINITY ? 1.f : fmaxf(exp2_fast(m - mn), 0x1p-126f);
-          l *= alpha;
+        for (int i = 0; i < 16; ++i)
+          top = kAsR ? fminf(top, sc[kt][i]) : fmaxf(top, sc[kt][i]);
+      const float mx = max_with_other_half(fmaf(top, unit, base));
+      if (__builtin_amdgcn_ballot_w64(mx > m + kLag)) {
+        const float mn = fmaxf(m, mx);
+        // (Sums before the first score are 0, or what take_not_finite() put
+        // there, which a factor of 0 must not meet.)
+        const float alpha =
+            m == -INFINITY ? 1.f : fmaxf(exp2_fast(m - mn), 0x1p-126f);
+        l *= alpha;
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c)
+        for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) oacc[c][i] *= alpha;
-          m = mn;
-        }
+          for (int i = 0; i < 16; ++i) oacc[c][i] *= alpha;
+        m = mn;
       }
       const float ref = base - (m == -INFINITY ? 0.f : m);
       float sum[2] = {0.f, 0.f};
@@ -386,9 +380,7 @@ void score_fwd_kernel(ScoreFwdParams p) {
   }
 
   // O = acc / l, LSE = (m + log2 l - slope off) ln 2; 0 and -inf without a key.
-  float lt = l + __shfl_xor(l, 32);
-  // A part without the row's nearest key may weigh next to nothing.
-  if (lt < 0x1p-126f) lt = 0.f;
+  const float lt = l + __shfl_xor(l, 32);
   const float inv = lt > 0.f ? 1.f / lt : lt;
   float lse = lt == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(lt);
   if (m == -INFINITY && lt != 0.f) lse = lt;  // NaN

@@ -291,13 +291,5 @@ __device__ __forceinline__ float cap_r(const Cap& c, float x) {
   return __builtin_amdgcn_rcpf(1.f + exp2_fast(x * c.in));
 }
 
-// The distance bias of a block: -slope (|i - j| - off), j the block's first
-// position plus step times 32 kt + acc_row.  Without a branch per key where all
-// of a wave's keys lie on one side of its rows.
-struct Bias {
-  float d0, step, off;
-  bool mixed;
-};
-
 }  // namespace dev
 }  // namespace mesh_attn

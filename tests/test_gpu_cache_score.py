@@ -184,6 +184,34 @@ def test_long_tables_are_cut(d, new, group):
         assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
 
 
+@pytest.mark.parametrize("d,new,group,dtype", [
+    (64, 1, 2, torch.float32), (128, 1, 4, torch.bfloat16),
+    (64, 20, 3, torch.bfloat16), (128, 6, 4, torch.float32)])
+@pytest.mark.parametrize("kind,cap,slopes", [("window", 4.0, True),
+                                             ("any", 0.0, True)])
+def test_more_short_sequences_than_waves(d, new, group, dtype, kind, cap,
+                                         slopes):
+    """Short tables and many requests: a wave for every sequence."""
+    b, rng = 500, np.random.default_rng(d)
+    c = cache_of(head_dim=d, num_kv_heads=9, num_pages=b * 8, max_pages=8)
+    lens = np.maximum(rng.integers(1, 128, b), new)
+    s = Scored(c, lens.tolist(), [new] * b, rule_of(kind, cap, slopes),
+               group=group)
+    got = s.run(dtype)
+    # The oracle on a few of them.
+    some = [0, 1, 250, 498, 499]
+    rows = np.concatenate([np.arange(s.cu[i], s.cu[i + 1]) for i in some])
+    part = Scored.__new__(Scored)
+    part.c, part.hq, part.scale, part.data = c, s.hq, s.scale, s.data
+    part.q, part.positions = s.q[rows], s.positions[rows]
+    part.cu = np.arange(len(some) + 1) * new
+    part.lens, part.table = s.lens[some], s.table[some]
+    part.rule = {k: x if k in ("cap", "slopes") else x[rows]
+                 for k, x in s.rule.items()}
+    at = torch.tensor(rows).cuda()
+    part.check((got[0][at], got[1][:, at]))
+
+
 def test_no_rule_is_the_call_without():
     c = cache_of(num_pages=100)
     b = Scored(c, [5, 100, 190], [1, 9, 2], {})

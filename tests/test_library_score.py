@@ -72,8 +72,9 @@ BAD_TILES = [
     (dict(prob=_prob(softmax_scale=0.0)), INVALID, "softmax_scale"),
     (dict(prob=_prob(softmax_scale=float("nan"))), INVALID, "softmax_scale"),
     (dict(prob=_prob(softmax_scale=3e38)), INVALID, "softmax_scale"),
-    (dict(prob=_prob(partition_len=2**27, num_q_heads=4)), UNSUPPORTED,
-     "2^28"),
+    (dict(prob=_prob(partition_len=2**24, num_q_heads=4)), UNSUPPORTED,
+     "2^27"),
+    (dict(prob=_prob(num_q_heads=65536)), UNSUPPORTED, "num_q_heads"),
     (dict(q_idx=[]), INVALID, "lists"), (dict(kv_idx=[]), INVALID, "lists"),
     (dict(nq=-1), INVALID, "lists"),
     (dict(q_idx=None, nq=2), INVALID, "q_idx is NULL"),
