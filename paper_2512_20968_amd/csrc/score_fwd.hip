@@ -11,6 +11,15 @@
 // it.  S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16: every lane owns
 // a query row, Q and O stay in registers, K and V stream from memory straight into
 // LDS, a block ahead.
+//
+// Bound by the vector unit (16384 causal rows of 32/8 heads of 128, cap: 2375 to
+// 2490 us, 0.88 to 0.93 PFLOP/s; vector unit busy 0.75 of the time, matrix unit
+// 0.45): a cap costs an exponential, a reciprocal and two more instructions per
+// score beside the softmax's own.  Rows of a wave, 32: a range, a position and a
+// slope per row are held beside O and Q, and two workgroups share a compute unit so
+// that one's products run beside the other's exponentials.  Documents packed into
+// 8192 rows 155 to 160 us, 0.5 PFLOP/s, by blocks that hold a border and the round
+// trips at an item's start; 77 rows 9 us, all round trips.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
