@@ -254,6 +254,24 @@ def test_a_steep_bias_over_a_bad_last_page():
             assert (o[r, :2] - v[0, 0].float()).abs().max() <= 2.0 ** -14 * 6
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cap", [30.0, 48.0, 50.0, 55.0])
+def test_a_gentle_bias_under_scores_at_the_low_end_of_the_cap(cap, dtype):
+    """Every score is -cap: the weights of a thousand keys with a bias of one to
+    eleven units count, however far the reference lies from them."""
+    c, n = cache_of(num_pages=300, max_pages=128), 2000
+    rule = {"cap": cap, "slopes": np.float32([0.005, 0.01, 0.002, 0.0])}
+    b = Scored(c, [n], [3], rule)
+    r = np.arange(n)
+    slots = b.table[0, r // 16] * 16 + r % 16
+    k = torch.ones(n, 2, 64, dtype=torch.bfloat16, device="cuda")
+    v = torch.randn(n, 2, 64, device="cuda",
+                    generator=torch.Generator("cuda").manual_seed(4))
+    ma.mesh_attn_cache_append(c, k, v.bfloat16(), i64(slots), b.data)
+    b.q = torch.full_like(b.q, -50.0)
+    b.check(b.run(dtype))
+
+
 def test_keys_before_the_first_rows_begin_are_not_seen():
     c = cache_of(num_pages=60)
     b = Scored(c, [150], [4], {"key_begin": np.array([70, 10, 90, 0])})
