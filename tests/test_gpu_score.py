@@ -311,6 +311,25 @@ def test_slices_of_a_fused_projection(d):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_widest_strides_pass_32_bits(d):
+    prob = problem(205, hq=2, hkv=1, d=d)
+    rule = on_gpu(make_rule(prob, [0], "docs", 5.0, True, 2))
+    q, k, v, do = (x.cuda() for x in tile_inputs(prob, [0], [0], 7))
+    o, lse = run_forward(prob, [0], [0], rule, q, k, v)
+    grads = run_backward(prob, [0], [0], rule, q, k, v, o, do, lse)
+    wide = torch.empty(205, 2 ** 24, dtype=torch.bfloat16, device="cuda")
+    parts = [wide[:, at:at + n * d].view(205, n, d)
+             for at, n in ((0, 2), (2 ** 23, 1), (2 ** 24 - d, 1))]
+    for x, y in zip(parts, (q, k, v)):
+        x.copy_(y)
+    o2, lse2 = run_forward(prob, [0], [0], rule, *parts)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    for x, y in zip(grads, run_backward(prob, [0], [0], rule, *parts, o, do,
+                                        lse)):
+        assert torch.equal(x, y)
+
+
 def test_other_streams_and_workspaces():
     """Calls on a stream of their own, with a workspace and without; a
     workspace's old contents do not matter, and nothing behind it is touched."""
