@@ -188,6 +188,12 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
   using L = KvLayout<D>;
   using T = Staged<D>;
   constexpr int kRow = T::kRowBytes;
+  // dO V^T is held beside the scores, and P T' enters dS in float32 (3001 rows of 12
+  // heads 49 us, 52 with P T' in bf16).  At head dim 128 that spills 31 to 89
+  // registers: P T' waits for dO V^T in bf16 there, 2^-8 of it, and dK is off by
+  // 0.0029 of its norm instead of 0.0025 (as it is with 16 bits without a sign,
+  // which take 4 % longer).
+  constexpr bool kBoth = D == 64;
   int* s_flags = reinterpret_cast<int*>(smem + KvLayout<D>::kFlags);
   const ScoreTile& t = p.t;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
@@ -362,16 +368,30 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
         const float kpos_rel = BIAS ? static_cast<float>(kpos - st.pos) : 0.f;
 #pragma unroll
         for (int qt = 0; qt < 2; ++qt) {
-          f32x16 x;
-          auto scores = [&](const bf16x8 (&f)[D / 16], int tile) {
+          auto product = [&](const bf16x8 (&f)[D / 16], int tile, f32x16 z) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
-              x = mfma32(lds_row((ra ^ (32 * kk)) + tile + qt * 32 * kRow),
-                         f[kk], x);
+              z = mfma32(lds_row((ra ^ (32 * kk)) + tile + qt * 32 * kRow),
+                         f[kk], z);
             pipeline_reads<D / 16, 1, 3>();
+            return z;
           };
+          // dO V^T - D: the accumulators start with -D.
+          auto d_probs = [&]() {
+            f32x16 z;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const f32x4 dlt = lds_four<f32x4>(
+                  fa + 256 + 4 * (qt * 32 + (i >> 1) * 16 + (i & 1) * 4));
+#pragma unroll
+              for (int e = 0; e < 4; ++e) z[i * 4 + e] = dlt[e];
+            }
+            return product(vf, L::kTile, z);
+          };
+          f32x16 x, y;
+          if (kBoth) y = d_probs();
           zero(x);
-          scores(kf, 0);
+          x = product(kf, 0, x);
           // Four queries at a time: more would not fit the registers.
           bf16x4 p4[4], d4[4];
 #pragma unroll
@@ -393,7 +413,7 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
               float g1;
               e4[e] = probability<CAP, BIAS>(cap, t.scale_log2, slope,
                                              x[i * 4 + e], far, lse[e], &g1);
-              g4[e] = g1;
+              g4[e] = kBoth ? g1 * y[i * 4 + e] : g1;
             }
             if (__builtin_expect(fix, 0)) {
               const uint32_t b4 = static_cast<uint32_t>(
@@ -408,37 +428,31 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
             }
             p4[i] = __builtin_convertvector(e4, bf16x4);
             // Unpacked below instead of rounded again.
-            asm("" : "+v"(p4[i]));
-            if (CAP) {
+            if (!kBoth) asm("" : "+v"(p4[i]));
+            if (CAP || kBoth) {
               d4[i] = __builtin_convertvector(g4, bf16x4);
-              asm("" : "+v"(d4[i]));
+              if (!kBoth) asm("" : "+v"(d4[i]));
             }
             if (D == 128) __builtin_amdgcn_sched_barrier(0);
           }
-          // dO V^T - D: the accumulators start with -D.
+          if (!kBoth) {
+            y = d_probs();
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x4 dlt = lds_four<f32x4>(
-                fa + 256 + 4 * (qt * 32 + (i >> 1) * 16 + (i & 1) * 4));
+            for (int i = 0; i < 4; ++i) {
+              f32x4 g4 = __builtin_convertvector(CAP ? d4[i] : p4[i], f32x4);
+              f32x4 z;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[i * 4 + e] = dlt[e];
-          }
-          scores(vf, L::kTile);
+              for (int e = 0; e < 4; ++e) z[e] = y[i * 4 + e];
+              if (__builtin_expect(fix, 0)) {  // a hidden pair's product with a NaN of dO V^T is 0
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            f32x4 g4 = __builtin_convertvector(CAP ? d4[i] : p4[i], f32x4);
-            f32x4 y;
+                for (int e = 0; e < 4; ++e)
+                  if (g4[e] == 0.f) z[e] = 0.f;
+              }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = x[i * 4 + e];
-            if (__builtin_expect(fix, 0)) {  // a hidden pair's product with a NaN of dO V^T is 0
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (g4[e] == 0.f) y[e] = 0.f;
+              for (int e = 0; e < 4; ++e) g4[e] *= z[e];
+              d4[i] = __builtin_convertvector(g4, bf16x4);
+              __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) g4[e] *= y[e];
-            d4[i] = __builtin_convertvector(g4, bf16x4);
-            if (D == 128) __builtin_amdgcn_sched_barrier(0);
           }
           bf16x8 pf[2], ds[2];
 #pragma unroll
