@@ -18,10 +18,11 @@ namespace {
 // Attention over the cache, with a score rule or without.
 ma_status_t cache_fwd(
     const ma_cache_t* cache, int32_t num_q_heads, float softmax_scale,
-    bool rule, const ma_score_t* score, int32_t num_requests, int64_t rows, const void* q, int64_t q_stride,
-    const int32_t* positions, const int32_t* cu_new, const int32_t* lens,
-    const int32_t* block_table, const void* data, void* o, ma_dtype_t o_dtype,
-    float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+    bool rule, const ma_score_t* score, int32_t num_requests, int64_t rows,
+    const void* q, int64_t q_stride, const int32_t* positions,
+    const int32_t* cu_new, const int32_t* lens, const int32_t* block_table,
+    const void* data, void* o, ma_dtype_t o_dtype, float* lse, void* ws,
+    size_t ws_bytes, hipStream_t stream) {
   CacheFwdParams p;
   MA_TRY(check_cache(cache, &p.c));
   MA_TRY(check_q_heads(num_q_heads, p.c.hkv));

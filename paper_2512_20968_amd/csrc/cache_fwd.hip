@@ -1057,7 +1057,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
           if (whole) {
             const TokenHead th = token_head(p, rr, prev.kvh);
             store_row<D, OUT_F32, RULE>(p, prev.first + th.tok, th.head,
-                                        prev.from, prev.local, dim0, acc, ref, L);
+                                        prev.from, prev.local, dim0, acc, ref,
+                                        L);
           } else {
             const int64_t pr = int64_t{slot} * kRows + 16 * q + row16;
             if (dim0 == 0) {
@@ -1192,7 +1193,8 @@ void cache_fwd_kernel(CacheFwdParams p) {
                        (RULE && !OUT_F32 ? factor : 1.f);
             store_row<D, OUT_F32, RULE>(
                 p, it.first + th.tok, th.head, it.from, it.local,
-                g * (D / 4) + 8 * j, acc, st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
+                g * (D / 4) + 8 * j, acc,
+                st.limit[q] == -INFINITY ? 0.f : -st.neg_ref[q], l);
           }
         }
       }
@@ -1296,7 +1298,8 @@ void cache_fold_kernel(CacheFwdParams p) {
     if (pg == 0 && valid) {
       const TokenHead th = token_head(p, rr, f.kvh);
       store_row<D, OUT_F32, RULE>(p, f.first + th.tok, th.head, f.from,
-                                  f.local, dim0, acc, M == -INFINITY ? 0.f : M, L);
+                                  f.local, dim0, acc,
+                                  M == -INFINITY ? 0.f : M, L);
     }
     __syncthreads();
   }

@@ -443,7 +443,8 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
               f32x4 z;
 #pragma unroll
               for (int e = 0; e < 4; ++e) z[e] = y[i * 4 + e];
-              if (__builtin_expect(fix, 0)) {  // a hidden pair's product with a NaN of dO V^T is 0
+              // A hidden pair's product with a NaN of dO V^T is 0.
+              if (__builtin_expect(fix, 0)) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                   if (g4[e] == 0.f) z[e] = 0.f;
