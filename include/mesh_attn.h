@@ -584,7 +584,7 @@ ma_status_t mesh_attn_rope(const ma_rope_t* rope, int64_t rows,
  * the prefix's; a window of w: begin at least p_i - w + 1; padding: begin = end.
  * ------------------------------------------------------------------------- */
 typedef struct {
-  float cap;                /* 0: none; else finite and > 0                  */
+  float cap;                /* 0: none; else > 0, at most 2^100              */
   const float* slopes;      /* [num_q_heads] device, or NULL: no bias        */
   const int32_t* key_begin; /* [rows] device, or NULL: 0                     */
   const int32_t* key_end;   /* [rows] device, or NULL: p_i + 1 (the tile calls

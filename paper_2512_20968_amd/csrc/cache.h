@@ -7,6 +7,12 @@
 
 namespace mesh_attn {
 
+// Caps above this are wide ones: a capped score made as cap - 2 cap r is off by
+// 2^-23 of the cap (2^-15 of one up to here, 2^-7 of a bf16 weight's rounding),
+// whatever its own size; under a wide cap small arguments of the tanh take its
+// series.
+constexpr float kWideCap = 256.f;
+
 // Which positions of a sequence a cache stores, and how many of them lie below
 // a position.
 struct CacheShare {

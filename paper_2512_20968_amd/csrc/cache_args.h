@@ -129,13 +129,15 @@ inline ma_status_t check_q_heads(int32_t hq, int32_t hkv) {
 }
 
 // A score rule: a cap of 0 or a positive one that the scores can be divided by.
+// (Up to 2^100: a score over the cap is then a normal float32 down to scores of
+// 2^-26.)
 inline ma_status_t check_score(const ma_score_t* s, float softmax_scale) {
   if (!s) return MA_OK;
   if (!(s->cap >= 0.f) || !std::isfinite(s->cap))
     return fail(MA_ERR_INVALID_ARG, "cap must be 0 or positive and finite");
   if (s->cap > 0.f) {
     const float in = 2.f * softmax_scale * 1.4426950408889634f / s->cap;
-    if (!std::isfinite(in) || !(in > 0.f) || !std::isfinite(4.f * s->cap))
+    if (!std::isfinite(in) || !(in >= 0x1p-124f) || s->cap > 0x1p100f)
       return fail(MA_ERR_INVALID_ARG, "cap %g: out of range of the scores",
                   s->cap);
   }

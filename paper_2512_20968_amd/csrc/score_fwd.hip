@@ -50,9 +50,9 @@ struct Layout {
 };
 
 // EXACT (float32 O): the probabilities enter the second product as a sum of three
-// bf16 that hold all 24 bits, and the tanh of small arguments is a polynomial;
-// else rounded to bf16, 2^-8 of each, as O itself is.
-template <int D, bool CAP, bool BIAS, bool EXACT>
+// bf16 that hold all 24 bits; else rounded to bf16, 2^-8 of each, as O itself is.
+// FINE (float32 O, and wide caps): the tanh of small arguments is a polynomial.
+template <int D, bool CAP, bool BIAS, bool EXACT, bool FINE>
 __global__ __launch_bounds__(NT, D == 128 ? 2 : 3)
 void score_fwd_kernel(ScoreFwdParams p) {
   using L = Layout<D>;
@@ -103,8 +103,8 @@ void score_fwd_kernel(ScoreFwdParams p) {
   const Cap cap = cap_of(t);
   // What is kept of a score: its product (scaled in the exponent), the r of the
   // cap (x = one - two r, the least of which is the largest score), or, with a
-  // bias or a float32 O, x itself in log2 units.
-  constexpr bool kAsR = CAP && !BIAS && !EXACT;
+  // bias or where the tanh is fine, x itself in log2 units.
+  constexpr bool kAsR = CAP && !BIAS && !FINE;
   const float unit = kAsR ? -cap.two : CAP || BIAS ? 1.f : t.scale_log2;
   const float base = kAsR ? cap.one : 0.f;
   const float slope = BIAS ? t.slopes[h] * kLog2E : 0.f;
@@ -221,15 +221,9 @@ void score_fwd_kernel(ScoreFwdParams p) {
               continue;
             }
             float y = fmaf(-cap.two, cap_r(cap, x), cap.one);
-            if (EXACT) {
-              // Taylor; the first term left out is below 2^-25 of the sum.
-              const float u = x * (t.scale / t.cap), z = u * u;
-              float s = fmaf(z, -1382.f / 155925, 62.f / 2835);
-              s = fmaf(s, z, -17.f / 315);
-              s = fmaf(s, z, 2.f / 15);
-              s = fmaf(s, z, -1.f / 3);
-              s = fmaf(s * z, u, u);
-              y = fabsf(u) < 0.4f ? s * cap.one : y;
+            if (FINE) {
+              const float u = x * cap.unit;
+              y = fabsf(u) < kSeries ? tanh_series(u) * cap.one : y;
             }
             sc[kt][i] = y;
           }
@@ -424,9 +418,9 @@ void score_fwd_kernel(ScoreFwdParams p) {
     }
 }
 
-template <int D, bool CAP, bool BIAS, bool EXACT>
+template <int D, bool CAP, bool BIAS, bool EXACT, bool FINE>
 hipError_t launch(const ScoreFwdParams& p, hipStream_t stream) {
-  constexpr auto kernel = score_fwd_kernel<D, CAP, BIAS, EXACT>;
+  constexpr auto kernel = score_fwd_kernel<D, CAP, BIAS, EXACT, FINE>;
   constexpr int lds = Layout<D>::kLds;
   const hipError_t e = ensure_dynamic_lds<kernel>(lds);
   if (e != hipSuccess) return e;
@@ -439,11 +433,14 @@ hipError_t launch(const ScoreFwdParams& p, hipStream_t stream) {
 
 template <int D, bool EXACT>
 hipError_t launch_d(const ScoreFwdParams& p, hipStream_t stream) {
+  if (p.t.cap > kWideCap)
+    return p.t.slopes ? launch<D, true, true, EXACT, true>(p, stream)
+                      : launch<D, true, false, EXACT, true>(p, stream);
   if (p.t.cap > 0.f)
-    return p.t.slopes ? launch<D, true, true, EXACT>(p, stream)
-                      : launch<D, true, false, EXACT>(p, stream);
-  return p.t.slopes ? launch<D, false, true, EXACT>(p, stream)
-                    : launch<D, false, false, EXACT>(p, stream);
+    return p.t.slopes ? launch<D, true, true, EXACT, EXACT>(p, stream)
+                      : launch<D, true, false, EXACT, EXACT>(p, stream);
+  return p.t.slopes ? launch<D, false, true, EXACT, EXACT>(p, stream)
+                    : launch<D, false, false, EXACT, EXACT>(p, stream);
 }
 
 }  // namespace

@@ -279,16 +279,30 @@ struct Cap {
   float in;    // product -> log2(e^(2u))
   float two;   // 2 cap log2(e)
   float one;   // cap log2(e)
+  float unit;  // product -> u
 };
 __device__ __forceinline__ Cap cap_of(const ScoreTile& t) {
   Cap c;
   c.in = t.cap > 0.f ? 2.f * t.scale_log2 / t.cap : 0.f;
   c.one = t.cap * kLog2E;
   c.two = 2.f * c.one;
+  c.unit = t.cap > 0.f ? t.scale / t.cap : 0.f;
   return c;
 }
 __device__ __forceinline__ float cap_r(const Cap& c, float x) {
   return __builtin_amdgcn_rcpf(1.f + exp2_fast(x * c.in));
+}
+
+// tanh(u) for |u| < kSeries, off by a few 2^-24 of itself (1 - 2 r is by 2^-23 of
+// one): Taylor; the first term left out is below 2^-23.9 of the sum.
+constexpr float kSeries = 0.4f;
+__device__ __forceinline__ float tanh_series(float u) {
+  const float z = u * u;
+  float s = fmaf(z, -1382.f / 155925, 62.f / 2835);
+  s = fmaf(s, z, -17.f / 315);
+  s = fmaf(s, z, 2.f / 15);
+  s = fmaf(s, z, -1.f / 3);
+  return fmaf(s * z, u, u);
 }
 
 }  // namespace dev

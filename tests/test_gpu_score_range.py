@@ -1,0 +1,70 @@
+"""Attention under a score rule at the ends of what its arguments may be, on the
+GPU: wide caps."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import score as os_
+
+from score_helpers import (E, Bounds, make_rule, on_gpu, problem, run_forward,
+                           tile_inputs)
+
+pytestmark = pytest.mark.gpu
+
+
+# -- wide caps ----------------------------------------------------------------
+
+class WideBounds(Bounds):
+    """The bounds for a cap that says nothing about the scores' size: what the
+    tanh is off by is relative to the score.  Of its series (|u| < 0.4) a few E;
+    of 1 - 2 r, with r's exponential, reciprocal and product off by a few E each
+    of at most one, 2^-21, and tanh is above 0.38: 2^-19 of the score covers
+    both."""
+
+    def __init__(self, prob, q_idx, kv_idx, rule, q, k, v):
+        super().__init__(prob, q_idx, kv_idx, rule, q, k, v)
+        qpos, kpos = (os_.positions(prob, x) for x in (q_idx, kv_idx))
+        lo, hi = os_.ranges(prob, rule, qpos)
+        s, d, hq = (prob["softmax_scale"], prob["head_dim"],
+                    prob["num_q_heads"])
+        for h in range(hq):
+            hk = h // (hq // prob["num_kv_heads"])
+            slope = float(rule["slopes"][h]) if "slopes" in rule else 0.0
+            x, seen, _ = os_.scores(self.q[:, h], self.k[:, hk], s,
+                                    rule["cap"], slope, qpos, kpos, lo, hi)
+            far = np.abs(qpos[:, None] - kpos[None, :]) * abs(slope)
+            mag = s * np.abs(self.q[:, h]) @ np.abs(self.k[:, hk]).T
+            # (The nearest key is the row's own: no bias that all share.)
+            e = (E * (d + 8) * mag + 2.0 ** -19 * np.abs(x + far)
+                 + 8 * E * far + 2.0 ** -21)
+            e = np.where(self.p[h] > 2.0 ** -40, e, 0)
+            self.err[h] = e.max(1, initial=0)
+
+
+WIDE_CAPS = [300.0, 1e3, 1e4, 1e5, 1e7, 1e30]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("cap", WIDE_CAPS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_wide_caps(cap, slopes, d, dtype):
+    prob = problem(150, hq=2, hkv=1, d=d)
+    rule = make_rule(prob, [0], "causal", cap, slopes, 3)
+    q, k, v, do = (x.cuda() for x in tile_inputs(prob, [0], [0], 5))
+    want = WideBounds(prob, [0], [0], rule, q, k, v)
+    o, lse = run_forward(prob, [0], [0], on_gpu(rule), q, k, v, dtype)
+    want.check_forward(o, lse, dtype is torch.float32)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_wide_caps_that_bend(dtype):
+    """Scores of a few times a cap of 1000."""
+    prob = problem(140, hq=2, hkv=1, d=64)
+    q, k, v, do = (x.cuda() for x in
+                   tile_inputs(prob, [0], [0], 9, wide=300.0))
+    rule = dict(cap=1000.0)
+    want = WideBounds(prob, [0], [0], rule, q, k, v)
+    o, lse = run_forward(prob, [0], [0], rule, q, k, v, dtype)
+    want.check_forward(o, lse, dtype is torch.float32)
