@@ -3,7 +3,8 @@
 //
 // With P = exp(x - LSE) over the keys that are seen and T' = 1 - tanh^2 of the cap
 // (4 r (1 - r) with the r of cap_r()):  dV = P^T dO,  dS = P T' (dO V^T - D),
-// D = <dO, O>,  dK = s dS^T Q,  dQ = s dS K.
+// D = <dO, O>,  dK = s dS^T Q,  dQ = s dS K.  (Under a wide cap small arguments of
+// the tanh take its series, and T' is 1 - tanh^2 of that.)
 //
 // Two launches, and one more for each pass whose items are cut:
 //  1. prep: D and LSE log2(e) of every (row, head); every row's range and
@@ -105,23 +106,33 @@ __global__ __launch_bounds__(NT) void score_prep_kernel(ScoreBwdParams p,
     }
     p.delta[at] = -s;
     // Without the cap's constant part (see probability()).
-    p.lse2[at] = lse == -INFINITY
-                     ? INFINITY
-                     : fmaf(lse, kLog2E, -t.cap * kLog2E);
+    const float part = t.cap > kWideCap ? 0.f : t.cap;
+    p.lse2[at] =
+        lse == -INFINITY ? INFINITY : fmaf(lse, kLog2E, -part * kLog2E);
   }
 }
 
-// Scores x -> probability and, in *g, its product with a quarter of the cap's
-// derivative 4 r (1 - r).  lse2: LSE less the cap; far: |i - j|.
-template <bool CAP, bool BIAS>
+// What the scores are put through: nothing, a cap, a wide one.
+constexpr int kNoCap = 0, kCap = 1, kFineCap = 2;
+
+// Scores x -> probability and, in *g, its product with the cap's derivative: a
+// quarter of 4 r (1 - r), or 1 - tanh^2 of a wide one.  lse2: LSE less a cap that
+// is not wide; far: |i - j|.
+template <int CAP, bool BIAS>
 __device__ __forceinline__ float probability(const Cap& cap, float scale_log2,
                                              float slope, float x, float far,
                                              float lse2, float* g) {
   float y, d = 1.f;
-  if (CAP) {
+  if (CAP == kCap) {
     const float r = cap_r(cap, x);
     y = fmaf(-cap.two, r, -lse2);
     d = fmaf(-r, r, r);
+  } else if (CAP == kFineCap) {
+    const float u = x * cap.unit;
+    const float h =
+        fabsf(u) < kSeries ? tanh_series(u) : fmaf(-2.f, cap_r(cap, x), 1.f);
+    y = fmaf(cap.one, h, -lse2);
+    d = fmaf(-h, h, 1.f);
   } else {
     y = fmaf(x, scale_log2, -lse2);
   }
@@ -132,9 +143,9 @@ __device__ __forceinline__ float probability(const Cap& cap, float scale_log2,
 }
 
 // The factor of dQ and dK that the sums lack.
-template <bool CAP>
+template <int CAP>
 __device__ __forceinline__ float grad_scale(const ScoreTile& t) {
-  return CAP ? 4.f * t.scale : t.scale;
+  return CAP == kCap ? 4.f * t.scale : t.scale;
 }
 
 template <int N>
@@ -182,7 +193,7 @@ __device__ __forceinline__ void stage_words(const void* src, char* dst,
                                            0, 0);
 }
 
-template <int D, bool CAP, bool BIAS, bool OUT_F32>
+template <int D, int CAP, bool BIAS, bool OUT_F32>
 __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
                                           int id) {
   using L = KvLayout<D>;
@@ -527,7 +538,7 @@ struct QLayout {
   static constexpr int kLds = 2 * kStage;
 };
 
-template <int D, bool CAP, bool BIAS, bool OUT_F32>
+template <int D, int CAP, bool BIAS, bool OUT_F32>
 __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
                                         int id) {
   using L = QLayout<D>;
@@ -731,7 +742,7 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
 
 // Both passes in one launch: the dK/dV items first, the longest of a causal tile
 // at their front, and dQ items wherever one of them ends.
-template <int D, bool CAP, bool BIAS, bool OUT_F32>
+template <int D, int CAP, bool BIAS, bool OUT_F32>
 __global__ __launch_bounds__(NT, D == 128 ? 2 : 3)
 void score_bwd_kernel(ScoreBwdParams p) {
   extern __shared__ __align__(16) char smem[];
@@ -799,7 +810,7 @@ hipError_t launch_sum(const SumParams& p, int arrays, bool out_f32,
   return hipGetLastError();
 }
 
-template <int D, bool CAP, bool BIAS, bool OUT_F32>
+template <int D, int CAP, bool BIAS, bool OUT_F32>
 hipError_t launch(const ScoreBwdParams& p, hipStream_t stream) {
   constexpr auto kernel = score_bwd_kernel<D, CAP, BIAS, OUT_F32>;
   constexpr int lds = KvLayout<D>::kLds;
@@ -846,11 +857,14 @@ hipError_t launch(const ScoreBwdParams& p, hipStream_t stream) {
 
 template <int D, bool OUT_F32>
 hipError_t launch_d(const ScoreBwdParams& p, hipStream_t stream) {
+  if (p.t.cap > kWideCap)
+    return p.t.slopes ? launch<D, kFineCap, true, OUT_F32>(p, stream)
+                      : launch<D, kFineCap, false, OUT_F32>(p, stream);
   if (p.t.cap > 0.f)
-    return p.t.slopes ? launch<D, true, true, OUT_F32>(p, stream)
-                      : launch<D, true, false, OUT_F32>(p, stream);
-  return p.t.slopes ? launch<D, false, true, OUT_F32>(p, stream)
-                    : launch<D, false, false, OUT_F32>(p, stream);
+    return p.t.slopes ? launch<D, kCap, true, OUT_F32>(p, stream)
+                      : launch<D, kCap, false, OUT_F32>(p, stream);
+  return p.t.slopes ? launch<D, kNoCap, true, OUT_F32>(p, stream)
+                    : launch<D, kNoCap, false, OUT_F32>(p, stream);
 }
 
 }  // namespace

@@ -7,7 +7,7 @@ import torch
 
 from oracle import score as os_
 
-from score_helpers import (E, Bounds, make_rule, on_gpu, problem, run_forward,
+from score_helpers import (E, Bounds, make_rule, on_gpu, problem, run_backward, run_forward,
                            tile_inputs)
 
 pytestmark = pytest.mark.gpu
@@ -58,6 +58,23 @@ def test_wide_caps(cap, slopes, d, dtype):
     want.check_forward(o, lse, dtype is torch.float32)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("cap", WIDE_CAPS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gradients_under_wide_caps(cap, slopes, d, dtype):
+    """LSE from the oracle, so that the backward stands by itself."""
+    prob = problem(150, hq=2, hkv=1, d=d)
+    rule = make_rule(prob, [0], "causal", cap, slopes, 3)
+    q, k, v, do = (x.cuda() for x in tile_inputs(prob, [0], [0], 5))
+    want = WideBounds(prob, [0], [0], rule, q, k, v)
+    o = torch.tensor(want.o).to(torch.bfloat16).cuda()
+    lse = torch.tensor(want.lse).float().cuda()
+    grads = run_backward(prob, [0], [0], on_gpu(rule), q, k, v, o, do, lse,
+                         grads=dtype)
+    want.check_backward(o, lse, do, *grads)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_wide_caps_that_bend(dtype):
     """Scores of a few times a cap of 1000."""
@@ -68,3 +85,16 @@ def test_wide_caps_that_bend(dtype):
     want = WideBounds(prob, [0], [0], rule, q, k, v)
     o, lse = run_forward(prob, [0], [0], rule, q, k, v, dtype)
     want.check_forward(o, lse, dtype is torch.float32)
+
+
+@pytest.mark.parametrize("cap", [255.0, 256.0, 257.0])
+def test_caps_around_the_wide_ones(cap):
+    """On both sides of where the kernels change over, each other's results."""
+    prob = problem(150, hq=2, hkv=1, d=128)
+    q, k, v, do = (x.cuda() for x in tile_inputs(prob, [0], [0], 5))
+    rule = dict(cap=cap)
+    want = Bounds(prob, [0], [0], rule, q, k, v)
+    o, lse = run_forward(prob, [0], [0], rule, q, k, v)
+    want.check_forward(o, lse, False)
+    grads = run_backward(prob, [0], [0], rule, q, k, v, o, do, lse)
+    want.check_backward(o, lse, do, *grads)
