@@ -72,6 +72,7 @@ ma_status_t cache_fwd(
   p.group = num_q_heads / p.c.hkv;
   p.num_requests = num_requests;
   p.rule = rule;
+  p.wide_cap = score && score->cap > kWideCap;
   p.cap_in = p.cap_two = p.cap_u = 0.f;
   p.slopes = nullptr;
   p.key_begin = p.key_end = nullptr;

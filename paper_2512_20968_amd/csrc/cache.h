@@ -114,7 +114,7 @@ struct CacheFwdParams {
   int32_t max_units;  // most of a launch
   // The score rule (rule = 1): cap_two = 2 cap log2(e), 0 without a cap; a
   // product times cap_in is log2(e^(2u)), times cap_u u = score / cap.
-  int32_t rule;
+  int32_t rule, wide_cap;
   float cap_in, cap_two, cap_u;
   const float* slopes;
   const int32_t* key_begin;

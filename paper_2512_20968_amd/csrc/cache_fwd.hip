@@ -255,15 +255,15 @@ __device__ __forceinline__ RuleRow rule_row(const CacheFwdParams& p,
 }
 
 // Products of a step -> scores in log2 units: capped (tanh(u) = 1 - 2 / (1 +
-// e^(2u)); small arguments of a float32 O by its series) and biased.
-template <bool EXACT>
+// e^(2u)); FINE: small arguments by its series) and biased.
+template <bool FINE>
 __device__ __forceinline__ float capped(const CacheFwdParams& p, float v,
                                         float add) {
   const float r =
       __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * p.cap_in));
   const float y = fmaf(-p.cap_two, r, fmaf(0.5f, p.cap_two, add));
-  if (!EXACT) return y;
-  // Taylor; the first term left out is below 2^-25 of the sum.
+  if (!FINE) return y;
+  // Taylor; the first term left out is below 2^-23.9 of the sum.
   const float u = v * p.cap_u, z = u * u;
   float t = fmaf(z, -1382.f / 155925, 62.f / 2835);
   t = fmaf(t, z, -17.f / 315);
@@ -291,10 +291,14 @@ __device__ __forceinline__ void rule_step(const CacheFwdParams& p,
   for (int q = 0; q < NQ; ++q) {
     const float add =
         before ? -rs.slope[q] * static_cast<float>(behind(q) - rs.off[q]) : 0.f;
-    if (p.cap_two > 0.f) {
+    if (p.cap_two > 0.f && (EXACT || p.wide_cap)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        x[q][i >> 2][i & 3] = capped<EXACT>(p, x[q][i >> 2][i & 3], add);
+        x[q][i >> 2][i & 3] = capped<true>(p, x[q][i >> 2][i & 3], add);
+    } else if (p.cap_two > 0.f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[q][i >> 2][i & 3] = capped<false>(p, x[q][i >> 2][i & 3], add);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)

@@ -5,10 +5,14 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2512_20968_amd as ma
+from oracle import cache as oc
 from oracle import score as os_
 
-from score_helpers import (E, Bounds, make_rule, on_gpu, problem, run_backward, run_forward,
-                           tile_inputs)
+from score_helpers import (E, U, Bounds, make_rule, np64, on_gpu, problem,
+                           run_backward, run_forward, tile_inputs)
+from test_gpu_cache import cache_of, i64
+from test_gpu_cache_score import Scored
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +102,46 @@ def test_caps_around_the_wide_ones(cap):
     want.check_forward(o, lse, False)
     grads = run_backward(prob, [0], [0], rule, q, k, v, o, do, lse)
     want.check_backward(o, lse, do, *grads)
+
+
+def one_request(c, rows, length, rule, group, dtype):
+    """O, LSE of a request's last rows, the oracle's, and the error of a score
+    that the products make."""
+    b = Scored(c, [length], [rows], rule, group=group)
+    o, lse = b.run(dtype)
+    n = oc.stored(c, length)
+    r = np.arange(n)
+    page = b.table[0, r // c["page_size"]]
+    slots = page * c["page_size"] + r % c["page_size"]
+    d = c["head_dim"]
+    k = torch.empty(n, c["num_kv_heads"], d, dtype=torch.bfloat16,
+                    device="cuda")
+    v = torch.empty_like(k)
+    ma.mesh_attn_cache_read(c, i64(slots), b.data, k, v)
+    q, k, v = np64(b.q), np64(k), np64(v)
+    args = (b.scale, b.rule, q, b.positions, oc.key_positions(c, n), k)
+    wo, wl = os_.cached(*args, v, length)
+    mass, _ = os_.cached(*args, np.abs(v), length)
+    reach = b.scale * np.stack(
+        [np.abs(q[:, h]) @ np.abs(k[:, h // group]).T
+         for h in range(q.shape[1])])
+    err = (d + 16) * 2.0 ** -23 * reach.max(-1)
+    return np64(o), np64(lse), wo, wl, mass, err
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", WIDE_CAPS)
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_wide_caps_over_the_cache(cap, rows, d, dtype):
+    """As over a tile; 2^-14 for the exponentials and sums."""
+    c = cache_of(head_dim=d, num_pages=40, max_pages=20)
+    o, lse, wo, wl, mass, err = one_request(c, rows, 300, dict(cap=cap), 2,
+                                            dtype)
+    # Scores that weigh 2^-40 of the row or more lie within 28 of its LSE.
+    err = err + 2.0 ** -19 * (np.abs(wl) + 28) + 2.0 ** -14
+    assert (np.abs(lse - wl) <= err).all(), np.abs(lse - wl).max()
+    tol = 2 * mass * err.T[:, :, None]
+    if dtype is torch.bfloat16:
+        tol += U * (mass + np.abs(wo))
+    assert (np.abs(o - wo) <= tol).all(), (np.abs(o - wo) - tol).max()
