@@ -99,8 +99,9 @@ __global__ __launch_bounds__(NT) void score_prep_kernel(ScoreBwdParams p,
     float lse = valid ? p.lse[int64_t{h} * t.rows_q + row] : -INFINITY;
     const int64_t at = int64_t{h} * p.rows_pad + row;
     // A D that is not finite makes the probabilities NaN instead, which hidden
-    // pairs do not have.
-    if (!(fabsf(s) < INFINITY)) {
+    // pairs do not have.  (One that dO V^T could take to infinity counts as such;
+    // rows without keys need none.)
+    if (!(fabsf(s) < 0x1.cp127f) || lse == -INFINITY) {
       s = 0.f;
       if (lse != -INFINITY) lse = NAN;
     }
@@ -148,8 +149,9 @@ __device__ __forceinline__ float grad_scale(const ScoreTile& t) {
   return CAP == kCap ? 4.f * t.scale : t.scale;
 }
 
+// Whether an operand holds large values or some that are not finite.
 template <int N>
-__device__ __forceinline__ bool not_finite(const bf16x8 (&f)[N]) {
+__device__ __forceinline__ bool holds_large(const bf16x8 (&f)[N]) {
   typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
   bool bad = false;
 #pragma unroll
@@ -157,7 +159,7 @@ __device__ __forceinline__ bool not_finite(const bf16x8 (&f)[N]) {
     const u32x4v w = __builtin_bit_cast(u32x4v, f[i]);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      bad |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
+      bad |= (w[j] & 0x7f80u) >= kLarge || (w[j] & 0x7f800000u) >= kLarge << 16;
   }
   return bad;
 }
@@ -341,7 +343,7 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
     wait_vmem();
     __syncthreads();
     int buf = 0;
-    const bool keys_bad = __any(not_finite(kf) || not_finite(vf));
+    const bool keys_large = __any(holds_large(kf) || holds_large(vf));
     // Operand addresses with the stage's base in them.
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
     uint32_t ra = lds0 + T::row_read(lane);
@@ -358,11 +360,14 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
       // 0 times an infinity or a NaN of a row that does not see the key is NaN:
       // in stages that some of the workgroup's pairs are hidden in, rows that
       // hold one give NaN to the keys that they see, and zeros to the products.
+      // What products of large values overflow to is taken out the same way.
       uint64_t bad = 0;
+      bool large = false;
       if (__builtin_expect(
               !wg_whole || st.lo_max > wg_first || st.hi_min <= wg_last, 0)) {
         char* at = smem + buf * L::kStage;
-        if (__builtin_expect(tiles_not_finite<D, 2>(at, tid, s_flags), 0)) {
+        if (__builtin_expect(tiles_reach<D, 2, kLarge>(at, tid, s_flags), 0)) {
+          large = true;
           bad = rows_not_finite<D>(at, lane) |
                 rows_not_finite<D>(at + L::kTile, lane);
           lds_barrier();  // every wave has looked
@@ -375,7 +380,7 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
       if (touched) {
         const bool full = wave_whole && st.lo_max <= wave_first &&
                           st.hi_min > wave_last;
-        const bool fix = bad != 0 || (!full && keys_bad);
+        const bool fix = large || (!full && keys_large);
         const float kpos_rel = BIAS ? static_cast<float>(kpos - st.pos) : 0.f;
 #pragma unroll
         for (int qt = 0; qt < 2; ++qt) {
@@ -454,7 +459,7 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
               f32x4 z;
 #pragma unroll
               for (int e = 0; e < 4; ++e) z[e] = y[i * 4 + e];
-              // A hidden pair's product with a NaN of dO V^T is 0.
+              // A hidden pair's product with dO V^T is 0, whatever that is.
               if (__builtin_expect(fix, 0)) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -695,7 +700,8 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
       uint64_t bad = 0;
       if (!all_see) {
         char* at = smem + buf * L::kStage;
-        if (__builtin_expect(tiles_not_finite<D, 1>(at, tid, s_flags), 0)) {
+        if (__builtin_expect(tiles_reach<D, 1, kNotFinite>(at, tid, s_flags),
+                             0)) {
           bad = rows_not_finite<D>(at, lane);
           lds_barrier();  // every wave has looked
           clear_not_finite<D>(at, tid);

@@ -364,8 +364,8 @@ void score_fwd_kernel(ScoreFwdParams p) {
       if (!all_see) {
         char* vt = smem + buf * L::kStage + L::kTile;
         if (__builtin_expect(
-                tiles_not_finite<D, 1>(vt, tid,
-                                       reinterpret_cast<int*>(s_range + 4)),
+                tiles_reach<D, 1, kNotFinite>(
+                    vt, tid, reinterpret_cast<int*>(s_range + 4)),
                 0))
           take_not_finite(k0, vt);
       }

@@ -94,12 +94,17 @@ __device__ __forceinline__ void pipeline_reads() {
   __builtin_amdgcn_sched_group_barrier(0x008, G * AHEAD, 0);
 }
 
-// Whether some of `tiles` staged tiles one after the other hold an infinity or a
-// NaN: every wave looks at a quarter, the answers meet in s_flags.  For all waves
-// of the workgroup together; between two calls lies another barrier.
-template <int D, int tiles>
-__device__ __forceinline__ bool tiles_not_finite(const char* tile, int tid,
-                                                 int* s_flags) {
+// Exponent bits of bf16 values: of infinities and NaN, and of 2^59, below which
+// the sums of 128 products stay below 2^125.
+constexpr uint32_t kNotFinite = 0x7f80, kLarge = 0x5d00;
+
+// Whether some of `tiles` staged tiles one after the other hold a value with the
+// exponent `kFrom` or above: every wave looks at a quarter, the answers meet in
+// s_flags.  For all waves of the workgroup together; between two calls lies another
+// barrier.
+template <int D, int tiles, uint32_t kFrom>
+__device__ __forceinline__ bool tiles_reach(const char* tile, int tid,
+                                            int* s_flags) {
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
   typedef int i32x4v __attribute__((ext_vector_type(4)));
@@ -113,7 +118,7 @@ __device__ __forceinline__ bool tiles_not_finite(const char* tile, int tid,
       top = __builtin_elementwise_max(
           top, __builtin_bit_cast(u16x2, w[j] & 0x7f807f80u));
   }
-  const bool any = __any(top[0] == 0x7f80 || top[1] == 0x7f80);
+  const bool any = __any(top[0] >= kFrom || top[1] >= kFrom);
   if ((tid & 63) == 0) s_flags[tid >> 6] = any;
   lds_barrier();
   const i32x4v f = *reinterpret_cast<const i32x4v*>(s_flags);

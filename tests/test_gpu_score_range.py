@@ -1,5 +1,6 @@
 """Attention under a score rule at the ends of what its arguments may be, on the
-GPU: wide caps."""
+GPU: wide caps, products that
+overflow."""
 
 import numpy as np
 import pytest
@@ -145,3 +146,42 @@ def test_wide_caps_over_the_cache(cap, rows, d, dtype):
     if dtype is torch.bfloat16:
         tol += U * (mass + np.abs(wo))
     assert (np.abs(o - wo) <= tol).all(), (np.abs(o - wo) - tol).max()
+
+
+# -- products that overflow ---------------------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap,slopes", [(0.0, False), (5.0, False),
+                                        (0.0, True), (300.0, True)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_hidden_products_that_overflow_reach_nobody(cap, slopes, d, dtype):
+    """Padding rows and keys that hold finite numbers whose products are
+    infinite, or infinite with both signs: results are those of zeros there."""
+    prob = problem(330, hq=4, hkv=2, d=d)
+    at = np.arange(330)
+    hole = (at % 110) >= 90  # rows and keys of no document
+    lo = at // 110 * 110
+    rule = make_rule(prob, [0], "causal", cap, slopes, 1)
+    rule.update(key_begin=np.where(hole, 0, lo),
+                key_end=np.where(hole, 0, at + 1))
+    q, k, v, do = (x.cuda() for x in tile_inputs(prob, [0], [0], 1))
+    for x in (q, k, v, do):
+        x[hole] = 0
+    dev = on_gpu(rule)
+    o, lse = run_forward(prob, [0], [0], dev, q, k, v, dtype)
+    ob = o.to(torch.bfloat16)
+    grads = run_backward(prob, [0], [0], dev, q, k, v, ob, do, lse, dtype)
+    for large in (1e38, 1e20, 2.0 ** 64):
+        for which in range(5):  # each by itself, then all of them
+            ins = [x.clone() for x in (q, k, v, do)]
+            for i, x in enumerate(ins):
+                if which in (i, 4):
+                    sign = torch.ones(d, device="cuda")
+                    sign[i::3] = -1
+                    x[hole] = (large * sign).to(torch.bfloat16)
+            o2, lse2 = run_forward(prob, [0], [0], dev, *ins[:3], dtype)
+            assert torch.equal(o, o2) and torch.equal(lse, lse2)
+            got = run_backward(prob, [0], [0], dev, *ins[:3], ob, ins[3], lse,
+                               dtype)
+            for a, b in zip(grads, got):
+                assert torch.equal(a, b), (large, which)
