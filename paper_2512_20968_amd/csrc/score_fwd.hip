@@ -252,9 +252,14 @@ void score_fwd_kernel(ScoreFwdParams p) {
                                d0),
                   sc[kt][i]);
         } else {
-          const float d0 = static_cast<float>(int64_t{qpos} - pos0) -
-                           step * (8.f * lh);
-          const float offf = static_cast<float>(off);
+          // A row before or behind all of the block's keys is as far from the
+          // nearest end as `beyond` says: the rest is small enough for a float
+          // (the rows of a wave may be of partitions that lie far apart).
+          const int64_t at = int64_t{qpos} - pos0, end = last - pos0;
+          const int64_t inside = at < 0 ? 0 : at > end ? end : at;
+          const int64_t beyond = at < 0 ? -at : at > end ? at - end : 0;
+          const float d0 = static_cast<float>(inside) - step * (8.f * lh);
+          const float offf = static_cast<float>(off - beyond);
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
 #pragma unroll

@@ -1,6 +1,6 @@
 """Attention under a score rule at the ends of what its arguments may be, on the
-GPU: wide caps, products that
-overflow."""
+GPU: wide caps, positions
+that float32 does not hold, products that overflow."""
 
 import numpy as np
 import pytest
@@ -146,6 +146,32 @@ def test_wide_caps_over_the_cache(cap, rows, d, dtype):
     if dtype is torch.bfloat16:
         tol += U * (mass + np.abs(wo))
     assert (np.abs(o - wo) <= tol).all(), (np.abs(o - wo) - tol).max()
+
+
+# -- positions that float32 does not hold ------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_a_billion_positions_apart(d, dtype):
+    """128 rows of which the first 100 are 2^30 positions before all keys and
+    the others among them: biases of far keys differ by their distances from
+    each other.  The weights' error leaves out what all keys of a row share."""
+    n = 2 ** 30 // 100
+    prob = problem(100, n=n, hq=2, hkv=1, d=d, causal=0)
+    lists = [0, n - 1], [n - 1]
+    q, k, v, _ = (x.cuda() for x in tile_inputs(prob, *lists, 2))
+    rule = dict(slopes=np.float32([0.5, 0.03]))
+    want = Bounds(prob, *lists, rule, q, k, v)
+    qpos, kpos = (os_.positions(prob, x) for x in lists)
+    far = np.abs(qpos[:, None] - kpos[None, :]).min(1)
+    near = 4 * E * rule["slopes"][:, None].astype(float) * far
+    want.err = want.err - near
+    o, lse = run_forward(prob, *lists, on_gpu(rule), q, k, v, dtype)
+    tol = 2 * want.err.T[:, :, None] * want.a + 16 * E * want.a
+    if dtype is torch.bfloat16:
+        tol += U * (want.a + np.abs(want.o))
+    assert (np.abs(np64(o) - want.o) <= 1.1 * tol).all()
+    assert (np.abs(np64(lse) - want.lse) <= 1.1 * (want.err + near)).all()
 
 
 # -- products that overflow ---------------------------------------------------
