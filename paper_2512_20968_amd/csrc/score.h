@@ -54,7 +54,9 @@ static_assert(sizeof(ScoreFwdParams) <= 4096, "kernel arguments");
 // = 0: there is none), and what all of them see.
 struct ScoreStage {
   int32_t lo_min, hi_max, lo_max, hi_min;
-  int32_t pos, pad[3];  // its first row's position
+  int32_t pos;   // its first row's position
+  int32_t wide;  // rows of far partitions: pos_rel are integers
+  int32_t pad[2];
 };
 
 struct ScoreBwdParams {
@@ -70,7 +72,9 @@ struct ScoreBwdParams {
   int32_t* lo;    // [rows_pad]: a row's begin, end and position
   int32_t* hi;
   int32_t* pos;
-  float* pos_rel;      // position less that of the stage's first row
+  // Position less that of the stage's first row, as an integer's bits where one of
+  // them is 2^23 or more.
+  float* pos_rel;
   ScoreStage* stages;  // [rows_pad / 64]
   // Partial dK, dV of 128 keys whose stages are cut into parts of about
   // part_stages, at most kv_splits of them: [part][rows_kv][hkv][d]; how many there

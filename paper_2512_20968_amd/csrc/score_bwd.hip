@@ -66,7 +66,9 @@ __global__ __launch_bounds__(NT) void score_prep_kernel(ScoreBwdParams p,
     p.pos[my] = pos;
     ScoreStage g;
     g.pos = __builtin_amdgcn_readfirstlane(pos);
-    p.pos_rel[my] = static_cast<float>(pos - g.pos);
+    const int rel = pos - g.pos;
+    g.wide = wave_max(abs(rel)) >= 1 << 23;
+    p.pos_rel[my] = g.wide ? __int_as_float(rel) : static_cast<float>(rel);
     const bool some = s.lo < s.hi;
     g.lo_min = wave_min(some ? s.lo : INT32_MAX);
     g.hi_max = wave_max(s.hi);
@@ -381,7 +383,8 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
         const bool full = wave_whole && st.lo_max <= wave_first &&
                           st.hi_min > wave_last;
         const bool fix = large || (!full && keys_large);
-        const float kpos_rel = BIAS ? static_cast<float>(kpos - st.pos) : 0.f;
+        const float kpos_rel =
+            BIAS && !st.wide ? static_cast<float>(kpos - st.pos) : 0.f;
 #pragma unroll
         for (int qt = 0; qt < 2; ++qt) {
           auto product = [&](const bf16x8 (&f)[D / 16], int tile, f32x16 z) {
@@ -422,7 +425,17 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
                 if (kpos < lo[e] || kpos >= hi[e]) lse[e] = INFINITY;
             }
             f32x4 e4, g4, pos;
-            if (BIAS) pos = lds_four<f32x4>(at + 1024);
+            if (BIAS) {
+              pos = lds_four<f32x4>(at + 1024);
+              if (__builtin_expect(st.wide, 0)) {
+                // In 32 bits: what wraps is not seen.
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  pos[e] = static_cast<float>(static_cast<int>(
+                      __float_as_uint(pos[e]) -
+                      static_cast<uint32_t>(kpos - st.pos)));
+              }
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float far = BIAS ? fabsf(pos[e] - kpos_rel) : 0.f;
@@ -747,9 +760,10 @@ __device__ __forceinline__ void dq_item(const ScoreBwdParams& p, char* smem,
 }
 
 // Both passes in one launch: the dK/dV items first, the longest of a causal tile
-// at their front, and dQ items wherever one of them ends.
+// at their front, and dQ items wherever one of them ends.  (A wide cap's tanh and a
+// bias beside each other take 179 registers at head dim 64: two workgroups.)
 template <int D, int CAP, bool BIAS, bool OUT_F32>
-__global__ __launch_bounds__(NT, D == 128 ? 2 : 3)
+__global__ __launch_bounds__(NT, D == 128 || CAP == kFineCap ? 2 : 3)
 void score_bwd_kernel(ScoreBwdParams p) {
   extern __shared__ __align__(16) char smem[];
   const int id = blockIdx.x;

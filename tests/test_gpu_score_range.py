@@ -174,6 +174,27 @@ def test_rows_a_billion_positions_apart(d, dtype):
     assert (np.abs(np64(lse) - want.lse) <= 1.1 * (want.err + near)).all()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 6.0])
+def test_gradients_of_rows_a_billion_positions_apart(d, cap):
+    """Partitions of 100 rows at both ends of 2^30 positions: rows 64 .. 127 are
+    of both, and the later ones see keys beside them."""
+    n = 2 ** 30 // 100
+    prob = problem(100, n=n, hq=2, hkv=1, d=d)
+    lists = [0, n - 1], [n - 1, 0]
+    q, k, v, do = (x.cuda() for x in tile_inputs(prob, *lists, 2))
+    qpos = os_.positions(prob, lists[0])
+    rule = dict(slopes=np.float32([0.5, 0.03]), key_begin=qpos // 100 * 100)
+    if cap:
+        rule["cap"] = cap
+    want = Bounds(prob, *lists, rule, q, k, v)
+    dev = on_gpu(rule)
+    o, lse = run_forward(prob, *lists, dev, q, k, v)
+    want.check_forward(o, lse, False)
+    grads = run_backward(prob, *lists, dev, q, k, v, o, do, lse)
+    want.check_backward(o, lse, do, *grads)
+
+
 # -- products that overflow ---------------------------------------------------
 
 @pytest.mark.parametrize("d", [64, 128])
