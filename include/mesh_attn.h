@@ -610,7 +610,8 @@ size_t mesh_attn_score_fwd_workspace_size(const ma_problem_t* prob, int32_t nq,
  *                  device; strides in elements, multiples of 8, at least heads
  *                  * head_dim, at most 2^24 (slices of a fused projection);
  *   lists          at most MA_SCORE_MAX_LIST partitions each; (rows + 63) times
- *                  heads at most 2^27, heads at most 65535.
+ *                  heads at most 2^27, heads at most 65535; with slopes and
+ *                  striped partitions, at most 2^18 of those.
  *   o              [nq*P][Hq][d] dense, bf16 or float32.  The probabilities
  *                  enter the second product in bf16 for a bf16 O, and as a sum
  *                  of three bf16 for a float32 O (a partial to be merged).

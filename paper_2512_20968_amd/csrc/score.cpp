@@ -124,6 +124,12 @@ ma_status_t check_tile(const ma_problem_t* prob, const int32_t* q_idx,
   MA_TRY(check_indices("q_idx", q_idx, nq, prob->num_partitions));
   MA_TRY(check_indices("kv_idx", kv_idx, nkv, prob->num_partitions));
   MA_TRY(check_score(score, prob->softmax_scale));
+  // The kernels take the distances within a block of 64 keys in float32.
+  if (score && score->slopes && prob->layout == MA_LAYOUT_STRIPED &&
+      prob->num_partitions > 1 << 18)
+    return fail(MA_ERR_UNSUPPORTED,
+                "slopes with %d striped partitions, above 2^18",
+                prob->num_partitions);
   const int64_t d = prob->head_dim;
   MA_TRY(check_row_stride("q_stride", q_stride, prob->num_q_heads * d));
   MA_TRY(check_row_stride("k_stride", k_stride, prob->num_kv_heads * d));

@@ -195,6 +195,26 @@ def test_gradients_of_rows_a_billion_positions_apart(d, cap):
     want.check_backward(o, lse, do, *grads)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 6.0])
+def test_most_striped_partitions_with_a_bias(d, cap):
+    """Rows and keys almost 2^18 positions apart, each beside a key of another partition:
+    the nearest one's bias is exact."""
+    n = 2 ** 18 - 3
+    prob = problem(200, n=n, hq=2, hkv=1, d=d, causal=0, layout=1)
+    lists = [5, n - 1], [7, n - 4]
+    q, k, v, do = (x.cuda() for x in tile_inputs(prob, *lists, 2))
+    rule = dict(slopes=np.float32([0.5, 2.0 ** -18]))
+    if cap:
+        rule["cap"] = cap
+    want = Bounds(prob, *lists, rule, q, k, v)
+    dev = on_gpu(rule)
+    o, lse = run_forward(prob, *lists, dev, q, k, v)
+    want.check_forward(o, lse, False)
+    grads = run_backward(prob, *lists, dev, q, k, v, o, do, lse)
+    want.check_backward(o, lse, do, *grads)
+
+
 # -- products that overflow ---------------------------------------------------
 
 @pytest.mark.parametrize("d", [64, 128])

@@ -22,3 +22,22 @@ def test_caps(call):
     # The largest one passes: refused for what is checked after it.
     assert call(score=_score(cap=2.0 ** 100), qs=255) == b.MA_ERR_INVALID_ARG
     assert "q_stride" in ma.mesh_attn_last_error()
+
+
+@pytest.mark.parametrize("call", [_fwd, _bwd])
+def test_slopes_of_very_many_striped_partitions(call):
+    """Positions of 64 rows of a partition span 64 n: more than 2^24 of them is
+    more than a float32 holds.  Contiguous partitions, and rules without a bias,
+    have no such limit."""
+    for n, kw, status in ((2 ** 18 + 1, {}, b.MA_ERR_UNSUPPORTED),
+                          (2 ** 20, {}, b.MA_ERR_UNSUPPORTED),
+                          (2 ** 18, {}, b.MA_ERR_INVALID_ARG),
+                          (2 ** 20, dict(layout=0), b.MA_ERR_INVALID_ARG)):
+        prob = _prob(num_partitions=n, **dict(dict(layout=1), **kw))
+        # (An odd stride: refused after the check in question.)
+        assert call(prob=prob, score=_score(slopes=0x100000), qs=255) == status
+        assert ("2^18" in ma.mesh_attn_last_error()) == (
+            status == b.MA_ERR_UNSUPPORTED)
+    prob = _prob(num_partitions=2 ** 20, layout=1)
+    assert call(prob=prob, score=_score(cap=1.0),
+                qs=255) == b.MA_ERR_INVALID_ARG
