@@ -273,6 +273,10 @@ __device__ __forceinline__ float capped(const CacheFwdParams& p, float v,
   return fabsf(u) < 0.4f ? fmaf(t, 0.5f * p.cap_two, add) : y;
 }
 
+// Most positions from one stored key to the next for which the bias of a step is
+// taken term by term: 2^-24 of 7 of them is below 2^-14, for slopes up to one.
+constexpr int kNearSteps = 128;
+
 template <int NQ, bool EXACT>
 __device__ __forceinline__ void rule_step(const CacheFwdParams& p,
                                           const RuleState<NQ>& rs,
@@ -285,8 +289,10 @@ __device__ __forceinline__ void rule_step(const CacheFwdParams& p,
     return static_cast<int>(static_cast<uint32_t>(rs.qpos[q]) -
                             static_cast<uint32_t>(k0));
   };
-  // All keys before all rows: one more term per score.
-  const bool before = p.slopes && kb + kStep <= rs.before;
+  // All keys before all rows: one more term per score.  (What the terms of eight
+  // keys cancel is 2^-24 of 7 steps' bias: too much where keys lie far apart.)
+  const bool before =
+      p.slopes && kb + kStep <= rs.before && step <= kNearSteps;
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
     const float add =

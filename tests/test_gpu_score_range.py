@@ -215,6 +215,22 @@ def test_most_striped_partitions_with_a_bias(d, cap):
     want.check_backward(o, lse, do, *grads)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_cache_of_a_million_partitions(dtype):
+    """Stored keys 2^20 positions apart, the rows right behind the last one: the
+    nearest key's bias is exact."""
+    n = 2 ** 20
+    c = cache_of(num_pages=40, max_pages=20, num_partitions=n, partition=n - 1)
+    rule = dict(slopes=np.float32([0.5, 0.3, 0.2, 2.0 ** -20]))
+    o, lse, wo, wl, mass, err = one_request(c, 3, 192 * n + 3, rule, 2, dtype)
+    err = err + 2.0 ** -14
+    assert (np.abs(lse - wl) <= err + 8 * E * np.abs(wl)).all()
+    tol = 2 * mass * err.T[:, :, None]
+    if dtype is torch.bfloat16:
+        tol += U * (mass + np.abs(wo))
+    assert (np.abs(o - wo) <= tol).all()
+
+
 # -- products that overflow ---------------------------------------------------
 
 @pytest.mark.parametrize("d", [64, 128])
