@@ -149,31 +149,33 @@ class Rope(ctypes.Structure):
 
 
 class Score(ctypes.Structure):
-    """ma_score_t.  ``Score.make`` takes a mapping with any of the field names:
-    a float and GPU tensors (``slopes`` float32 [heads]; ``key_begin``,
-    ``key_end`` int32 [rows]), which the structure keeps alive."""
+    """ma_score_t: a float and GPU tensors (``slopes`` float32 [heads];
+    ``key_begin``, ``key_end`` int32 [rows]), which the structure keeps alive.
+    ``Score.make`` takes a mapping with any of the field names."""
     _fields_ = [("cap", ctypes.c_float),
                 ("slopes", ctypes.c_void_p),
                 ("key_begin", ctypes.c_void_p),
                 ("key_end", ctypes.c_void_p)]
-    tensors = (None, None, None)
+    ARRAYS = ("slopes", "key_begin", "key_end")
+
+    def __init__(self, cap=0.0, slopes=None, key_begin=None, key_end=None):
+        self.tensors = (slopes, key_begin, key_end)
+        for t in self.tensors:
+            if t is not None and not isinstance(t, _torch().Tensor):
+                raise TypeError("a score rule's arrays must be torch.Tensors")
+        super().__init__(float(cap), *(None if t is None else t.data_ptr()
+                                       for t in self.tensors))
 
     @classmethod
     def make(cls, score):
         if isinstance(score, Score):
             return score
         score = dict(score or {})
-        cap = float(score.pop("cap", 0.0))
-        ts = tuple(score.pop(n, None)
-                   for n in ("slopes", "key_begin", "key_end"))
-        if score:
-            raise ValueError(f"unknown fields of a score rule: {sorted(score)}")
-        for t in ts:
-            if t is not None and not isinstance(t, _torch().Tensor):
-                raise TypeError("a score rule's arrays must be torch.Tensors")
-        self = cls(cap, *(None if t is None else t.data_ptr() for t in ts))
-        self.tensors = ts
-        return self
+        unknown = set(score) - {"cap", *cls.ARRAYS}
+        if unknown:
+            raise ValueError(
+                f"unknown fields of a score rule: {sorted(unknown)}")
+        return cls(**score)
 
 
 _i32 = ctypes.c_int32
@@ -868,6 +870,10 @@ def _score_args(score, rows, hq, dev):
     """The rule, its tensors checked against the call's rows and heads."""
     s, t = Score.make(score), _torch_module
     slopes, begin, end = s.tensors
+    for name, x in zip(s.ARRAYS, s.tensors):
+        # (A pointer set by hand: nothing says what is there.)
+        if getattr(s, name) != (None if x is None else x.data_ptr() or None):
+            raise ValueError(f"{name} of a score rule must come as a tensor")
     if slopes is not None:
         _arg(slopes, "slopes", (hq,), t.float32, dev)
     if begin is not None:

@@ -2,6 +2,7 @@
 the CPU."""
 
 import pytest
+import torch
 
 import paper_2512_20968_amd as ma
 from paper_2512_20968_amd import _binding as b
@@ -41,3 +42,31 @@ def test_slopes_of_very_many_striped_partitions(call):
     prob = _prob(num_partitions=2 ** 20, layout=1)
     assert call(prob=prob, score=_score(cap=1.0),
                 qs=255) == b.MA_ERR_INVALID_ARG
+
+
+def test_a_rule_from_tensors():
+    """The structure's own constructor takes what a mapping holds, keeps the
+    tensors alive, and has them checked by the calls."""
+    slopes, begin = torch.ones(4), torch.zeros(10, dtype=torch.int32)
+    rule = ma.Score(cap=30.0, slopes=slopes, key_begin=begin, key_end=None)
+    assert rule.cap == 30.0 and rule.slopes == slopes.data_ptr()
+    assert rule.key_begin == begin.data_ptr() and rule.key_end is None
+    assert rule.tensors[0] is slopes and rule.tensors[1] is begin
+    assert ma.Score.make(rule) is rule
+    same = ma.Score.make(dict(cap=30.0, slopes=slopes, key_begin=begin))
+    assert bytes(same) == bytes(rule)
+    assert ma.Score().cap == 0.0
+    with pytest.raises(TypeError, match="torch.Tensors"):
+        ma.Score(slopes=[1.0])
+    with pytest.raises(TypeError, match="torch.Tensors"):
+        ma.Score(1.0, slopes.data_ptr())
+    with pytest.raises(TypeError):
+        ma.Score(window=3)
+
+
+def test_pointers_set_by_hand_are_refused():
+    rule = ma.Score(cap=1.0)
+    rule.key_end = 0x100000
+    with pytest.raises(ValueError, match="key_end of a score rule must come"):
+        b._score_args(rule, 10, 4, 0)
+    assert b._score_args(ma.Score(cap=1.0), 10, 4, 0).cap == 1.0
