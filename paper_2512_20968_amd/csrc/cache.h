@@ -87,7 +87,10 @@ hipError_t launch_cache_read(const LoadParams& p, hipStream_t stream);
 // `parts` runs from `start` on (0: none).
 struct CacheFold {
   int32_t first, rr0, rr_end, kvh, parts, start;
-  int32_t from, local;  // under a score rule: the request's stored keys
+};
+// Its request's stored keys, under a score rule.
+struct CacheFoldKeys {
+  int32_t from, local;
 };
 
 struct CacheFwdParams {
@@ -120,6 +123,7 @@ struct CacheFwdParams {
   const int32_t* key_begin;
   const int32_t* key_end;
   CacheFold* fold;           // [workgroup][2]: goes on in its run, starts in it
+  CacheFoldKeys* fold_keys;  // [workgroup][2]
   float* part_o;             // [2 * workgroups][rows of a tile][d]
   float* part_ml;            // .. [2]: reference (log2 units) and sum
 };

@@ -1218,15 +1218,13 @@ void cache_fwd_kernel(CacheFwdParams p) {
       f.rr0 = it.rr0;
       f.rr_end = it.rr_end;
       f.kvh = it.kvh;
-      if (RULE) {
-        f.from = it.from;
-        f.local = it.local;
-      }
       f.start = goes_on ? (per * run - it.u0) / per : run;
       const int more_runs = goes_on ? (it.nu - it.u0 - 1) / per
                                     : (it.nu - it.u1 + per - 1) / per;
       f.parts = min(run + more_runs, int(gridDim.x) - 1) - f.start + 1;
       p.fold[2 * run + (goes_on ? 0 : 1)] = f;
+      if (RULE)
+        p.fold_keys[2 * run + (goes_on ? 0 : 1)] = {it.from, it.local};
     }
     prev = it;
     have_prev = true;
@@ -1254,6 +1252,8 @@ void cache_fold_kernel(CacheFwdParams p) {
   for (int which = 0; which < 2; ++which) {
     const CacheFold f = load_const(p.fold, 2 * run + which);
     if (f.parts < 2) continue;
+    CacheFoldKeys keys = {0, 0};
+    if (RULE) keys = load_const(p.fold_keys, 2 * run + which);
     // Rows of a slice; more than one run, so they are half of all at most.
     int n = kRows / 2;
     while (n > 1 && kRows / n * 2 <= f.parts) n /= 2;
@@ -1307,8 +1307,8 @@ void cache_fold_kernel(CacheFwdParams p) {
     }
     if (pg == 0 && valid) {
       const TokenHead th = token_head(p, rr, f.kvh);
-      store_row<D, OUT_F32, RULE>(p, f.first + th.tok, th.head, f.from,
-                                  f.local, dim0, acc,
+      store_row<D, OUT_F32, RULE>(p, f.first + th.tok, th.head, keys.from,
+                                  keys.local, dim0, acc,
                                   M == -INFINITY ? 0.f : M, L);
     }
     __syncthreads();
@@ -1424,9 +1424,11 @@ Shape shape_of(const CacheDims& c, int32_t hq, int32_t num_requests,
   return s;
 }
 
-// Workspace of a cut launch of `groups` workgroups: two CacheFold of each, then the
-// partial results: O, reference and sum of two tiles each.
-size_t fold_bytes(int groups) { return 2 * sizeof(CacheFold) * groups; }
+// Workspace of a cut launch of `groups` workgroups: two CacheFold of each, then two
+// CacheFoldKeys, then the partial results: O, reference and sum of two tiles each.
+size_t fold_bytes(int groups) {
+  return 2 * (sizeof(CacheFold) + sizeof(CacheFoldKeys)) * groups;
+}
 size_t part_rows(int groups, int nq) { return size_t{32} * nq * groups; }
 
 template <int D, int NQ, bool OUT_F32, bool RULE, bool OWN>
@@ -1511,9 +1513,11 @@ hipError_t launch_cache_fwd(const CacheFwdParams& params, bool out_f32, void* ws
   p.group_mul = static_cast<uint32_t>(
       ((uint64_t{1} << p.group_shift) + p.group - 1) / p.group);
   p.fold = nullptr;
+  p.fold_keys = nullptr;
   p.part_o = p.part_ml = nullptr;
   if (s.cut) {
     p.fold = static_cast<CacheFold*>(ws);
+    p.fold_keys = reinterpret_cast<CacheFoldKeys*>(p.fold + 2 * s.cut_grid);
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) +
                                         fold_bytes(s.cut_grid));
     p.part_ml = p.part_o + part_rows(s.cut_grid, s.nq) * p.c.d;
