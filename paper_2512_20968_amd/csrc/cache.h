@@ -116,7 +116,8 @@ struct CacheFwdParams {
   int32_t seq_units;  // units that a sequence costs beside its keys
   int32_t max_units;  // most of a launch
   // The score rule (rule = 1): cap_two = 2 cap log2(e), 0 without a cap; a
-  // product times cap_in is log2(e^(2u)), times cap_u u = score / cap.
+  // product times cap_in is log2(e^(2u)), times cap_u u = score / cap; wide_cap: the
+  // kernels that take small arguments from the tanh's series.
   int32_t rule, wide_cap;
   float cap_in, cap_two, cap_u;
   const float* slopes;

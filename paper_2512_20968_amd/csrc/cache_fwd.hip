@@ -277,7 +277,7 @@ __device__ __forceinline__ float capped(const CacheFwdParams& p, float v,
 // taken term by term: 2^-24 of 7 of them is below 2^-14, for slopes up to one.
 constexpr int kNearSteps = 128;
 
-template <int NQ, bool EXACT>
+template <int NQ, bool FINE>
 __device__ __forceinline__ void rule_step(const CacheFwdParams& p,
                                           const RuleState<NQ>& rs,
                                           f32x4 (&x)[NQ][2], int kb, int g) {
@@ -297,14 +297,10 @@ __device__ __forceinline__ void rule_step(const CacheFwdParams& p,
   for (int q = 0; q < NQ; ++q) {
     const float add =
         before ? -rs.slope[q] * static_cast<float>(behind(q) - rs.off[q]) : 0.f;
-    if (p.cap_two > 0.f && (EXACT || p.wide_cap)) {
+    if (p.cap_two > 0.f) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        x[q][i >> 2][i & 3] = capped<true>(p, x[q][i >> 2][i & 3], add);
-    } else if (p.cap_two > 0.f) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x[q][i >> 2][i & 3] = capped<false>(p, x[q][i >> 2][i & 3], add);
+        x[q][i >> 2][i & 3] = capped<FINE>(p, x[q][i >> 2][i & 3], add);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -877,8 +873,10 @@ __device__ __forceinline__ Item locate(const CacheFwdParams& p, bool split,
 }
 
 // OWN: every wave has items of its own, whole sequences, and nothing to fold.
-// RULE: scores under a rule (mesh_attn_cache_score_fwd).
-template <int D, int NQ, bool OUT_F32, bool P16, bool OWN, bool RULE>
+// RULE: scores under a rule (mesh_attn_cache_score_fwd).  FINE: the tanh of small
+// arguments by its series (a float32 O, and wide caps: as a branch of the step it
+// took 2 % of a chunk under a usual cap at head dim 128, 6 % at 64).
+template <int D, int NQ, bool OUT_F32, bool P16, bool OWN, bool RULE, bool FINE>
 __global__ __launch_bounds__(NT, (kWavesPerSimd<D, NQ>))
 void cache_fwd_kernel(CacheFwdParams p) {
   constexpr int kRows = 16 * NQ;
@@ -1169,7 +1167,7 @@ void cache_fwd_kernel(CacheFwdParams p) {
         if (more_keys) load_k<D, P16>(h, pn, next, r, &s);
         u32x2 vs = s.vs;
         const bool ok = lane_ok<P16>(h, pg, g);
-        if constexpr (RULE) rule_step<NQ, OUT_F32>(p, rs, x, kb, g);
+        if constexpr (RULE) rule_step<NQ, FINE>(p, rs, x, kb, g);
         if (kb + kStep > all_see || (RULE && kb < all_from) || !__all(ok))
           vs = mask_step<D, NQ, RULE>(st, rs, x, s, ok, kb, h.local, g);
         finish_step<D, NQ, OUT_F32, RULE>(st, rs, x, s,
@@ -1251,9 +1249,9 @@ void cache_fold_kernel(CacheFwdParams p) {
 #pragma unroll 1
   for (int which = 0; which < 2; ++which) {
     const CacheFold f = load_const(p.fold, 2 * run + which);
-    if (f.parts < 2) continue;
-    CacheFoldKeys keys = {0, 0};
+    CacheFoldKeys keys = {0, 0};  // (of no use without a sequence)
     if (RULE) keys = load_const(p.fold_keys, 2 * run + which);
+    if (f.parts < 2) continue;
     // Rows of a slice; more than one run, so they are half of all at most.
     int n = kRows / 2;
     while (n > 1 && kRows / n * 2 <= f.parts) n /= 2;
@@ -1431,21 +1429,21 @@ size_t fold_bytes(int groups) {
 }
 size_t part_rows(int groups, int nq) { return size_t{32} * nq * groups; }
 
-template <int D, int NQ, bool OUT_F32, bool RULE, bool OWN>
+template <int D, int NQ, bool OUT_F32, bool RULE, bool OWN, bool FINE>
 hipError_t launch_fwd(const CacheFwdParams& p, int groups, hipStream_t stream) {
   const size_t n = static_cast<size_t>(p.num_requests);
   const size_t lds =
       (n + 1) * 4 + (n <= kKeptRequests ? n * sizeof(Request<RULE>) : 0);
-  const auto kernel = p.c.page_log2 == 4
-                          ? cache_fwd_kernel<D, NQ, OUT_F32, true, OWN, RULE>
-                          : cache_fwd_kernel<D, NQ, OUT_F32, false, OWN,
-                                             RULE>;
+  const auto kernel =
+      p.c.page_log2 == 4
+          ? cache_fwd_kernel<D, NQ, OUT_F32, true, OWN, RULE, FINE>
+          : cache_fwd_kernel<D, NQ, OUT_F32, false, OWN, RULE, FINE>;
   hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(groups)), dim3(NT), lds,
                      stream, p);
   return hipGetLastError();
 }
 
-template <int D, int NQ, bool OUT_F32, bool RULE>
+template <int D, int NQ, bool OUT_F32, bool RULE, bool FINE = OUT_F32>
 hipError_t launch(CacheFwdParams p, const Shape& s, hipStream_t stream) {
   hipError_t e = hipSuccess;
   p.split = 0;
@@ -1453,15 +1451,15 @@ hipError_t launch(CacheFwdParams p, const Shape& s, hipStream_t stream) {
   p.most_keys = INT32_MAX;
   if (s.own_keys >= 0) {
     if (s.cut) p.most_keys = s.own_keys;
-    e = launch_fwd<D, NQ, OUT_F32, RULE, true>(p, s.own_grid, stream);
+    e = launch_fwd<D, NQ, OUT_F32, RULE, true, FINE>(p, s.own_grid, stream);
     if (e != hipSuccess || !s.cut) return e;
     p.least_keys = s.own_keys + 1;
     p.most_keys = INT32_MAX;
   }
   if (!s.cut)
-    return launch_fwd<D, NQ, OUT_F32, RULE, false>(p, s.whole_grid, stream);
+    return launch_fwd<D, NQ, OUT_F32, RULE, false, FINE>(p, s.whole_grid, stream);
   p.split = 1;
-  e = launch_fwd<D, NQ, OUT_F32, RULE, false>(p, s.cut_grid, stream);
+  e = launch_fwd<D, NQ, OUT_F32, RULE, false, FINE>(p, s.cut_grid, stream);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((cache_fold_kernel<D, NQ, OUT_F32, RULE>),
                      dim3(static_cast<unsigned>(s.cut_grid)),
@@ -1472,6 +1470,15 @@ hipError_t launch(CacheFwdParams p, const Shape& s, hipStream_t stream) {
 template <int D, bool RULE>
 hipError_t launch_d(const CacheFwdParams& p, const Shape& s, bool out_f32,
                     hipStream_t stream) {
+  if constexpr (RULE) {
+    if (p.wide_cap && !out_f32) {
+      if constexpr (D == 64) {
+        if (s.nq == 4) return launch<D, 4, false, true, true>(p, s, stream);
+      }
+      return s.nq == 2 ? launch<D, 2, false, true, true>(p, s, stream)
+                       : launch<D, 1, false, true, true>(p, s, stream);
+    }
+  }
   if constexpr (!RULE || D == 64) {
     if (s.nq == 4) return launch<D, 4, false, RULE>(p, s, stream);
   }
