@@ -581,7 +581,14 @@ ma_status_t mesh_attn_rope(const ma_rope_t* rope, int64_t rows,
  * A row that sees none has O = 0 and LSE = -inf, whatever is in Q, K and V.
  * Documents packed one after the other: begin and end of the row's document (end
  * p_i + 1 if causal); a prefix that all of its document's rows see: end at least
- * the prefix's; a window of w: begin at least p_i - w + 1; padding: begin = end.
+ * the prefix's; a window of w: begin at least p_i - w + 1; padding: begin = end =
+ * 0.
+ *
+ * Capped scores are off by 2^-23 of the cap up to a cap of 256 (a bf16 O and the
+ * gradients), by 2^-19 of themselves under a wider one and for a float32 O;
+ * 1 - tanh^2 in the gradients by 2^-21 of one.  Biases count from the row's
+ * nearest key, whose own is left to the LSE: a float32, 2^-24 of its size, which
+ * the backward's probabilities are then off by.
  * ------------------------------------------------------------------------- */
 typedef struct {
   float cap;                /* 0: none; else > 0, at most 2^100              */
@@ -662,8 +669,13 @@ ma_status_t mesh_attn_score_bwd(const ma_problem_t* prob, const int32_t* q_idx,
  * at position p_r = positions[r] sees the stored keys at positions in
  * [key_begin[r], key_end[r]) (without a key_end: up to its own) that lie below
  * lens[b]; a NULL score is no rule.  No row of a request sees keys before the
- * key_begin of the request's first row: they are not read, so that a window
- * costs what it holds.  The workspace is that of mesh_attn_cache_fwd. */
+ * key_begin of the request's first row (the least of the request's, then; 0 for
+ * padding in front): they are not read.  A single token's window so costs what it
+ * holds; each tile of a chunk's rows goes over the stored keys from there on, and
+ * masks those that its own rows do not see.  Under a cap of 34 to 51 a row's sums
+ * hold weights of up to 2^40 before they are divided: stored values of V times the
+ * number of keys have to stay below 2^87, elsewhere below 2^119.  The workspace is
+ * that of mesh_attn_cache_fwd. */
 size_t mesh_attn_cache_score_fwd_workspace_size(const ma_cache_t* cache,
                                                 int32_t num_q_heads,
                                                 int32_t num_requests,

@@ -974,7 +974,8 @@ def mesh_attn_cache_score_fwd(cache, softmax_scale, score, q, positions, cu_new,
                               stream=None):
     """``mesh_attn_cache_fwd`` under a score rule, whose ``key_begin`` and
     ``key_end`` are indexed by the query rows; keys before the ``key_begin`` of
-    a request's first row are seen by none of its rows."""
+    a request's first row are seen by none of its rows (padding in front of a
+    request: 0 and 0)."""
     dev, torch = _device_index(stream, q, "q"), _torch_module
     c, i32 = Cache.make(cache), torch.int32
     if q.dim() != 3:

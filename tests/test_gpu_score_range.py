@@ -1,6 +1,6 @@
 """Attention under a score rule at the ends of what its arguments may be, on the
-GPU: wide caps, positions
-that float32 does not hold, products that overflow."""
+GPU: wide caps, positions that float32 does not hold, products that overflow,
+padding in front of a request."""
 
 import numpy as np
 import pytest
@@ -268,3 +268,21 @@ def test_hidden_products_that_overflow_reach_nobody(cap, slopes, d, dtype):
                                dtype)
             for a, b in zip(grads, got):
                 assert torch.equal(a, b), (large, which)
+
+
+# -- padding in front ---------------------------------------------------------
+
+@pytest.mark.parametrize("window", [0, 40])
+def test_padding_in_front_of_a_request(window):
+    """Rows with begin = end = 0 in front: the rows behind them have the results
+    that they have without them."""
+    c = cache_of(num_pages=40, max_pages=20)
+    b = Scored(c, [300], [30], {})
+    begin = np.maximum(b.positions - window + 1, 0) if window else (
+        b.positions * 0)
+    end = b.positions + 1
+    begin[:7] = end[:7] = 0
+    b.rule = dict(cap=4.0, key_begin=begin, key_end=end)
+    b.check(b.run())
+    o, lse = b.run()
+    assert (o[:7] == 0).all() and torch.isneginf(lse[:, :7]).all()
