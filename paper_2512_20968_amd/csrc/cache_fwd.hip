@@ -25,8 +25,8 @@
 // request's units begin at the first key that its rows see.  64 requests seen
 // through windows of 4096 tokens, 8 KV heads of 4 query heads, head dim 128: 37 us,
 // 3.1 TB/s, by the round trips of 512 sequences of 4 steps; 2 x 1000 rows over 16500
-// keys with cap and bias 970 to 1007 us, 0.53 PFLOP/s, by the vector unit (busy 0.74
-// of the time, the matrix unit 0.21): tiles of 32 rows (a row's range, position and
+// keys with cap and bias 971 to 984 us, 0.53 PFLOP/s, by the vector unit (busy 0.73
+// of the time, the matrix unit 0.22): tiles of 32 rows (a row's range, position and
 // slope do not fit beside 64), twice the conversions, and a reciprocal and two
 // exponentials per score.
 //
@@ -1118,9 +1118,9 @@ void cache_fwd_kernel(CacheFwdParams p) {
       st.neg_ref[q] = st.l[q] = 0.f;
       if (RULE) rs.rounded[q] = 0.f;
       // Under a moderate cap, with a bias that falls, the largest probability
-      // lies between 2^-kLow and 2^40 around a fixed reference, and what a bias
-      // leaves of others is a normal number down to 2^-21 of it.  (A float32 O's
-      // third parts are 2^16 smaller.)
+      // lies between 2^-kLow and 2^40 around a fixed reference (1, where twice the
+      // cap fits in kLow), and what a bias leaves of others is a normal number down
+      // to 2^-21 of it.  (A float32 O's third parts are 2^16 smaller.)
       constexpr float kLow = OUT_F32 ? 100.f : 105.f;
       if (RULE && p.cap_two > 0.f && p.cap_two <= kLow + 40.f &&
           !(rs.slope[q] < 0.f) && sure) {

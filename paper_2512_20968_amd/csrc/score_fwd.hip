@@ -18,8 +18,9 @@
 // score beside the softmax's own.  Rows of a wave, 32: a range, a position and a
 // slope per row are held beside O and Q, and two workgroups share a compute unit so
 // that one's products run beside the other's exponentials.  Documents packed into
-// 8192 rows 155 to 160 us, 0.5 PFLOP/s, by blocks that hold a border and the round
-// trips at an item's start; 77 rows 9 us, all round trips.
+// 8192 rows 155 to 160 us, 0.5 PFLOP/s, by an uneven load (items come from the last
+// rows on, not longest first) and the round trips at an item's start; 77 rows 9 us,
+// all round trips.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
