@@ -647,8 +647,7 @@ size_t mesh_attn_score_bwd_workspace_size(const ma_problem_t* prob, int32_t nq,
  *   dq          [nq*P][Hq][d];  dk, dv [nkv*P][Hkv][d], dense, grad_dtype: the
  *               float32 sums themselves (partials of several GPUs to be added)
  *               or rounded once to bf16.  As in mesh_attn_tile_bwd, P and dS enter
- *               the products in bf16 either way, off by 2^-8 of each at most (dS
- *               of dK at head dim 128 twice that).
+ *               the products in bf16 either way, off by 2^-8 of each at most.
  * Rows that see no key have dQ = 0 and give nothing to dK, dV; a NaN or an
  * infinity of a pair that is seen gives NaN to its row's dQ and its key's dK or dV
  * and to no other.  Deterministic (no atomics); may be captured. */

@@ -21,7 +21,7 @@
 // Bound by the matrix and the vector unit together (8192 causal rows of 32/8 heads
 // of 128, matrix unit busy 47 % of the time, vector unit 56 %): with a cap 2024 to
 // 2150 us, 0.64 to 0.68 PFLOP/s of the five products, 0.90 to 0.95 of the seven,
-// where a large product reaches 1.22; without 1766 to 1790 us.  Documents in 4096
+// where a large product reaches 1.22; without 1747 to 1790 us.  Documents in 4096
 // rows 159 to 161 us; under the profiler prep takes 14 (a read of O and dO at the
 // card's rate), the main kernel 141 to 146 and the sum of parts 13.
 
@@ -203,11 +203,11 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
   using L = KvLayout<D>;
   using T = Staged<D>;
   constexpr int kRow = T::kRowBytes;
-  // dO V^T is held beside the scores, and P T' enters dS in float32 (3001 rows of 12
-  // heads 49 us, 52 with P T' in bf16).  At head dim 128 that spills 31 to 89
-  // registers: P T' waits for dO V^T in bf16 there, 2^-8 of it, and dK is off by
-  // 0.0029 of its norm instead of 0.0025 (as it is with 16 bits without a sign,
-  // which take 4 % longer).
+  // P T' enters dS in float32, so that dS is rounded once.  At head dim 64 dO V^T is
+  // held beside the scores.  At 128 that spills 31 to 89 registers: P goes into dV
+  // first there, and P T' waits for dO V^T in the scores' registers (8192 causal
+  // rows 2080 us, as with P T' in bf16, which left dK off by 0.0029 of its norm
+  // instead of 0.0025).
   constexpr bool kBoth = D == 64;
   int* s_flags = reinterpret_cast<int*>(smem + KvLayout<D>::kFlags);
   const ScoreTile& t = p.t;
@@ -456,52 +456,61 @@ __device__ __forceinline__ void dkdv_item(const ScoreBwdParams& p, char* smem,
               }
             }
             p4[i] = __builtin_convertvector(e4, bf16x4);
-            // Unpacked below instead of rounded again.
-            if (!kBoth) asm("" : "+v"(p4[i]));
-            if (CAP || kBoth) {
+            if (kBoth) {
               d4[i] = __builtin_convertvector(g4, bf16x4);
-              if (!kBoth) asm("" : "+v"(d4[i]));
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[i * 4 + e] = g4[e];
+              __builtin_amdgcn_sched_barrier(0);
             }
-            if (D == 128) __builtin_amdgcn_sched_barrier(0);
           }
+          auto joined = [](const bf16x4 (&f)[4], int hh) {
+            return __builtin_shufflevector(f[2 * hh], f[2 * hh + 1], 0, 1, 2, 3,
+                                           4, 5, 6, 7);
+          };
+          auto add = [&](int c, int hh, const bf16x4 (&f)[4], int tile,
+                         f32x16& acc) {
+            acc = mfma32(joined(f, hh),
+                         lds_tr(t0 ^ (64 * c), t1 ^ (64 * c),
+                                tile + (2 * qt + hh) * 16 * kRow),
+                         acc);
+          };
           if (!kBoth) {
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+              for (int hh = 0; hh < 2; ++hh)
+                add(c, hh, p4, L::kTile, acc_v[c]);
+            pipeline_reads<D / 16, 2, 2>();
             y = d_probs();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              f32x4 g4 = __builtin_convertvector(CAP ? d4[i] : p4[i], f32x4);
-              f32x4 z;
+              f32x4 g4;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) z[e] = y[i * 4 + e];
+              for (int e = 0; e < 4; ++e) g4[e] = x[i * 4 + e] * y[i * 4 + e];
               // A hidden pair's product with dO V^T is 0, whatever that is.
               if (__builtin_expect(fix, 0)) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  if (g4[e] == 0.f) z[e] = 0.f;
+                  if (x[i * 4 + e] == 0.f) g4[e] = 0.f;
               }
-#pragma unroll
-              for (int e = 0; e < 4; ++e) g4[e] *= z[e];
               d4[i] = __builtin_convertvector(g4, bf16x4);
-              __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+              for (int hh = 0; hh < 2; ++hh) add(c, hh, d4, 0, acc_k[c]);
+            pipeline_reads<D / 16, 2, 2>();
+          } else {
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+              for (int hh = 0; hh < 2; ++hh) {
+                add(c, hh, p4, L::kTile, acc_v[c]);
+                add(c, hh, d4, 0, acc_k[c]);
+              }
+            pipeline_reads<D / 8, 2, 2>();
           }
-          bf16x8 pf[2], ds[2];
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            pf[hh] = __builtin_shufflevector(p4[2 * hh], p4[2 * hh + 1], 0, 1,
-                                             2, 3, 4, 5, 6, 7);
-            ds[hh] = __builtin_shufflevector(d4[2 * hh], d4[2 * hh + 1], 0, 1,
-                                             2, 3, 4, 5, 6, 7);
-          }
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-              const uint32_t a0 = t0 ^ (64 * c), a1 = t1 ^ (64 * c);
-              const int at = (2 * qt + hh) * 16 * kRow;
-              acc_v[c] = mfma32(pf[hh], lds_tr(a0, a1, L::kTile + at), acc_v[c]);
-              acc_k[c] = mfma32(ds[hh], lds_tr(a0, a1, at), acc_k[c]);
-            }
-          pipeline_reads<D / 8, 2, 2>();
         }
       }
       if (nxt < 0) break;

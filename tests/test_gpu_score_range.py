@@ -286,3 +286,37 @@ def test_padding_in_front_of_a_request(window):
     b.check(b.run())
     o, lse = b.run()
     assert (o[:7] == 0).all() and torch.isneginf(lse[:, :7]).all()
+
+
+# -- how often the backward rounds -------------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap,slopes", [(0.0, False), (5.0, False),
+                                        (0.0, True), (300.0, True)])
+def test_the_scores_gradient_is_rounded_once(cap, slopes, d):
+    """dS enters its products rounded to bf16 once: an error of 2^-8 / sqrt(3) of
+    the last power of two, 0.54^(1/2) 2^-8 / sqrt(3) = 0.00166 of a value of any
+    size in the root mean square, each apart from the others.  dQ and dK in
+    float32 are then off by 0.00166 of the root of the sum of the squared terms; a
+    second rounding would make that 1.41 times as much."""
+    prob = problem(400, hq=2, hkv=1, d=d)
+    rule = make_rule(prob, [0], "causal", cap, slopes, 3)
+    q, k, v, do = (x.cuda() for x in tile_inputs(prob, [0], [0], 5))
+    want = Bounds(prob, [0], [0], rule, q, k, v)
+    o = torch.tensor(want.o).to(torch.bfloat16).cuda()
+    lse = torch.tensor(want.lse).float().cuda()
+    grads = run_backward(prob, [0], [0], on_gpu(rule), q, k, v, o, do, lse,
+                         grads=torch.float32)
+    q, k, v, o, do = (np64(x) for x in (q, k, v, o, do))
+    exact = os_.backward(prob, [0], [0], rule, q, k, v, o, np64(lse), do)
+    s, step = prob["softmax_scale"], 0.00166
+    own = [np.zeros(q.shape), np.zeros(k.shape)]
+    for h in range(2):
+        ds = s * want.p[h] * want.grad[h] * (
+            do[:, h] @ v[:, 0].T - np.sum(do[:, h] * o[:, h], 1)[:, None])
+        own[0][:, h] = ds ** 2 @ k[:, 0] ** 2
+        own[1][:, 0] += (ds ** 2).T @ q[:, h] ** 2
+    for name, got, x, e in zip(("dq", "dk"), grads, exact, own):
+        off = np.sqrt(np.sum((np64(got) - x) ** 2))
+        assert off < 1.2 * step * np.sqrt(np.sum(e)), (
+            name, off / (step * np.sqrt(np.sum(e))))
