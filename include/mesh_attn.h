@@ -695,10 +695,11 @@ ma_status_t mesh_attn_cache_score_fwd(
  *              mesh_attn_cache_append; not changed.
  *   slots, data  as there.
  * The rotated K goes from its angles in float64 to 4 bits without a rounding in
- * between, so that a stored value is the nearest to the exact one; values next to
- * the border of two may differ from those of the two calls, which round K to bf16
- * first.  rope->head_dim is the cache's; rows whose slot is out of range are
- * rotated, not stored. */
+ * between, so that a stored value is the nearest to the exact one (of angles off by
+ * 2^-34 turns at the farthest positions); values next to the border of two may
+ * differ from those of the two calls, which round K to bf16 first.
+ * rope->head_dim is the cache's; rows whose slot is out of range are rotated, not
+ * stored. */
 ma_status_t mesh_attn_cache_rope_append(
     const ma_cache_t* cache, const ma_rope_t* rope, int64_t rows,
     const int32_t* positions, int32_t q_heads, const void* q, int64_t q_stride,

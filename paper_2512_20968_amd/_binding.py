@@ -157,6 +157,7 @@ class Score(ctypes.Structure):
                 ("key_begin", ctypes.c_void_p),
                 ("key_end", ctypes.c_void_p)]
     ARRAYS = ("slopes", "key_begin", "key_end")
+    tensors = (None, None, None)
 
     def __init__(self, cap=0.0, slopes=None, key_begin=None, key_end=None):
         self.tensors = (slopes, key_begin, key_end)
