@@ -22,7 +22,7 @@
 // of 128, matrix unit busy 47 % of the time, vector unit 54 %): with a cap 2024 to
 // 2150 us, 0.64 to 0.68 PFLOP/s of the five products, 0.90 to 0.95 of the seven,
 // where a large product reaches 1.22; without 1747 to 1790 us.  Documents in 4096
-// rows 159 to 161 us; under the profiler prep takes 14 (a read of O and dO at the
+// rows 159 to 163 us; under the profiler prep takes 14 (a read of O and dO at the
 // card's rate), the main kernel 142 to 151 and the sum of parts 13.
 
 #include <hip/hip_runtime.h>
