@@ -1,6 +1,6 @@
 """Attention under a score rule at the ends of what its arguments may be, on the
 GPU: wide caps, positions that float32 does not hold, products that overflow,
-padding in front of a request."""
+padding in front of a request; and how often the backward rounds."""
 
 import numpy as np
 import pytest
